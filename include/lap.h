@@ -22,6 +22,8 @@
  *   lap_evaluate_weights  many weight vectors of the aggregated score (Section IV-C), each
  *                     walked to a limit and replayed: the overhead every vector would cause.
  *   lap_detect_iteration  finds one iteration in a recorded request stream (Section V).
+ *   lap_attention, lap_attention_grad, lap_attention_weights, lap_attention_step, lap_cache_evict, lap_cache_insert
+ *                     attention that stores no probabilities, and caches held to a number of slots (last section).
  *   lap_select_swaps  AutoSwap selection (Section IV-D): candidates taken in
  *                     priority order until the peak load is within a limit,
  *                     for several scores (SWDOA of Section IV-B (iv) among
@@ -76,7 +78,11 @@ enum {
     LAP_E_LINK = -5,       /* link_GBps <= 0, not finite, or rounds to 0 bytes per microsecond */
     LAP_E_TRACE = -6,      /* size 0, alloc >= free, free > n_steps, gap outside [alloc, free-1], step_ns 0 */
     LAP_E_RANGE = -7,      /* sum of sizes >= 2^63, a size >= 2^53, sum of step_ns >= 2^53, max size * n_steps >= 2^64 */
-    LAP_E_HIP = -8         /* a HIP runtime call or kernel launch failed */
+    LAP_E_HIP = -8,        /* a HIP runtime call or kernel launch failed */
+    LAP_E_ATTENTION = -9,  /* unknown element type, query heads no multiple of the key heads, scale not positive and
+                              finite, window without causal, a call's own rule on its shape broken, caches that differ */
+    LAP_E_LAYOUT = -10     /* rows not 16-byte aligned, head_dim no multiple of 8, a stride negative or no multiple of 8,
+                              a row stride of 2^24 or more, or an output whose rows overlap */
 };
 
 /* One training iteration's variable trace (Section III-A), structure of arrays. */
@@ -364,6 +370,99 @@ int lap_profile_ordering_ms(uint32_t n_vars, uint32_t n_steps, uint32_t B, const
  * Errors: LAP_E_NULL, LAP_E_SIZE (a zero count), LAP_E_WORKSPACE, LAP_E_HIP. */
 int lap_plan_pool_orders(uint32_t n_vars, uint32_t n_steps, uint32_t B, const void *ws, size_t ws_bytes,
                          void *hip_stream, uint32_t *orders);
+
+/* ---- Attention within a memory limit --------------------------------------------------------------------------------
+ *
+ * The largest variables of a transformer's iteration are attention's scores and probabilities (queries x keys of every
+ * head, kept from the forward to the backward pass); placement cannot remove them and swapping them is slow.  These calls
+ * compute attention and its gradient without ever storing them.  In serving, the variable that grows is the cache of keys
+ * and values; as swapping ranks variables by a score (Section IV-B) and walks them down to a limit (Section IV-D), a cache
+ * is held to a number of slots by the attention weight that every slot has received.
+ *
+ *   s_ij = scale q_i.k_j      lse_i = log sum_j exp(s_ij)      p_ij = exp(s_ij - lse_i)      o_i = sum_j p_ij v_j
+ *
+ * with j over the keys that row i sees.  Query head h uses key head h / (q_heads / kv_heads).
+ *   - q_lens[b], k_lens[b] (device, or NULL: all) are the rows in use of sequence b, clamped to 0 .. q_len, k_len; what
+ *     stands in memory after them is never read.  Queries are aligned to the end of the keys: row i stands at key
+ *     i + k_lens[b] - q_lens[b].
+ *   - causal: a row sees the keys up to where it stands; with window > 0 only the last `window` of those.
+ *   - A row that sees no key, and a row beyond its sequence's length, has o = 0, lse = minus infinity and gradients of 0.
+ *     A score below -1e30 / scale counts as hidden.  A value that is not finite in a row in use may reach every row of
+ *     its sequence that shares a tile with it.
+ * Sums, scores and probabilities are held in 32 bits; probabilities and their gradients are rounded to the element type
+ * where they enter the next product, results once when they are written.  Every sum has a fixed order: equal calls give
+ * equal bits.  Rows are [batch, heads, length, head_dim] by strides, which also serve [batch, length, heads, head_dim];
+ * inputs may be broadcast (stride 0).  Nothing is allocated, and all calls can be captured in a graph. */
+enum { LAP_T_BF16 = 0, LAP_T_F16 = 1 };      /* bfloat16, IEEE binary16 */
+#define LAP_MAX_HEAD_DIM 128u
+
+typedef struct {
+    void *data;                 /* device, 16-byte aligned */
+    int64_t batch, head, row;   /* strides in elements, multiples of 8, row < 2^24; head_dim elements lie side by side */
+} lap_rows;
+
+typedef struct {
+    uint32_t type;              /* LAP_T_* of all rows */
+    uint32_t batch, q_heads, kv_heads;
+    uint32_t q_len, k_len;      /* up to 2^30, may be 0 */
+    uint32_t head_dim;          /* multiple of 8 up to LAP_MAX_HEAD_DIM; sizes above 64 cost what 128 costs, others what 64 does */
+    uint32_t causal, window;    /* 0 or 1; 0: no window */
+    float scale;
+    const int32_t *q_lens, *k_lens;
+} lap_attention_shape;
+
+/* Bytes of workspace of a call with this shape, 256-byte aligned (0: ws may be NULL; also for a shape that is refused). */
+enum { LAP_AT_FORWARD = 0, LAP_AT_GRAD = 1, LAP_AT_WEIGHTS = 2, LAP_AT_STEP = 3 };
+size_t lap_attention_workspace_bytes(int which_call, const lap_attention_shape *shape);
+
+/* out, and lse [batch, q_heads, q_len], which the backward pass and lap_attention_weights take. */
+int lap_attention(const lap_attention_shape *shape, const lap_rows *q, const lap_rows *k, const lap_rows *v,
+                  const lap_rows *out, float *lse, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Gradients of q, k and v from dout, the gradient of out, with the out and lse of the forward call on the same shape.  A
+ * key head's gradients are summed over its query heads. */
+int lap_attention_grad(const lap_attention_shape *shape, const lap_rows *dout, const lap_rows *q, const lap_rows *k,
+                       const lap_rows *v, const lap_rows *out, const float *lse,
+                       const lap_rows *dq, const lap_rows *dk, const lap_rows *dv, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* weights[j] = before[j] + sum over the rows and query heads that see key j of p_ij, [batch, kv_heads, k_len]; before may
+ * be NULL (zeros) or weights itself. */
+int lap_attention_weights(const lap_attention_shape *shape, const lap_rows *q, const lap_rows *k, const float *lse,
+                          const float *before, float *weights, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* One new token of every sequence against its cache of k_len slots, in any order: shape with q_len 1, causal 0, q_lens
+ * NULL and up to 256 query heads to a key head; q and out: row unused.  A slot takes part if it is below k_lens[b] and, where positions [batch, kv_heads, k_len] is
+ * given, its position is not negative; what an empty slot holds does not matter.  weights as above, of this token alone;
+ * before and weights both NULL: not asked for.  lse [batch, q_heads]. */
+int lap_attention_step(const lap_attention_shape *shape, const lap_rows *q, const lap_rows *k, const lap_rows *v,
+                       const int32_t *positions, const float *before, const lap_rows *out, float *lse, float *weights,
+                       void *ws, size_t ws_bytes, void *hip_stream);
+
+/* A cache of one layer: `slots` places for every sequence and key head. */
+typedef struct {
+    uint32_t type, batch, kv_heads, slots, head_dim;      /* batch * kv_heads up to 65535 */
+    lap_rows k, v;
+    float *weights;         /* [batch, kv_heads, slots] weight received so far */
+    int32_t *positions;     /* [batch, kv_heads, slots] the token's place in its sequence, negative: empty.  As a source of
+                               lap_cache_evict NULL: a slot's own index */
+} lap_cache;
+
+size_t lap_cache_workspace_bytes(const lap_cache *to);
+
+/* The keep slots that stay of every sequence and head of `from` (a prompt, or a cache), in the order of their slots, into
+ * `to`, whose further slots are marked empty (rows and weights 0, position -1).  Of the slots below lens[b] (NULL: all) that
+ * are not empty those stay that hold the newest `recent` positions (position > newest - recent), then those of the highest
+ * weight, equal ones by lower slot; a weight that is not a number is below all others.  1 <= keep <= to->slots, recent <=
+ * keep.  lens_out [batch]: min(lens, keep).  The two caches have the same type and sizes but for slots, and do not overlap. */
+int lap_cache_evict(const lap_cache *from, const int32_t *lens, uint32_t keep, uint32_t recent, const lap_cache *to,
+                    int32_t *lens_out, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* One new token into every row of the cache: k_new and v_new (row unused) go, with weight 0 and position[b], into the lowest
+ * empty slot, or in place of the slot that an eviction of one would drop, that is, of those that are not among the newest
+ * `recent` (position > position[b] - recent; the new token is one of them) the one of least weight, the highest of equal
+ * ones.  A sequence with position[b] < 0 is left alone.  recent <= slots.  slots_out [batch, kv_heads]: the slot, or -1. */
+int lap_cache_insert(const lap_cache *cache, const lap_rows *k_new, const lap_rows *v_new, const int32_t *position,
+                     uint32_t recent, int32_t *slots_out, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -1,9 +1,9 @@
 """liblap: lifetime-aware memory-pool planning on MI355X (hand-written HIP, gfx950).
 
 Thin Python binding over the C-ABI library declared in include/lap.h.  PyTorch
-is used for device memory and streams only; every step of the planner runs in
-the library's kernels.  There is no CPU fallback: if liblap.so is missing or a
-call fails, an exception is raised.
+is used for device memory and streams only; every step of the planner and of
+the attention operators runs in the library's kernels.  There is no CPU
+fallback: if liblap.so is missing or a call fails, an exception is raised.
 """
 from .binding import (  # noqa: F401
     OPT_SEG_MIN_VARS,
@@ -31,6 +31,14 @@ from .binding import (  # noqa: F401
     status_string,
     validate_trace,
     workspace_bytes,
+)
+from .attention_ops import (  # noqa: F401
+    attention,
+    attention_grad,
+    attention_step,
+    attention_weights,
+    cache_evict,
+    cache_insert,
 )
 
 ORD_SIZE_DESC, ORD_LIFE_DESC, ORD_AREA_DESC, ORD_ALLOC_ASC, ORD_SEEDED, ORD_EXPLICIT, ORD_CLASS_SEEDED = range(7)

@@ -15,6 +15,8 @@ EXPORTS = [
     "lap_workspace_bytes", "lap_load_profile", "lap_load_profile_static", "lap_plan_pool", "lap_score_swaps", "lap_select_swaps",
     "lap_detect_iteration", "lap_schedule_swaps", "lap_simulate_swaps", "lap_evaluate_weights",
     "lap_validate_trace", "lap_status_string", "lap_profile_enable", "lap_profile_last_ms", "lap_profile_ordering_ms", "lap_plan_pool_orders", "lap_set_option",
+    "lap_attention_workspace_bytes", "lap_cache_workspace_bytes", "lap_attention", "lap_attention_grad", "lap_attention_weights",
+    "lap_attention_step", "lap_cache_evict", "lap_cache_insert",
 ]
 
 
@@ -99,6 +101,8 @@ def load_library():
     lib.lap_plan_pool_orders.restype = C.c_int
     lib.lap_plan_pool_orders.argtypes = [C.c_uint32, C.c_uint32, C.c_uint32, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
     lib.lap_profile_last_ms.argtypes = [C.c_int]
+    from . import attention_ops
+    attention_ops.declare(lib)
     _lib = lib
     return lib
 

@@ -292,6 +292,8 @@ const char *lap_status_string(int s)
     case LAP_E_TRACE: return "invalid trace content";
     case LAP_E_RANGE: return "trace values out of the supported range";
     case LAP_E_HIP: return "HIP runtime error";
+    case LAP_E_ATTENTION: return "bad attention type, heads, scale, mask or cache";
+    case LAP_E_LAYOUT: return "rows misaligned, overlapping or with unsupported strides";
     default: return "unknown status";
     }
 }

@@ -1,0 +1,145 @@
+// Attention of a training step or a prompt: o_i = sum_j p_ij v_j, p_ij = exp(scale q_i.k_j - lse_i), lse_i = the logarithm
+// of the sum of exp(scale q_i.k_j) over the keys that row i sees.
+//
+// One pass over the keys with a running maximum m and sum l for every row: a tile of keys gives s = K Q^T, p = 2^(c s - c m)
+// with c = scale log2(e), l += sum p, O^T += V^T P^T.  Nothing of the size queries x keys is ever stored.
+#include "attn_core.h"
+
+namespace lap {
+namespace {
+
+constexpr int KT = 64;      // keys of a tile
+
+template <class T, int DP, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnShape s, Rows q, Rows k, Rows v, Rows o, float *lse, uint32_t tiles)
+{
+    constexpr int BQ = 32 * NW;
+    __shared__ __align__(16) T lk[2][KT * DP];
+    __shared__ __align__(16) T lv[2][KT * DP];
+    uint32_t item;
+    if (!work_item(s.batch * s.q_heads * tiles, item)) return;
+    const uint32_t head = item / tiles, b = head / s.q_heads, h = head % s.q_heads;
+    const uint32_t kvh = h / (s.q_heads / s.kv_heads);
+    const int first = (int)(tiles - 1 - item % tiles) * BQ;      // the longest rows of a causal head first
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Span sp = span_of(s, b);
+
+    const int w0 = first + 32 * wave;               // this wave's rows
+    const int row = w0 + (lane & 31);
+    T *orow = (T *)o.data + (int64_t)b * o.batch + (int64_t)h * o.head + (int64_t)row * o.row;
+    float *lrow = lse + ((int64_t)b * s.q_heads + h) * s.q_len + row;
+
+    f32x16 acc[DP / 32] = {};
+    float m = LOWEST, l = 0.f;
+    const int end = min(first + BQ, sp.ql);         // rows in use
+    const int k0 = first < sp.ql ? key_lo(s, sp, first) / KT * KT : 0;
+    const int k1 = first < sp.ql ? key_hi(s, sp, end - 1) : 0;
+    if (k0 < k1) {
+        const int used = min(row, sp.ql - 1);       // padding takes the last row's part and is thrown away
+        typename Elem<T>::x8 qf[DP / 16];
+        load_kept<DP>(qf, (const T *)q.data + (int64_t)b * q.batch + (int64_t)h * q.head + (int64_t)used * q.row, s.head_dim, lane);
+        const int hi = key_hi(s, sp, used), lo = key_lo(s, sp, used);
+        const int w_last = min(w0 + 31, sp.ql - 1), w_first = min(w0, sp.ql - 1);
+        const int all_hi = key_hi(s, sp, w_first), all_lo = key_lo(s, sp, w_last);      // every row of the wave sees these
+        const int any_hi = key_hi(s, sp, w_last), any_lo = key_lo(s, sp, w_first);      // and some row these
+        const float c = s.scale * LOG2E;
+        const T *gk = (const T *)k.data + (int64_t)b * k.batch + (int64_t)kvh * k.head;
+        const T *gv = (const T *)v.data + (int64_t)b * v.batch + (int64_t)kvh * v.head;
+        const int last_chunk = (int)s.head_dim / 8 - 1;
+        const RowRead<DP, T> rows(lane);
+        const ColRead<DP, T> cols(lane);
+
+        const TileLoad<DP, KT, NW> tk(k.row, last_chunk, wave, lane), tv(v.row, last_chunk, wave, lane);
+        tk.issue(lk[0], gk, k0, sp.kl - 1, wave);
+        tv.issue(lv[0], gv, k0, sp.kl - 1, wave);
+        int buf = 0;
+        for (int kt = k0; kt < k1; kt += KT, buf ^= 1) {
+            tiles_arrive();
+            if (kt + KT < k1) {
+                tk.issue(lk[buf ^ 1], gk, kt + KT, sp.kl - 1, wave);
+                tv.issue(lv[buf ^ 1], gv, kt + KT, sp.kl - 1, wave);
+            }
+            if (kt >= any_hi || kt + KT <= any_lo) continue;
+            float p[2][16];
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                f32x16 x = {};
+#pragma unroll
+                for (int d = 0; d < DP / 16; ++d) x = Elem<T>::mfma(rows.get(lk[buf], kb, d), qf[d], x);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) p[kb][i] = x[i];
+            }
+            if (kt + KT > all_hi || kt < all_lo) {
+                const int at = kt + 4 * (lane >> 5);
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int key = at + 32 * kb + 8 * (i / 4) + i % 4;
+                        p[kb][i] = key < hi && key >= lo ? p[kb][i] : -ATTN_INF;
+                    }
+            }
+            float top = p[0][0];
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, p[kb][i]);
+            top = half_max(top);
+            if (__ballot(top > m)) {
+                const float up = fmaxf(m, top), by = exp2_fast((m - up) * c);
+                m = up;
+                l *= by;
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[d][i] *= by;
+            }
+            const float mc = m * c;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    p[kb][i] = exp2_fast(__builtin_fmaf(p[kb][i], c, -mc));
+                    l += p[kb][i];
+                }
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const auto pf = round8<T>(p[kb], 8 * t);
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d) acc[d] = Elem<T>::mfma(cols.get(lv[buf], 2 * kb + t, d), pf, acc[d]);
+                }
+        }
+    }
+    l = half_sum(l);
+    if (row < (int)s.q_len) {
+        const bool some = row < sp.ql && l != 0.f;      // (a sum that is not a number is some)
+        if (!some)
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) acc[d] = f32x16{};
+        store_kept<DP>(orow, acc, some ? 1.f / l : 0.f, s.head_dim, lane);
+        if (lane < 32) *lrow = some ? m * s.scale + __logf(l) : -ATTN_INF;
+    }
+}
+
+template <class T, int DP>
+hipError_t launch(const AttnShape &s, const Rows &q, const Rows &k, const Rows &v, const Rows &out, float *lse, hipStream_t st)
+{
+    constexpr int NW = 4;
+    const uint32_t tiles = (s.q_len + 32 * NW - 1) / (32 * NW);
+    const uint32_t total = s.batch * s.q_heads * tiles;
+    k_attention<T, DP, NW><<<(total + 7) / 8 * 8, NW * 64, 0, st>>>(s, q, k, v, out, lse, tiles);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attention(const AttnShape &s, const Rows &q, const Rows &k, const Rows &v, const Rows &out, float *lse, hipStream_t st)
+{
+    if (s.half)
+        return s.head_dim <= 64 ? launch<_Float16, 64>(s, q, k, v, out, lse, st) : launch<_Float16, 128>(s, q, k, v, out, lse, st);
+    return s.head_dim <= 64 ? launch<__bf16, 64>(s, q, k, v, out, lse, st) : launch<__bf16, 128>(s, q, k, v, out, lse, st);
+}
+
+}  // namespace lap

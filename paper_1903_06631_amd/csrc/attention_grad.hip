@@ -1,0 +1,240 @@
+// Attention's backward pass.  With p_ij = exp(scale q_i.k_j - lse_i) computed again from the rows and the forward pass's
+// sums, g_i the gradient of o_i and delta_i = g_i.o_i:
+//   dv_j = sum_i p_ij g_i      ds_ij = p_ij (g_i.v_j - delta_i)      dq_i = scale sum_j ds_ij k_j      dk_j = scale sum_i ds_ij q_i
+//
+// Two kernels, each with its sums in registers from the first product to the last, added in a fixed order: one keeps
+// query rows and streams keys (dq; it also leaves delta and the sums in base 2 in the workspace), the other keeps keys and
+// streams the rows of every query head that shares them (dk and dv).  Scores and g.v are computed in both, seven products
+// in place of five: the price for results that do not depend on the order in which workgroups finish.
+#include "attn_core.h"
+
+namespace lap {
+namespace {
+
+constexpr int KT = 64;      // keys of a tile of the first kernel
+constexpr int QT = 32;      // rows of a tile of the second
+
+template <class T, int DP, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void k_attention_dq(AttnShape s, Rows g, Rows q, Rows k, Rows v, Rows o, const float *lse,
+                                                          Rows dq, float2 *stats, uint32_t tiles)
+{
+    constexpr int BQ = 32 * NW;
+    __shared__ __align__(16) T lk[2][KT * DP];
+    __shared__ __align__(16) T lv[2][KT * DP];
+    uint32_t item;
+    if (!work_item(s.batch * s.q_heads * tiles, item)) return;
+    const uint32_t head = item / tiles, b = head / s.q_heads, h = head % s.q_heads;
+    const uint32_t kvh = h / (s.q_heads / s.kv_heads);
+    const int first = (int)(tiles - 1 - item % tiles) * BQ;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Span sp = span_of(s, b);
+
+    const int w0 = first + 32 * wave;
+    const int row = w0 + (lane & 31);
+    T *drow = (T *)dq.data + (int64_t)b * dq.batch + (int64_t)h * dq.head + (int64_t)row * dq.row;
+    const int64_t at = ((int64_t)b * s.q_heads + h) * s.q_len;
+
+    f32x16 acc[DP / 32] = {};
+    const int end = min(first + BQ, sp.ql);
+    const int k0 = first < sp.ql ? key_lo(s, sp, first) / KT * KT : 0;
+    const int k1 = first < sp.ql ? key_hi(s, sp, end - 1) : 0;
+    if (first < sp.ql) {
+        const int used = min(row, sp.ql - 1);
+        typename Elem<T>::x8 qf[DP / 16], gf[DP / 16];
+        load_kept<DP>(qf, (const T *)q.data + (int64_t)b * q.batch + (int64_t)h * q.head + (int64_t)used * q.row, s.head_dim, lane);
+        load_kept<DP>(gf, (const T *)g.data + (int64_t)b * g.batch + (int64_t)h * g.head + (int64_t)used * g.row, s.head_dim, lane);
+        float delta = 0.f;
+        {
+            typename Elem<T>::x8 of[DP / 16];
+            load_kept<DP>(of, (const T *)o.data + (int64_t)b * o.batch + (int64_t)h * o.head + (int64_t)used * o.row, s.head_dim, lane);
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) delta = __builtin_fmaf((float)gf[d][j], (float)of[d][j], delta);
+            delta = half_sum(delta);
+        }
+        // a row without keys gets probabilities of zero
+        const float sum = lse[at + used], l2 = sum == -ATTN_INF ? ATTN_INF : sum * LOG2E;
+        if (row < sp.ql && lane < 32) stats[at + row] = make_float2(l2, delta);
+
+        if (k0 < k1) {
+            const int hi = key_hi(s, sp, used), lo = key_lo(s, sp, used);
+            const int w_last = min(w0 + 31, sp.ql - 1), w_first = min(w0, sp.ql - 1);
+            const int all_hi = key_hi(s, sp, w_first), all_lo = key_lo(s, sp, w_last);
+            const int any_hi = key_hi(s, sp, w_last), any_lo = key_lo(s, sp, w_first);
+            const float c = s.scale * LOG2E;
+            const T *gk = (const T *)k.data + (int64_t)b * k.batch + (int64_t)kvh * k.head;
+            const T *gv = (const T *)v.data + (int64_t)b * v.batch + (int64_t)kvh * v.head;
+            const int last_chunk = (int)s.head_dim / 8 - 1;
+            const RowRead<DP, T> rows(lane);
+            const ColRead<DP, T> cols(lane);
+            const TileLoad<DP, KT, NW> tk(k.row, last_chunk, wave, lane), tv(v.row, last_chunk, wave, lane);
+            tk.issue(lk[0], gk, k0, sp.kl - 1, wave);
+            tv.issue(lv[0], gv, k0, sp.kl - 1, wave);
+            int buf = 0;
+            for (int kt = k0; kt < k1; kt += KT, buf ^= 1) {
+                tiles_arrive();
+                if (kt + KT < k1) {
+                    tk.issue(lk[buf ^ 1], gk, kt + KT, sp.kl - 1, wave);
+                    tv.issue(lv[buf ^ 1], gv, kt + KT, sp.kl - 1, wave);
+                }
+                if (kt >= any_hi || kt + KT <= any_lo) continue;
+                const bool whole = kt + KT <= all_hi && kt >= all_lo;
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    f32x16 x = {}, y = {};
+#pragma unroll
+                    for (int d = 0; d < DP / 16; ++d) x = Elem<T>::mfma(rows.get(lk[buf], kb, d), qf[d], x);
+#pragma unroll
+                    for (int d = 0; d < DP / 16; ++d) y = Elem<T>::mfma(rows.get(lv[buf], kb, d), gf[d], y);
+                    float ds[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) ds[i] = exp2_fast(__builtin_fmaf(x[i], c, -l2)) * (y[i] - delta);
+                    if (!whole) {
+                        const int key0 = kt + 4 * (lane >> 5) + 32 * kb;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int key = key0 + 8 * (i / 4) + i % 4;
+                            ds[i] = key < hi && key >= lo ? ds[i] : 0.f;
+                        }
+                    }
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        const auto df = round8<T>(ds, 8 * t);
+#pragma unroll
+                        for (int d = 0; d < DP / 32; ++d) acc[d] = Elem<T>::mfma(cols.get(lk[buf], 2 * kb + t, d), df, acc[d]);
+                    }
+                }
+            }
+        }
+    }
+    if (row < (int)s.q_len) {
+        if (row >= sp.ql)
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) acc[d] = f32x16{};
+        store_kept<DP>(drow, acc, s.scale, s.head_dim, lane);
+    }
+}
+
+template <class T, int DP, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void k_attention_dkv(AttnShape s, Rows g, Rows q, Rows k, Rows v, const float2 *stats, Rows dk,
+                                                           Rows dv, uint32_t tiles)
+{
+    constexpr int BK = 32 * NW;
+    __shared__ __align__(16) T lq[2][QT * DP];
+    __shared__ __align__(16) T lg[2][QT * DP];
+    __shared__ __align__(16) float2 lst[2][QT];
+    uint32_t item;
+    if (!work_item(s.batch * s.kv_heads * tiles, item)) return;
+    const uint32_t head = item / tiles, b = head / s.kv_heads, kvh = head % s.kv_heads;
+    const int first = (int)(item % tiles) * BK;      // the first keys of a causal head are seen by the most rows
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Span sp = span_of(s, b);
+    const uint32_t group = s.q_heads / s.kv_heads;
+
+    const int w0 = first + 32 * wave;
+    const int key = w0 + (lane & 31);
+    f32x16 ak[DP / 32] = {}, av[DP / 32] = {};
+    const int end = min(first + BK, sp.kl);
+    const int r0 = first < sp.kl ? row_lo(s, sp, first) / QT * QT : 0;
+    const int r1 = first < sp.kl ? row_hi(s, sp, end - 1) : 0;
+    if (r0 < r1) {
+        const int used = min(key, sp.kl - 1);
+        typename Elem<T>::x8 kf[DP / 16], vf[DP / 16];
+        load_kept<DP>(kf, (const T *)k.data + (int64_t)b * k.batch + (int64_t)kvh * k.head + (int64_t)used * k.row, s.head_dim, lane);
+        load_kept<DP>(vf, (const T *)v.data + (int64_t)b * v.batch + (int64_t)kvh * v.head + (int64_t)used * v.row, s.head_dim, lane);
+        const int hi = row_hi(s, sp, used), lo = row_lo(s, sp, used);
+        const int w_last = min(w0 + 31, sp.kl - 1), w_first = min(w0, sp.kl - 1);
+        const int all_hi = row_hi(s, sp, w_first), all_lo = row_lo(s, sp, w_last);
+        const int any_hi = row_hi(s, sp, w_last), any_lo = row_lo(s, sp, w_first);
+        const float c = s.scale * LOG2E;
+        const int last_chunk = (int)s.head_dim / 8 - 1;
+        const RowRead<DP, T> rows(lane);
+        const ColRead<DP, T> cols(lane);
+        const TileLoad<DP, QT, NW> tq(q.row, last_chunk, wave, lane), tg(g.row, last_chunk, wave, lane);
+        const int per = (r1 - r0 + QT - 1) / QT, count = per * (int)group;
+        const T *gq = (const T *)q.data + (int64_t)b * q.batch + (int64_t)kvh * group * q.head;
+        const T *gg = (const T *)g.data + (int64_t)b * g.batch + (int64_t)kvh * group * g.head;
+        const float2 *gs = stats + ((int64_t)b * s.q_heads + (int64_t)kvh * group) * s.q_len;
+        int next = r0;      // rows and head of the next tile to ask for
+        auto issue = [&](int to) {
+            tq.issue(lq[to], gq, next, sp.ql - 1, wave);
+            tg.issue(lg[to], gg, next, sp.ql - 1, wave);
+            if (wave == 0 && lane < QT) lst[to][lane] = gs[min(next + lane, sp.ql - 1)];
+            next += QT;
+            if (next >= r1) next = r0, gq += q.head, gg += g.head, gs += s.q_len;
+        };
+        issue(0);
+        int buf = 0, qt = r0;
+        for (int n = 0; n < count; ++n, buf ^= 1) {
+            tiles_arrive();
+            if (n + 1 < count) issue(buf ^ 1);
+            const int at = qt;
+            qt = qt + QT >= r1 ? r0 : qt + QT;
+            if (at >= any_hi || at + QT <= any_lo) continue;
+            f32x16 x = {}, y = {};
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d) x = Elem<T>::mfma(rows.get(lq[buf], 0, d), kf[d], x);
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d) y = Elem<T>::mfma(rows.get(lg[buf], 0, d), vf[d], y);
+            float p[16], ds[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float2 st = lst[buf][8 * (i / 4) + 4 * (lane >> 5) + i % 4];
+                p[i] = exp2_fast(__builtin_fmaf(x[i], c, -st.x));
+                ds[i] = p[i] * (y[i] - st.y);
+            }
+            if (at + QT > all_hi || at < all_lo) {
+                const int row0 = at + 4 * (lane >> 5);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int row = row0 + 8 * (i / 4) + i % 4;
+                    const bool in = row < hi && row >= lo;
+                    p[i] = in ? p[i] : 0.f;
+                    ds[i] = in ? ds[i] : 0.f;
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const auto pf = round8<T>(p, 8 * t), df = round8<T>(ds, 8 * t);
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d) {
+                    av[d] = Elem<T>::mfma(cols.get(lg[buf], t, d), pf, av[d]);
+                    ak[d] = Elem<T>::mfma(cols.get(lq[buf], t, d), df, ak[d]);
+                }
+            }
+        }
+    }
+    if (key < (int)s.k_len) {
+        if (key >= sp.kl)
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) ak[d] = av[d] = f32x16{};
+        store_kept<DP>((T *)dk.data + (int64_t)b * dk.batch + (int64_t)kvh * dk.head + (int64_t)key * dk.row, ak, s.scale, s.head_dim, lane);
+        store_kept<DP>((T *)dv.data + (int64_t)b * dv.batch + (int64_t)kvh * dv.head + (int64_t)key * dv.row, av, 1.f, s.head_dim, lane);
+    }
+}
+
+template <class T, int DP>
+hipError_t launch(const AttnShape &s, const AttnGrad &a, hipStream_t st)
+{
+    constexpr int NW = 4;
+    const uint32_t qtiles = (s.q_len + 32 * NW - 1) / (32 * NW), qtotal = s.batch * s.q_heads * qtiles;
+    const uint32_t ktiles = (s.k_len + 32 * NW - 1) / (32 * NW), ktotal = s.batch * s.kv_heads * ktiles;
+    if (qtotal) {
+        k_attention_dq<T, DP, NW><<<(qtotal + 7) / 8 * 8, NW * 64, 0, st>>>(s, a.g, a.q, a.k, a.v, a.out, a.lse, a.dq, a.stats, qtiles);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (ktotal) k_attention_dkv<T, DP, NW><<<(ktotal + 7) / 8 * 8, NW * 64, 0, st>>>(s, a.g, a.q, a.k, a.v, a.stats, a.dk, a.dv, ktiles);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attention_grad(const AttnShape &s, const AttnGrad &a, hipStream_t st)
+{
+    if (s.half) return s.head_dim <= 64 ? launch<_Float16, 64>(s, a, st) : launch<_Float16, 128>(s, a, st);
+    return s.head_dim <= 64 ? launch<__bf16, 64>(s, a, st) : launch<__bf16, 128>(s, a, st);
+}
+
+}  // namespace lap

@@ -1,0 +1,234 @@
+// Attention of one new token of every sequence over its cache, and the weight that every slot receives from it:
+//   o = sum_j p_j v_j, p_j = exp(scale q.k_j - lse), over the slots in use; w_j += sum of p_j over the heads that share slot j
+//
+// Every key and value is read once and takes part in a few products only: the pass is bound by memory, and there are few
+// sequences and heads to share it out to.  So the slots are cut into chunks of STEP_CHUNK or so, a workgroup each.  Its four
+// waves go through 32 slots at a time of their own, without waiting for each other: keys from memory straight into
+// registers as a matrix operand, values through LDS, which is where they are transposed.  The heads of a group are the
+// kept rows (up to 32; with fewer, part of the matrix instructions runs empty, at a rate that is far from binding).  A
+// second kernel joins the chunks' sums and outputs; the weights need the joined sums, so the first one leaves the scores
+// (4 bytes for each slot and head beside the slot's 4 head_dim).
+#include "attn_core.h"
+
+namespace lap {
+namespace {
+
+constexpr int NW = 4, TS = 32;      // waves, slots of a wave's tile
+
+template <class T, int DP>
+__global__ __launch_bounds__(NW * 64, 2) void k_step(StepShape s, StepWork w)
+{
+    __shared__ __align__(16) char raw[NW * 2 * TS * DP * sizeof(T)];      // the waves' values; their outputs at the end
+    __shared__ float2 sums[NW][32];
+    T *const lv = (T *)raw;
+    const uint32_t group = s.q_heads / s.kv_heads, parts = (group + 31) / 32;
+    const uint32_t split = blockIdx.x, kvh = blockIdx.y / parts, part = blockIdx.y % parts, b = blockIdx.z;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+    const int n_rows = min(32, (int)(group - part * 32));
+    const uint32_t head0 = kvh * group + part * 32;
+    const int len = clamp_len(s.lens, b, s.slots);
+    const int c0 = split * s.chunk, c1 = min(c0 + (int)s.chunk, len);
+
+    const int r = lane & 31;
+    typename Elem<T>::x8 qf[DP / 16], kf[DP / 16];
+    load_kept<DP>(qf, (const T *)w.q.data + (int64_t)b * w.q.batch + (int64_t)(head0 + min(r, n_rows - 1)) * w.q.head, s.head_dim, lane);
+    const T *gk = (const T *)w.k.data + (int64_t)b * w.k.batch + (int64_t)kvh * w.k.head;
+    const T *gv = (const T *)w.v.data + (int64_t)b * w.v.batch + (int64_t)kvh * w.v.head;
+    const int32_t *pos = w.positions ? w.positions + ((int64_t)b * s.kv_heads + kvh) * s.slots : nullptr;
+    float *scores = w.scores ? w.scores + ((int64_t)b * s.q_heads + head0 + r) * s.score_row : nullptr;
+    const float c = s.scale * LOG2E;
+    const ColRead<DP, T> cols(lane);
+    const TileLoad<DP, TS, 1> tv(w.v.row, (int)s.head_dim / 8 - 1, 0, lane);
+    T *const mine = lv + wave * 2 * TS * DP;
+
+    f32x16 acc[DP / 32] = {};
+    float m = LOWEST, l = 0.f;
+    const auto fetch = [&](int at, int to) {      // slots at .. at + 31
+        tv.issue(mine + to * TS * DP, gv, at, len - 1, 0);
+        load_kept<DP>(kf, gk + (int64_t)min(at + r, len - 1) * w.k.row, s.head_dim, lane);
+    };
+    int at = c0 + wave * TS, buf = 0;
+    if (at < c1) fetch(at, 0);
+    for (; at < c1; at += NW * TS, buf ^= 1) {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070);      // this wave's keys and values are here
+        asm volatile("" ::: "memory");
+        f32x16 x = {};
+#pragma unroll
+        for (int d = 0; d < DP / 16; ++d) x = Elem<T>::mfma(kf[d], qf[d], x);
+        const int32_t held = pos ? pos[min(at + r, len - 1)] : 0;
+        if (at + NW * TS < c1) fetch(at + NW * TS, buf ^ 1);
+        float p[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[i] = x[i] * c;
+        const uint32_t live = (uint32_t)__ballot(at + r < len && held >= 0);      // one bit for each slot of the tile
+        if (live != ~0u) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) p[i] = (live >> (8 * (i / 4) + 4 * h + i % 4)) & 1 ? p[i] : -ATTN_INF;
+            if (pos) {      // what an empty slot holds may be anything, and zero times it is not always zero
+                for (int n = lane; n < TS * DP / 8; n += 64)
+                    if (!((live >> (n / (DP / 8))) & 1)) ((s16x8 *)(mine + buf * TS * DP))[n] = s16x8{};
+            }
+        }
+        if (scores && r < n_rows) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) *(f32x4 *)(scores + at + 2 * i + 4 * h) = f32x4{p[i], p[i + 1], p[i + 2], p[i + 3]};
+        }
+        float top = p[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, p[i]);
+        top = half_max(top);
+        if (__ballot(top > m)) {
+            const float up = fmaxf(m, top), by = exp2_fast(m - up);
+            m = up;
+            l *= by;
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[d][i] *= by;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            p[i] = exp2_fast(p[i] - m);
+            l += p[i];
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const auto pf = round8<T>(p, 8 * t);
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) acc[d] = Elem<T>::mfma(cols.get(mine + buf * TS * DP, t, d), pf, acc[d]);
+        }
+    }
+    // join the waves: their sums, then their outputs, each on the workgroup's maximum
+    l = half_sum(l);
+    if (lane < 32) sums[wave][r] = make_float2(m, l);
+    __syncthreads();
+    float top = sums[0][r].x;
+    for (int i = 1; i < NW; ++i) top = fmaxf(top, sums[i][r].x);
+    const float by = exp2_fast(m - top);
+    float *out = (float *)raw;      // [row][wave][DP]
+    static_assert(2 * TS * sizeof(T) >= 32 * sizeof(float), "the outputs fit where the values were");
+    if (r < n_rows)
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                f32x4 y;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = acc[d][i + j] * by;
+                *(f32x4 *)(out + (r * NW + wave) * DP + 32 * d + 2 * i + 4 * h) = y;
+            }
+    __syncthreads();
+    for (int n = threadIdx.x; n < n_rows * (DP / 4); n += NW * 64) {
+        const int row = n / (DP / 4), e = n % (DP / 4) * 4;
+        f32x4 y = *(f32x4 *)(out + row * NW * DP + e);
+        for (int i = 1; i < NW; ++i) y += *(f32x4 *)(out + (row * NW + i) * DP + e);
+        *(f32x4 *)(w.outs + (((int64_t)b * s.q_heads + head0 + row) * s.splits + split) * DP + e) = y;
+    }
+    if (wave == 0 && lane < n_rows) {
+        float total = 0.f;
+        for (int i = 0; i < NW; ++i) total += sums[i][lane].y * exp2_fast(sums[i][lane].x - top);
+        w.sums[((int64_t)b * s.q_heads + head0 + lane) * s.splits + split] = make_float2(top, total);
+    }
+}
+
+constexpr int JOIN = 256, JOIN_SLOTS = 1024;
+
+// maximum and sum of a head over its chunks, by a wave
+__device__ __forceinline__ float2 join_sums(const float2 *sums, uint32_t n, int lane)
+{
+    float m = LOWEST;
+    for (uint32_t i = lane; i < n; i += 64) m = fmaxf(m, sums[i].x);
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+    float l = 0.f;
+    for (uint32_t i = lane; i < n; i += 64) l += sums[i].y * exp2_fast(sums[i].x - m);
+    for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d, 64);
+    return make_float2(m, l);
+}
+
+// The first batch * q_heads workgroups join the outputs of a head each, the others add the weights of JOIN_SLOTS slots.
+template <class T, int DP> __global__ __launch_bounds__(JOIN) void k_step_join(StepShape s, StepWork w, uint32_t pieces)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t heads = s.batch * s.q_heads;
+    if (blockIdx.x < heads) {
+        constexpr int ACROSS = DP / 4, LANES = JOIN / ACROSS;      // threads of a row, rows at a time
+        __shared__ f32x4 part[LANES][ACROSS];
+        const uint32_t b = blockIdx.x / s.q_heads, head = blockIdx.x % s.q_heads;
+        const float2 *sums = w.sums + (int64_t)blockIdx.x * s.splits;
+        const float2 all = join_sums(sums, s.splits, lane);
+        const int e = threadIdx.x % ACROSS, first = threadIdx.x / ACROSS;
+        f32x4 y = {};
+        const f32x4 *outs = (const f32x4 *)(w.outs + (int64_t)blockIdx.x * s.splits * DP);
+#pragma unroll 4
+        for (uint32_t i = first; i < s.splits; i += LANES) {
+            // a chunk without slots has written zeros
+            y += outs[(int64_t)i * ACROSS + e] * exp2_fast(sums[i].x - all.x);
+        }
+        part[first][e] = y;
+        __syncthreads();
+        if (first == 0) {
+            for (int i = 1; i < LANES; ++i) y += part[i][e];
+            const bool some = all.y != 0.f;
+            typename Elem<T>::x4 z;
+            for (int j = 0; j < 4; ++j) z[j] = (T)(some ? y[j] / all.y : 0.f);
+            if (e * 4 < (int)s.head_dim) *(typename Elem<T>::x4 *)((T *)w.out.data + (int64_t)b * w.out.batch + (int64_t)head * w.out.head + e * 4) = z;
+            if (threadIdx.x == 0) w.lse[blockIdx.x] = some ? all.x * LN2 + __logf(all.y) : -ATTN_INF;
+        }
+        return;
+    }
+    __shared__ float l2[MAX_GROUP];
+    const uint32_t group = s.q_heads / s.kv_heads;
+    const uint32_t item = (blockIdx.x - heads) / pieces, piece = (blockIdx.x - heads) % pieces;
+    const uint32_t b = item / s.kv_heads, head0 = b * s.q_heads + item % s.kv_heads * group;
+    for (uint32_t g = wave; g < group; g += JOIN / 64) {
+        const float2 all = join_sums(w.sums + (int64_t)(head0 + g) * s.splits, s.splits, lane);
+        if (lane == 0) l2[g] = all.y != 0.f ? all.x + __log2f(all.y) : ATTN_INF;
+    }
+    __syncthreads();
+    const int len = clamp_len(s.lens, b, s.slots);
+    for (uint32_t i = 0; i < JOIN_SLOTS; i += JOIN) {
+        const uint32_t slot = piece * JOIN_SLOTS + i + threadIdx.x;
+        if (slot >= s.slots) return;
+        float sum = 0.f;
+        if ((int)slot < len)
+            for (uint32_t g = 0; g < group; ++g) sum += exp2_fast(w.scores[(int64_t)(head0 + g) * s.score_row + slot] - l2[g]);
+        const int64_t at = (int64_t)item * s.slots + slot;
+        w.weights[at] = w.before[at] + sum;
+    }
+}
+
+template <class T, int DP> hipError_t launch(const StepShape &s, const StepWork &w, hipStream_t st)
+{
+    const uint32_t parts = (s.q_heads / s.kv_heads + 31) / 32;
+    k_step<T, DP><<<dim3(s.splits, s.kv_heads * parts, s.batch), NW * 64, 0, st>>>(s, w);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const uint32_t pieces = w.weights ? (s.slots + JOIN_SLOTS - 1) / JOIN_SLOTS : 0;
+    k_step_join<T, DP><<<s.batch * (s.q_heads + s.kv_heads * pieces), JOIN, 0, st>>>(s, w, pieces);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// Chunks: 2 workgroups fit a compute unit and 8 of them each keep the chip evenly loaded to the end, but a chunk is at
+// least one tile for every wave and no more than STEP_CHUNK slots are worth it.
+void step_split(StepShape &s)
+{
+    const uint64_t rows = (uint64_t)s.batch * s.kv_heads * ((s.q_heads / s.kv_heads + 31) / 32);
+    const uint64_t least = NW * TS, most = 512;
+    const uint64_t want = (uint64_t)s.slots * rows / 4096;
+    const uint64_t chunk = (want < least ? least : want > most ? most : want) / least * least;
+    s.chunk = (uint32_t)chunk;
+    s.splits = (uint32_t)((s.slots + chunk - 1) / chunk);
+    if (!s.splits) s.splits = 1;
+    s.score_row = ((uint64_t)s.slots + TS - 1) / TS * TS;
+}
+
+hipError_t launch_attention_step(const StepShape &s, const StepWork &w, hipStream_t st)
+{
+    if (s.half) return s.head_dim <= 64 ? launch<_Float16, 64>(s, w, st) : launch<_Float16, 128>(s, w, st);
+    return s.head_dim <= 64 ? launch<__bf16, 64>(s, w, st) : launch<__bf16, 128>(s, w, st);
+}
+
+}  // namespace lap

@@ -1,0 +1,228 @@
+// What the attention kernels share: element types, tiles of rows in LDS, matrix operands out of them, visible ranges.
+//
+// All products go through the 32x32x16 matrix instruction (C = A B, lane l with h = l / 32):
+//   A: row l % 32, contraction indices 8 h .. 8 h + 7          B: column l % 32, the same contraction indices
+//   C: column l % 32, element i of 16 is row 8 (i / 4) + 4 h + i % 4
+// Scores are computed with the side that a wave keeps in registers as B, so a lane holds scores of one kept row only, 16
+// of every 32 of the streamed rows.  Those 16, rounded and in order, are the B operand of the next product over the
+// streamed rows (elements 8 s .. 8 s + 7 for its step s), if its A operand takes the streamed rows in the order
+// 4 h .. 4 h + 3, 8 + 4 h .. 8 + 4 h + 3: the transposing LDS read fetches four rows at a time, from anywhere, so the
+// order costs nothing and no lane has to pass anything on.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "attn_kernels.h"
+
+namespace lap {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+#define ATTN_LDS __attribute__((address_space(3)))
+#define ATTN_GLB __attribute__((address_space(1)))
+
+template <class T> struct Elem;
+template <> struct Elem<__bf16> {
+    typedef __bf16 x8 __attribute__((ext_vector_type(8)));
+    typedef __bf16 x4 __attribute__((ext_vector_type(4)));
+    static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Elem<_Float16> {
+    typedef _Float16 x8 __attribute__((ext_vector_type(8)));
+    typedef _Float16 x4 __attribute__((ext_vector_type(4)));
+    static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LN2 = 0.6931471805599453f;
+constexpr float LOWEST = -1e30f;      // running maximum of a row that has seen no key
+#define ATTN_INF __builtin_inff()
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// the larger of a lane's value and its partner's in the other half of the wave (and the same for a sum)
+__device__ __forceinline__ float half_max(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Rows in LDS: DP elements (DP / 8 chunks of 16 bytes) one after the other, chunk c of row r at place c ^ swz(r).  Eight
+// rows that follow each other, read at one chunk, and four rows read at two neighbouring chunks, then come from eight
+// different places: neither kind of read below has conflicts.
+__device__ __forceinline__ int swz(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
+
+// ROWS rows from global memory into LDS, asynchronously, by NW waves.  Rows past `last` are copies of it and chunks past
+// the last one of a row copies of that one: padding is never read, and what stands in its place is part of the same row.
+// The compiler does not see these loads: it would wait for the ones just sent off before any read of LDS, as it cannot
+// tell the tiles apart.  tiles_arrive() waits for them.
+template <int DP, int ROWS, int NW> struct TileLoad {
+    static constexpr int CH = DP / 8, PER = ROWS * CH / 64 / NW;      // chunks of a row, instructions of a wave
+    static_assert(PER * 64 * NW == ROWS * CH, "whole instructions");
+    uint32_t off[PER];      // this lane's bytes of a whole tile
+    uint32_t stride;        // bytes of a row (at most 2^25: 64 rows stay within 32 bits)
+    int row0;
+    __device__ __forceinline__ static int chunk(int j, int lane, int wave, int last_chunk)
+    {
+        return min((lane % CH) ^ swz((wave * PER + j) * 64 / CH + lane / CH), last_chunk);
+    }
+    __device__ __forceinline__ TileLoad(int64_t row_stride, int last_chunk, int wave, int lane)
+    {
+        stride = (uint32_t)row_stride * 2u;
+        row0 = wave * PER * 64 / CH + lane / CH;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) off[j] = (uint32_t)(row0 + j * (64 / CH)) * stride + (uint32_t)chunk(j, lane, wave, last_chunk) * 16u;
+    }
+    // rows first .. first + ROWS - 1 of g; first <= last
+    template <class T> __device__ __forceinline__ void issue(T *lds, const T *g, int first, int last, int wave) const
+    {
+        const char *base = (const char *)g + (int64_t)first * stride;
+        const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(ATTN_LDS void *)lds + (uint32_t)(wave * PER * 1024));
+        const int left = last - first;
+        if (left >= ROWS - 1) {
+#pragma unroll
+            for (int j = 0; j < PER; ++j) send(to + j * 1024u, off[j], base);
+        } else {
+#pragma unroll
+            for (int j = 0; j < PER; ++j) send(to + j * 1024u, off[j] - (uint32_t)max(0, row0 + j * (64 / CH) - left) * stride, base);
+        }
+    }
+    // 16 bytes for every lane, from base + its offset, to LDS address `to` + 16 times the lane (the register that holds
+    // that address is not the compiler's to use)
+    static __device__ __forceinline__ void send(uint32_t to, uint32_t offset, const char *base)
+    {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+    }
+};
+
+// what has been asked for has arrived in LDS, for every wave, and every wave is done with what it has read there
+__device__ __forceinline__ void tiles_arrive()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);      // no memory or LDS access under way
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Operands out of a tile.  RowRead: A of a product over the elements of a row (lane l: row l % 32 of a block of 32).
+// The place of a chunk is an exclusive or; its two low bits are worked out once, the rest is an offset.
+template <int DP, class T> struct RowRead {
+    int at[4];
+    __device__ __forceinline__ explicit RowRead(int lane)
+    {
+        const int r = lane & 31, h = lane >> 5;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) at[k] = r * DP + (((2 * k) | h) ^ swz(r)) * 8;
+    }
+    // elements 16 k + 8 h .. of rows 32 block ..
+    __device__ __forceinline__ typename Elem<T>::x8 get(const T *tile, int block, int k) const
+    {
+        return *(const typename Elem<T>::x8 *)(tile + at[k & 3] + (k >> 2) * 64 + block * 32 * DP);
+    }
+};
+
+// ColRead: A of a product over the rows of the tile (lane l: element 32 d + l % 32 of rows 16 s .., in the order above)
+template <int DP, class T> struct ColRead {
+    int at[2];
+    __device__ __forceinline__ explicit ColRead(int lane)
+    {
+        const int g = lane >> 4, i = lane & 15, r = 4 * (g >> 1) + (i >> 2);
+#pragma unroll
+        for (int d = 0; d < 2; ++d) at[d] = r * DP + ((4 * d + 2 * (g & 1) + ((i & 3) >> 1)) ^ swz(r)) * 8 + (i & 1) * 4;
+    }
+    __device__ __forceinline__ typename Elem<T>::x8 get(const T *tile, int s, int d) const
+    {
+        T *p = const_cast<T *>(tile) + at[d & 1] + (d >> 1) * 64 + s * 16 * DP;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ATTN_LDS s16x4 *)p);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ATTN_LDS s16x4 *)(p + 8 * DP));
+        const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_bit_cast(typename Elem<T>::x8, both);
+    }
+};
+
+// B of a product over the elements of a row, straight from memory: lane l holds elements 16 k + 8 h .. of its row
+template <int DP, class T>
+__device__ __forceinline__ void load_kept(typename Elem<T>::x8 (&f)[DP / 16], const T *row, int head_dim, int lane)
+{
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k) {
+        const int e = 16 * k + 8 * (lane >> 5);
+        typename Elem<T>::x8 z = {};
+        f[k] = e < head_dim ? *(const typename Elem<T>::x8 *)(row + e) : z;
+    }
+}
+
+// eight values of C, from element `first` on, rounded to the nearest: B of the next product
+template <class T, int N>
+__device__ __forceinline__ typename Elem<T>::x8 round8(const float (&x)[N], int first)
+{
+    typename Elem<T>::x8 r;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r[j] = (T)x[first + j];
+    return r;
+}
+
+// C with the kept row as its column: elements 32 d + 8 (i / 4) + 4 h .. of that row, times `by`, rounded once
+template <int DP, class T>
+__device__ __forceinline__ void store_kept(T *row, const f32x16 (&c)[DP / 32], float by, int head_dim, int lane)
+{
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const int e = 32 * d + 2 * i + 4 * (lane >> 5);
+            typename Elem<T>::x4 x;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = (T)(c[d][i + j] * by);
+            if (e < head_dim) *(typename Elem<T>::x4 *)(row + e) = x;
+        }
+}
+
+// ---- who sees whom ------------------------------------------------------------------------------------------------
+
+struct Span {
+    int ql, kl;      // rows in use
+    int off;         // a query's place among the keys is its row + off
+};
+
+__device__ __forceinline__ int clamp_len(const int32_t *lens, uint32_t b, uint32_t most)
+{
+    return lens ? max(0, min(lens[b], (int)most)) : (int)most;
+}
+__device__ __forceinline__ Span span_of(const AttnShape &s, uint32_t b)
+{
+    Span p;
+    p.ql = clamp_len(s.q_lens, b, s.q_len);
+    p.kl = clamp_len(s.k_lens, b, s.k_len);
+    p.off = p.kl - p.ql;
+    return p;
+}
+// keys lo .. hi - 1 are visible to query row i (hi <= lo: none)
+__device__ __forceinline__ int key_hi(const AttnShape &s, const Span &p, int i) { return s.causal ? min(p.kl, i + p.off + 1) : p.kl; }
+__device__ __forceinline__ int key_lo(const AttnShape &s, const Span &p, int i) { return s.window ? max(0, i + p.off + 1 - s.window) : 0; }
+// query rows lo .. hi - 1 see key j
+__device__ __forceinline__ int row_lo(const AttnShape &s, const Span &p, int j) { return s.causal ? max(0, j - p.off) : 0; }
+__device__ __forceinline__ int row_hi(const AttnShape &s, const Span &p, int j)
+{
+    return s.window ? (int)min((int64_t)p.ql, (int64_t)j - p.off + s.window) : p.ql;
+}
+
+// Workgroups are dealt to the eight dies in turn, each with a cache of its own: the same work list, cut in eight pieces
+// that follow each other, so that the tiles of one head, which read the same rows, share a cache.  False: nothing to do.
+__device__ __forceinline__ bool work_item(uint32_t total, uint32_t &item)
+{
+    const uint32_t each = (total + 7) / 8;
+    const uint32_t n = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
+    item = n;
+    return (blockIdx.x >> 3) < each && n < total;
+}
+
+}  // namespace lap

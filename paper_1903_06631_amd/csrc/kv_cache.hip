@@ -1,0 +1,241 @@
+// Which slots of a key/value cache stay, by the attention weight they have received.
+//
+// Order of a row's slots (one cache of one head): empty ones, then those in use by weight (not a number counts as the
+// least), equal ones with the higher index first, then the newest `recent` positions.  An eviction keeps the last `keep`
+// of that order and copies them, in the order of their slots, into another cache; an insertion overwrites the first.
+#include "attn_core.h"
+
+namespace lap {
+namespace {
+
+constexpr uint32_t NEWEST = 0xFFFFFFFFu, LEAST = 1u, EMPTY = 0u;
+
+// weights as whole numbers in the same order (minus zero is zero)
+__device__ __forceinline__ uint32_t weight_key(float w)
+{
+    if (w != w) return LEAST;
+    const uint32_t u = __float_as_uint(w + 0.f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+constexpr int EV = 1024, EW = EV / 64, BINS = 2048, COPIES = 4;
+
+struct EvictRow {
+    const float *weights;
+    const int32_t *positions;
+    int len, from;      // slots in use; the first position that is among the newest
+    __device__ __forceinline__ uint32_t key(int slot) const
+    {
+        const int p = positions ? positions[slot] : slot;
+        if (p < 0) return EMPTY;
+        return p >= from ? NEWEST : weight_key(weights[slot]);
+    }
+};
+
+// The slots that stay, ascending, into kept[]; -1 after the last.  One workgroup for each row.  The key of the last one
+// that stays is found digit by digit (11, 11 and 10 bits) from counts in LDS, in four copies: weights agree in their
+// leading bits, and additions to one counter take turns.  Then every wave takes a stretch of the row of its own.  A row is
+// read five times, from the L2 cache after the first.
+__global__ __launch_bounds__(EV) void k_evict_choose(EvictShape s, const float *weights, const int32_t *positions, int32_t *kept,
+                                                   float *weights_out, int32_t *positions_out, int32_t *lens_out)
+{
+    __shared__ uint32_t bins[COPIES][BINS];
+    __shared__ uint32_t part[EW][2];
+    __shared__ uint32_t found[2];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const uint32_t b = blockIdx.x / s.kv_heads;
+    EvictRow row;
+    row.weights = weights + (int64_t)blockIdx.x * s.slots;
+    row.positions = positions ? positions + (int64_t)blockIdx.x * s.slots : nullptr;
+    row.len = clamp_len(s.lens, b, s.slots);
+
+    int newest = row.len - 1, used = row.len;
+    if (positions) {
+        newest = -1, used = 0;
+        for (int i = t; i < row.len; i += EV) {
+            const int p = row.positions[i];
+            newest = max(newest, p);
+            used += p >= 0;
+        }
+        for (int d = 32; d; d >>= 1) newest = max(newest, __shfl_xor(newest, d, 64)), used += __shfl_xor(used, d, 64);
+        if (lane == 0) part[wave][0] = (uint32_t)newest, part[wave][1] = (uint32_t)used;
+        __syncthreads();
+        used = 0;
+        for (int i = 0; i < EW; ++i) newest = max(newest, (int)part[i][0]), used += (int)part[i][1];
+        __syncthreads();
+    }
+    row.from = newest - (int)s.recent + 1;
+    const int keep = min((int)s.keep, used);
+
+    // everything above `bound` stays, and the first `equal` slots whose key is `bound`
+    uint32_t bound = LEAST, equal = 0xFFFFFFFFu;      // all slots in use
+    if (keep < used) {
+        uint32_t prefix = 0, mask = 0, want = (uint32_t)keep;      // of the slots whose key begins with prefix, the want-th
+        if (want == 0) bound = NEWEST, equal = 0;
+        for (int digit = 0; want && digit < 3; ++digit) {
+            const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, width = digit == 2 ? 10 : 11;
+            for (int i = t; i < COPIES * BINS; i += EV) ((uint32_t *)bins)[i] = 0;
+            __syncthreads();
+            for (int i = t; i < row.len; i += EV) {
+                const uint32_t k = row.key(i);
+                if (k != EMPTY && (k & mask) == prefix) atomicAdd(&bins[wave % COPIES][(k >> shift) & ((1u << width) - 1)], 1u);
+            }
+            __syncthreads();
+            // counts from the top: a thread holds two bins, bin 2047 first
+            const int hi = BINS - 1 - 2 * t;
+            uint32_t c1 = 0, c0 = 0;
+            for (int i = 0; i < COPIES; ++i) c1 += bins[i][hi], c0 += bins[i][hi - 1];
+            uint32_t up = c1 + c0;
+            for (int d = 1; d < 64; d <<= 1) {
+                const uint32_t x = __shfl_up(up, d, 64);
+                if (lane >= d) up += x;
+            }
+            if (lane == 63) part[wave][0] = up;
+            __syncthreads();
+            for (int i = 0; i < wave; ++i) up += part[i][0];
+            const uint32_t before = up - c1 - c0;
+            if (before < want && want <= up) {
+                const bool first = want <= before + c1;
+                found[0] = (uint32_t)(first ? hi : hi - 1);
+                found[1] = want - before - (first ? 0u : c1);
+            }
+            __syncthreads();
+            prefix |= found[0] << shift;
+            mask |= ((1u << width) - 1) << shift;
+            want = found[1];
+            __syncthreads();
+        }
+        if (mask) bound = prefix, equal = want;
+    }
+
+    // stretches of whole 64s, one for each wave: how many above the bound and at it, then the places
+    const int each = ((row.len + EW - 1) / EW + 63) / 64 * 64, i0 = wave * each, i1 = min(i0 + each, row.len);
+    uint32_t above = 0, at = 0;
+    for (int i = i0 + lane; i < i1; i += 64) {
+        const uint32_t k = row.key(i);
+        above += k > bound;
+        at += k == bound && k != EMPTY;
+    }
+    for (int d = 32; d; d >>= 1) above += __shfl_xor(above, d, 64), at += __shfl_xor(at, d, 64);
+    if (lane == 0) part[wave][0] = above, part[wave][1] = at;
+    __syncthreads();
+    uint32_t place = 0, seen = 0;
+    for (int i = 0; i < wave; ++i) place += part[i][0] + min(equal - min(equal, seen), part[i][1]), seen += part[i][1];
+    const int64_t out = (int64_t)blockIdx.x * s.slots_out;
+    for (int base = i0; base < i1; base += 64) {
+        const int i = base + lane;
+        const uint32_t k = i < i1 ? row.key(i) : EMPTY;
+        const uint64_t eq = __ballot(k == bound && k != EMPTY), below = ((uint64_t)1 << lane) - 1;
+        const bool stays = k > bound || (k == bound && k != EMPTY && seen + __popcll(eq & below) < equal);
+        const uint64_t all = __ballot(stays);
+        if (stays) {
+            const uint32_t to = place + __popcll(all & below);
+            kept[out + to] = i;
+            weights_out[out + to] = row.weights[i];
+            positions_out[out + to] = row.positions ? row.positions[i] : i;
+        }
+        place += __popcll(all);
+        seen += __popcll(eq);
+    }
+    for (int i = keep + t; i < (int)s.slots_out; i += EV) {
+        kept[out + i] = -1;
+        weights_out[out + i] = 0.f;
+        positions_out[out + i] = -1;
+    }
+    if (blockIdx.x % s.kv_heads == 0 && t == 0) lens_out[b] = min((int)s.keep, row.len);
+}
+
+// keys and values of the slots that stay: 16 bytes for each thread, rows side by side
+constexpr int CP = 256, CP_ROWS = 4;
+__global__ __launch_bounds__(CP) void k_evict_copy(EvictShape s, Rows k, Rows v, Rows k_out, Rows v_out, const int32_t *kept)
+{
+    const uint32_t across = s.head_dim / 8, rows = CP / across;
+    const uint32_t r = threadIdx.x / across, e = threadIdx.x % across * 8;
+    if (r >= rows) return;
+    const uint32_t b = blockIdx.y / s.kv_heads, h = blockIdx.y % s.kv_heads;
+    const uint16_t *gk = (const uint16_t *)k.data + (int64_t)b * k.batch + (int64_t)h * k.head + e;
+    const uint16_t *gv = (const uint16_t *)v.data + (int64_t)b * v.batch + (int64_t)h * v.head + e;
+    uint16_t *ok = (uint16_t *)k_out.data + (int64_t)b * k_out.batch + (int64_t)h * k_out.head + e;
+    uint16_t *ov = (uint16_t *)v_out.data + (int64_t)b * v_out.batch + (int64_t)h * v_out.head + e;
+#pragma unroll
+    for (int i = 0; i < CP_ROWS; ++i) {
+        const uint32_t to = blockIdx.x * rows * CP_ROWS + i * rows + r;
+        if (to >= s.slots_out) continue;
+        const int from = kept[(int64_t)blockIdx.y * s.slots_out + to];
+        uint4 x = {}, y = {};
+        if (from >= 0) {
+            x = *(const uint4 *)(gk + (int64_t)from * k.row);
+            y = *(const uint4 *)(gv + (int64_t)from * v.row);
+        }
+        *(uint4 *)(ok + (int64_t)to * k_out.row) = x;
+        *(uint4 *)(ov + (int64_t)to * v_out.row) = y;
+    }
+}
+
+// One workgroup for each row: the first slot in the order above, and the new token into it.
+constexpr int IN = 256;
+__global__ __launch_bounds__(IN) void k_insert(InsertShape s, Rows k_new, Rows v_new, Rows k, Rows v, float *weights, int32_t *positions,
+                                             const int32_t *position, int32_t *slots_out)
+{
+    __shared__ uint64_t part[IN / 64];
+    const int t = threadIdx.x, lane = t & 63;
+    const uint32_t b = blockIdx.x / s.kv_heads, h = blockIdx.x % s.kv_heads;
+    const int at = position[b];
+    if (at < 0) {
+        if (t == 0) slots_out[blockIdx.x] = -1;
+        return;
+    }
+    float *w = weights + (int64_t)blockIdx.x * s.slots;
+    int32_t *pos = positions + (int64_t)blockIdx.x * s.slots;
+    uint64_t least = ~0ull;
+    for (uint32_t i = t; i < s.slots; i += IN) {
+        const int p = pos[i];
+        const uint64_t hi = p < 0 ? EMPTY : (int64_t)p > (int64_t)at - (int64_t)s.recent ? NEWEST : weight_key(w[i]);
+        const uint64_t x = hi << 32 | (p < 0 ? i : ~i);
+        least = x < least ? x : least;
+    }
+    for (int d = 32; d; d >>= 1) {
+        const uint64_t x = __shfl_xor((unsigned long long)least, d, 64);
+        least = x < least ? x : least;
+    }
+    if (lane == 0) part[t >> 6] = least;
+    __syncthreads();
+    for (int i = 0; i < IN / 64; ++i) least = part[i] < least ? part[i] : least;
+    const uint32_t slot = (least >> 32) == EMPTY ? (uint32_t)least : ~(uint32_t)least;
+    const uint32_t across = s.head_dim / 8;
+    if (t < (int)(2 * across)) {
+        const bool second = t >= (int)across;
+        const uint32_t e = (second ? t - across : t) * 8;
+        const Rows &from = second ? v_new : k_new, &to = second ? v : k;
+        *(uint4 *)((uint16_t *)to.data + (int64_t)b * to.batch + (int64_t)h * to.head + (int64_t)slot * to.row + e) =
+            *(const uint4 *)((const uint16_t *)from.data + (int64_t)b * from.batch + (int64_t)h * from.head + e);
+    }
+    if (t == 0) {
+        w[slot] = 0.f;
+        pos[slot] = at;
+        slots_out[blockIdx.x] = (int32_t)slot;
+    }
+}
+
+}  // namespace
+
+hipError_t launch_cache_evict(const EvictShape &s, const Rows &k, const Rows &v, const float *weights, const int32_t *positions,
+                              const Rows &k_out, const Rows &v_out, float *weights_out, int32_t *positions_out, int32_t *lens_out,
+                              int32_t *kept, hipStream_t st)
+{
+    k_evict_choose<<<s.batch * s.kv_heads, EV, 0, st>>>(s, weights, positions, kept, weights_out, positions_out, lens_out);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const uint32_t per = CP / (s.head_dim / 8) * CP_ROWS;
+    k_evict_copy<<<dim3((s.slots_out + per - 1) / per, s.batch * s.kv_heads), CP, 0, st>>>(s, k, v, k_out, v_out, kept);
+    return hipGetLastError();
+}
+
+hipError_t launch_cache_insert(const InsertShape &s, const Rows &k_new, const Rows &v_new, const Rows &k, const Rows &v, float *weights,
+                               int32_t *positions, const int32_t *position, int32_t *slots_out, hipStream_t st)
+{
+    k_insert<<<s.batch * s.kv_heads, IN, 0, st>>>(s, k_new, v_new, k, v, weights, positions, position, slots_out);
+    return hipGetLastError();
+}
+
+}  // namespace lap
