@@ -79,8 +79,8 @@ enum {
     LAP_E_TRACE = -6,      /* size 0, alloc >= free, free > n_steps, gap outside [alloc, free-1], step_ns 0 */
     LAP_E_RANGE = -7,      /* sum of sizes >= 2^63, a size >= 2^53, sum of step_ns >= 2^53, max size * n_steps >= 2^64 */
     LAP_E_HIP = -8,        /* a HIP runtime call or kernel launch failed */
-    LAP_E_ATTENTION = -9,  /* unknown element type, query heads no multiple of the key heads, scale not positive and
-                              finite, window without causal, a call's own rule on its shape broken, caches that differ */
+    LAP_E_ATTENTION = -9,  /* unknown element type, query heads no multiple of the key heads, scale not positive or
+                              above 1e6, window without causal, a call's own rule on its shape broken, caches that differ */
     LAP_E_LAYOUT = -10     /* rows not 16-byte aligned, head_dim no multiple of 8, a stride negative or no multiple of 8,
                               a row stride of 2^24 or more, or an output whose rows overlap */
 };

@@ -14,13 +14,13 @@ template <class T, int DP, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnShape s, Rows q, Rows k, Rows v, Rows o, float *lse, uint32_t tiles)
 {
     constexpr int BQ = 32 * NW;
-    __shared__ __align__(16) T lk[2][KT * DP];
-    __shared__ __align__(16) T lv[2][KT * DP];
-    uint32_t item;
-    if (!work_item(s.batch * s.q_heads * tiles, item)) return;
-    const uint32_t head = item / tiles, b = head / s.q_heads, h = head % s.q_heads;
-    const uint32_t kvh = h / (s.q_heads / s.kv_heads);
-    const int first = (int)(tiles - 1 - item % tiles) * BQ;      // the longest rows of a causal head first
+    __shared__ __align__(16) T lk[2][Tile<DP>::size(KT)];
+    __shared__ __align__(16) T lv[2][Tile<DP>::size(KT)];
+    const uint32_t group = s.q_heads / s.kv_heads;
+    Work wk;
+    if (!work_item(s, group, wk)) return;
+    const uint32_t b = wk.b, h = wk.kvh * group + wk.g;
+    const int first = (int)(tiles - 1 - wk.tile) * BQ;      // the longest rows of a causal head first
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Span sp = span_of(s, b);
 
@@ -36,6 +36,11 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnShape s, Rows q, R
     const int k1 = first < sp.ql ? key_hi(s, sp, end - 1) : 0;
     if (k0 < k1) {
         const int used = min(row, sp.ql - 1);       // padding takes the last row's part and is thrown away
+        const int last_chunk = (int)s.head_dim / 8 - 1, last = sp.kl - 1;
+        const T *gk = (const T *)k.data + (int64_t)b * k.batch + (int64_t)wk.kvh * k.head;
+        const T *gv = (const T *)v.data + (int64_t)b * v.batch + (int64_t)wk.kvh * v.head;
+        const TileLoad<DP, KT, NW> tk(k.row, last_chunk, wave, lane), tv(v.row, last_chunk, wave, lane);
+        tk.issue(lk[0], gk, k0, last, wave);
         typename Elem<T>::x8 qf[DP / 16];
         load_kept<DP>(qf, (const T *)q.data + (int64_t)b * q.batch + (int64_t)h * q.head + (int64_t)used * q.row, s.head_dim, lane);
         const int hi = key_hi(s, sp, used), lo = key_lo(s, sp, used);
@@ -43,32 +48,24 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnShape s, Rows q, R
         const int all_hi = key_hi(s, sp, w_first), all_lo = key_lo(s, sp, w_last);      // every row of the wave sees these
         const int any_hi = key_hi(s, sp, w_last), any_lo = key_lo(s, sp, w_first);      // and some row these
         const float c = s.scale * LOG2E;
-        const T *gk = (const T *)k.data + (int64_t)b * k.batch + (int64_t)kvh * k.head;
-        const T *gv = (const T *)v.data + (int64_t)b * v.batch + (int64_t)kvh * v.head;
-        const int last_chunk = (int)s.head_dim / 8 - 1;
         const RowRead<DP, T> rows(lane);
         const ColRead<DP, T> cols(lane);
 
-        const TileLoad<DP, KT, NW> tk(k.row, last_chunk, wave, lane), tv(v.row, last_chunk, wave, lane);
-        tk.issue(lk[0], gk, k0, sp.kl - 1, wave);
-        tv.issue(lv[0], gv, k0, sp.kl - 1, wave);
+        tv.issue(lv[0], gv, k0, last, wave);
         int buf = 0;
         for (int kt = k0; kt < k1; kt += KT, buf ^= 1) {
             tiles_arrive();
             if (kt + KT < k1) {
-                tk.issue(lk[buf ^ 1], gk, kt + KT, sp.kl - 1, wave);
-                tv.issue(lv[buf ^ 1], gv, kt + KT, sp.kl - 1, wave);
+                tk.issue(lk[buf ^ 1], gk, kt + KT, last, wave);
+                tv.issue(lv[buf ^ 1], gv, kt + KT, last, wave);
             }
             if (kt >= any_hi || kt + KT <= any_lo) continue;
-            float p[2][16];
+            f32x16 x[2] = {};
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-                f32x16 x = {};
+            for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int d = 0; d < DP / 16; ++d) x = Elem<T>::mfma(rows.get(lk[buf], kb, d), qf[d], x);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) p[kb][i] = x[i];
-            }
+                for (int d = 0; d < DP / 16; ++d) x[kb] = Elem<T>::mfma(rows.get(lk[buf], kb, d), qf[d], x[kb]);
+            reads_ahead<DP / 8, 1, 8>();
             if (kt + KT > all_hi || kt < all_lo) {
                 const int at = kt + 4 * (lane >> 5);
 #pragma unroll
@@ -76,16 +73,18 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnShape s, Rows q, R
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int key = at + 32 * kb + 8 * (i / 4) + i % 4;
-                        p[kb][i] = key < hi && key >= lo ? p[kb][i] : -ATTN_INF;
+                        x[kb][i] = key < hi && key >= lo ? x[kb][i] : -ATTN_INF;
                     }
             }
-            float top = p[0][0];
+            float top = x[0][0];
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, p[kb][i]);
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, x[kb][i]);
             top = half_max(top);
-            if (__ballot(top > m)) {
+            // The sums stay on an old maximum until a score passes it by a factor of 2^8: what is rounded to 16 bits keeps
+            // its relative error, and rows seldom come to that more than once or twice.
+            if (__ballot((top - m) * c > 8.f)) {
                 const float up = fmaxf(m, top), by = exp2_fast((m - up) * c);
                 m = up;
                 l *= by;
@@ -95,21 +94,20 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnShape s, Rows q, R
                     for (int i = 0; i < 16; ++i) acc[d][i] *= by;
             }
             const float mc = m * c;
+            float part = 0.f;
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+            for (int t = 0; t < 4; ++t) {
+                float p[8];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    p[kb][i] = exp2_fast(__builtin_fmaf(p[kb][i], c, -mc));
-                    l += p[kb][i];
+                for (int i = 0; i < 8; ++i) {
+                    p[i] = exp2_fast(__builtin_fmaf(x[t / 2][8 * (t % 2) + i], c, -mc));
+                    part += p[i];
                 }
+                const auto pf = round8<T>(p, 0);
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const auto pf = round8<T>(p[kb], 8 * t);
-#pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) acc[d] = Elem<T>::mfma(cols.get(lv[buf], 2 * kb + t, d), pf, acc[d]);
-                }
+                for (int d = 0; d < DP / 32; ++d) acc[d] = Elem<T>::mfma(cols.get(lv[buf], t, d), pf, acc[d]);
+            }
+            l += part;
         }
     }
     l = half_sum(l);
@@ -128,8 +126,8 @@ hipError_t launch(const AttnShape &s, const Rows &q, const Rows &k, const Rows &
 {
     constexpr int NW = 4;
     const uint32_t tiles = (s.q_len + 32 * NW - 1) / (32 * NW);
-    const uint32_t total = s.batch * s.q_heads * tiles;
-    k_attention<T, DP, NW><<<(total + 7) / 8 * 8, NW * 64, 0, st>>>(s, q, k, v, out, lse, tiles);
+    const uint32_t total = padded_caches(s.batch * s.kv_heads) * (s.q_heads / s.kv_heads) * tiles;
+    k_attention<T, DP, NW><<<total, NW * 64, 0, st>>>(s, q, k, v, out, lse, tiles);
     return hipGetLastError();
 }
 

@@ -55,7 +55,7 @@ int check_shape(const lap_attention_shape *s)
     if (s->head_dim % 8) return LAP_E_LAYOUT;
     if (s->q_heads % s->kv_heads) return LAP_E_ATTENTION;
     if (s->causal > 1 || (s->window && !s->causal) || s->window > MAX_LEN) return LAP_E_ATTENTION;
-    if (!(s->scale > 0.f) || !isfinite(s->scale)) return LAP_E_ATTENTION;
+    if (!(s->scale > 0.f) || s->scale > 1e6f) return LAP_E_ATTENTION;
     return LAP_OK;
 }
 
@@ -74,7 +74,12 @@ lap::StepShape step_of(const lap_attention_shape *s)
 }
 inline size_t padded_dim(const lap_attention_shape *s) { return s->head_dim <= 64 ? 64 : 128; }
 
-size_t ws_grad(const lap_attention_shape *s) { return up((size_t)s->batch * s->q_heads * s->q_len * sizeof(float2)); }
+size_t ws_grad(const lap_attention_shape *s) { return up((size_t)s->batch * s->q_heads * s->q_len * 2 * sizeof(float)); }
+size_t ws_weights(const lap_attention_shape *s)
+{
+    const uint32_t parts = lap::weights_parts(shape_of(s));
+    return parts == 1 ? 0 : up((size_t)s->batch * s->kv_heads * parts * s->k_len * 4);
+}
 size_t ws_step(const lap_attention_shape *s)
 {
     const lap::StepShape p = step_of(s);
@@ -102,6 +107,7 @@ size_t lap_attention_workspace_bytes(int which_call, const lap_attention_shape *
     if (check_shape(s)) return 0;
     switch (which_call) {
     case LAP_AT_GRAD: return ws_grad(s);
+    case LAP_AT_WEIGHTS: return ws_weights(s);
     case LAP_AT_STEP: return ws_step(s);
     default: return 0;
     }
@@ -144,7 +150,7 @@ int lap_attention_grad(const lap_attention_shape *s, const lap_rows *dout, const
     if (!rc) rc = check_ws(ws, ws_bytes, ws_grad(s));
     if (rc || (!s->q_len && !s->k_len)) return rc;
     LAP_HIP(lap::launch_attention_grad(shape_of(s), {rows_of(dout), rows_of(q), rows_of(k), rows_of(v), rows_of(out), rows_of(dq),
-                                                     rows_of(dk), rows_of(dv), lse, (float2 *)ws}, (hipStream_t)hip_stream));
+                                                     rows_of(dk), rows_of(dv), lse, (float *)ws}, (hipStream_t)hip_stream));
     return LAP_OK;
 }
 
@@ -155,9 +161,9 @@ int lap_attention_weights(const lap_attention_shape *s, const lap_rows *q, const
     if (!rc) rc = check_rows(q, s->batch, s->q_heads, s->q_len, s->head_dim, false);
     if (!rc) rc = check_rows(k, s->batch, s->kv_heads, s->k_len, s->head_dim, false);
     if (!rc && ((s->q_len && !lse) || (s->k_len && !weights))) rc = LAP_E_NULL;
-    if (!rc) rc = check_ws(ws, ws_bytes, lap_attention_workspace_bytes(LAP_AT_WEIGHTS, s));
+    if (!rc) rc = check_ws(ws, ws_bytes, ws_weights(s));
     if (rc || !s->k_len) return rc;
-    LAP_HIP(lap::launch_attention_weights(shape_of(s), rows_of(q), rows_of(k), lse, before, weights, (hipStream_t)hip_stream));
+    LAP_HIP(lap::launch_attention_weights(shape_of(s), rows_of(q), rows_of(k), lse, before, weights, (float *)ws, (hipStream_t)hip_stream));
     return LAP_OK;
 }
 

@@ -16,16 +16,16 @@ constexpr int QT = 32;      // rows of a tile of the second
 
 template <class T, int DP, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void k_attention_dq(AttnShape s, Rows g, Rows q, Rows k, Rows v, Rows o, const float *lse,
-                                                          Rows dq, float2 *stats, uint32_t tiles)
+                                                          Rows dq, float *stats, uint32_t tiles)
 {
     constexpr int BQ = 32 * NW;
-    __shared__ __align__(16) T lk[2][KT * DP];
-    __shared__ __align__(16) T lv[2][KT * DP];
-    uint32_t item;
-    if (!work_item(s.batch * s.q_heads * tiles, item)) return;
-    const uint32_t head = item / tiles, b = head / s.q_heads, h = head % s.q_heads;
-    const uint32_t kvh = h / (s.q_heads / s.kv_heads);
-    const int first = (int)(tiles - 1 - item % tiles) * BQ;
+    __shared__ __align__(16) T lk[2][Tile<DP>::size(KT)];
+    __shared__ __align__(16) T lv[2][Tile<DP>::size(KT)];
+    const uint32_t group = s.q_heads / s.kv_heads;
+    Work wk;
+    if (!work_item(s, group, wk)) return;
+    const uint32_t b = wk.b, kvh = wk.kvh, h = kvh * group + wk.g;
+    const int first = (int)(tiles - 1 - wk.tile) * BQ;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Span sp = span_of(s, b);
 
@@ -55,7 +55,10 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_dq(AttnShape s, Rows g
         }
         // a row without keys gets probabilities of zero
         const float sum = lse[at + used], l2 = sum == -ATTN_INF ? ATTN_INF : sum * LOG2E;
-        if (row < sp.ql && lane < 32) stats[at + row] = make_float2(l2, delta);
+        if (row < sp.ql && lane < 32) {
+            stats[at + row] = l2;
+            stats[(int64_t)s.batch * s.q_heads * s.q_len + at + row] = delta;
+        }
 
         if (k0 < k1) {
             const int hi = key_hi(s, sp, used), lo = key_lo(s, sp, used);
@@ -117,17 +120,22 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_dq(AttnShape s, Rows g
 }
 
 template <class T, int DP, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void k_attention_dkv(AttnShape s, Rows g, Rows q, Rows k, Rows v, const float2 *stats, Rows dk,
+__global__ __launch_bounds__(NW * 64, 2) void k_attention_dkv(AttnShape s, Rows g, Rows q, Rows k, Rows v, const float *stats, Rows dk,
                                                            Rows dv, uint32_t tiles)
 {
     constexpr int BK = 32 * NW;
-    __shared__ __align__(16) T lq[2][QT * DP];
-    __shared__ __align__(16) T lg[2][QT * DP];
-    __shared__ __align__(16) float2 lst[2][QT];
-    uint32_t item;
-    if (!work_item(s.batch * s.kv_heads * tiles, item)) return;
-    const uint32_t head = item / tiles, b = head / s.kv_heads, kvh = head % s.kv_heads;
-    const int first = (int)(item % tiles) * BK;      // the first keys of a causal head are seen by the most rows
+    __shared__ __align__(16) T lq[2][Tile<DP>::size(QT)];
+    __shared__ __align__(16) T lg[2][Tile<DP>::size(QT)];
+    // The values of the kept rows are read from here: in registers they and the sums of two waves on a SIMD do not fit, and
+    // what the compiler then keeps in memory has to be waited for together with the next tile (8 x 16 heads x 2048 tokens x
+    // 128: both passes 566 us; with 26 registers in memory 753, with one wave on a SIMD 668).
+    __shared__ __align__(16) T lkept[Tile<DP>::size(BK)];
+    __shared__ __align__(16) float lst[2][2][64];
+    static_assert(QT <= 64, "a wave fetches the numbers of 64 rows at once");
+    Work wk;
+    if (!work_item(s, 1, wk)) return;
+    const uint32_t b = wk.b, kvh = wk.kvh;
+    const int first = (int)wk.tile * BK;      // the first keys of a causal head are seen by the most rows
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Span sp = span_of(s, b);
     const uint32_t group = s.q_heads / s.kv_heads;
@@ -140,9 +148,10 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_dkv(AttnShape s, Rows 
     const int r1 = first < sp.kl ? row_hi(s, sp, end - 1) : 0;
     if (r0 < r1) {
         const int used = min(key, sp.kl - 1);
-        typename Elem<T>::x8 kf[DP / 16], vf[DP / 16];
+        typename Elem<T>::x8 kf[DP / 16];
+        load_kept<DP>(kf, (const T *)v.data + (int64_t)b * v.batch + (int64_t)kvh * v.head + (int64_t)used * v.row, s.head_dim, lane);
+        keep_in_lds<DP>(lkept, wave, kf, lane);
         load_kept<DP>(kf, (const T *)k.data + (int64_t)b * k.batch + (int64_t)kvh * k.head + (int64_t)used * k.row, s.head_dim, lane);
-        load_kept<DP>(vf, (const T *)v.data + (int64_t)b * v.batch + (int64_t)kvh * v.head + (int64_t)used * v.row, s.head_dim, lane);
         const int hi = row_hi(s, sp, used), lo = row_lo(s, sp, used);
         const int w_last = min(w0 + 31, sp.kl - 1), w_first = min(w0, sp.kl - 1);
         const int all_hi = row_hi(s, sp, w_first), all_lo = row_lo(s, sp, w_last);
@@ -155,12 +164,13 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_dkv(AttnShape s, Rows 
         const int per = (r1 - r0 + QT - 1) / QT, count = per * (int)group;
         const T *gq = (const T *)q.data + (int64_t)b * q.batch + (int64_t)kvh * group * q.head;
         const T *gg = (const T *)g.data + (int64_t)b * g.batch + (int64_t)kvh * group * g.head;
-        const float2 *gs = stats + ((int64_t)b * s.q_heads + (int64_t)kvh * group) * s.q_len;
+        const float *gs = stats + ((int64_t)b * s.q_heads + (int64_t)kvh * group) * s.q_len;
+        const int64_t to_delta = (int64_t)s.batch * s.q_heads * s.q_len;
         int next = r0;      // rows and head of the next tile to ask for
-        auto issue = [&](int to) {
+        const auto issue = [&](int to) {
             tq.issue(lq[to], gq, next, sp.ql - 1, wave);
             tg.issue(lg[to], gg, next, sp.ql - 1, wave);
-            if (wave == 0 && lane < QT) lst[to][lane] = gs[min(next + lane, sp.ql - 1)];
+            if (wave < 2) load_floats(lst[to][wave], gs + wave * to_delta, next, sp.ql - 1, lane);
             next += QT;
             if (next >= r1) next = r0, gq += q.head, gg += g.head, gs += s.q_len;
         };
@@ -169,38 +179,42 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_dkv(AttnShape s, Rows 
         for (int n = 0; n < count; ++n, buf ^= 1) {
             tiles_arrive();
             if (n + 1 < count) issue(buf ^ 1);
-            const int at = qt;
+            const int tile = qt;
             qt = qt + QT >= r1 ? r0 : qt + QT;
-            if (at >= any_hi || at + QT <= any_lo) continue;
-            f32x16 x = {}, y = {};
 #pragma unroll
-            for (int d = 0; d < DP / 16; ++d) x = Elem<T>::mfma(rows.get(lq[buf], 0, d), kf[d], x);
+            for (int qb = 0; qb < QT / 32; ++qb) {
+                const int at = tile + 32 * qb;
+                if (at >= any_hi || at + 32 <= any_lo) continue;
+                f32x16 x = {}, y = {};
 #pragma unroll
-            for (int d = 0; d < DP / 16; ++d) y = Elem<T>::mfma(rows.get(lg[buf], 0, d), vf[d], y);
-            float p[16], ds[16];
+                for (int d = 0; d < DP / 16; ++d) x = Elem<T>::mfma(rows.get(lq[buf], qb, d), kf[d], x);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float2 st = lst[buf][8 * (i / 4) + 4 * (lane >> 5) + i % 4];
-                p[i] = exp2_fast(__builtin_fmaf(x[i], c, -st.x));
-                ds[i] = p[i] * (y[i] - st.y);
-            }
-            if (at + QT > all_hi || at < all_lo) {
-                const int row0 = at + 4 * (lane >> 5);
+                for (int d = 0; d < DP / 16; ++d) y = Elem<T>::mfma(rows.get(lg[buf], qb, d), rows.get(lkept, wave, d), y);
+                const float *const l2 = lst[buf][0] + 32 * qb + 4 * (lane >> 5), *const delta = lst[buf][1] + 32 * qb + 4 * (lane >> 5);
+                float p[16], ds[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int row = row0 + 8 * (i / 4) + i % 4;
-                    const bool in = row < hi && row >= lo;
-                    p[i] = in ? p[i] : 0.f;
-                    ds[i] = in ? ds[i] : 0.f;
+                    p[i] = exp2_fast(__builtin_fmaf(x[i], c, -l2[8 * (i / 4) + i % 4]));
+                    ds[i] = p[i] * (y[i] - delta[8 * (i / 4) + i % 4]);
                 }
-            }
+                if (at + 32 > all_hi || at < all_lo) {
+                    const int row0 = at + 4 * (lane >> 5);
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const auto pf = round8<T>(p, 8 * t), df = round8<T>(ds, 8 * t);
+                    for (int i = 0; i < 16; ++i) {
+                        const int row = row0 + 8 * (i / 4) + i % 4;
+                        const bool in = row < hi && row >= lo;
+                        p[i] = in ? p[i] : 0.f;
+                        ds[i] = in ? ds[i] : 0.f;
+                    }
+                }
 #pragma unroll
-                for (int d = 0; d < DP / 32; ++d) {
-                    av[d] = Elem<T>::mfma(cols.get(lg[buf], t, d), pf, av[d]);
-                    ak[d] = Elem<T>::mfma(cols.get(lq[buf], t, d), df, ak[d]);
+                for (int t = 0; t < 2; ++t) {
+                    const auto pf = round8<T>(p, 8 * t), df = round8<T>(ds, 8 * t);
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d) {
+                        av[d] = Elem<T>::mfma(cols.get(lg[buf], 2 * qb + t, d), pf, av[d]);
+                        ak[d] = Elem<T>::mfma(cols.get(lq[buf], 2 * qb + t, d), df, ak[d]);
+                    }
                 }
             }
         }
@@ -218,14 +232,15 @@ template <class T, int DP>
 hipError_t launch(const AttnShape &s, const AttnGrad &a, hipStream_t st)
 {
     constexpr int NW = 4;
-    const uint32_t qtiles = (s.q_len + 32 * NW - 1) / (32 * NW), qtotal = s.batch * s.q_heads * qtiles;
-    const uint32_t ktiles = (s.k_len + 32 * NW - 1) / (32 * NW), ktotal = s.batch * s.kv_heads * ktiles;
+    const uint32_t caches = padded_caches(s.batch * s.kv_heads);
+    const uint32_t qtiles = (s.q_len + 32 * NW - 1) / (32 * NW), qtotal = caches * (s.q_heads / s.kv_heads) * qtiles;
+    const uint32_t ktiles = (s.k_len + 32 * NW - 1) / (32 * NW), ktotal = caches * ktiles;
     if (qtotal) {
-        k_attention_dq<T, DP, NW><<<(qtotal + 7) / 8 * 8, NW * 64, 0, st>>>(s, a.g, a.q, a.k, a.v, a.out, a.lse, a.dq, a.stats, qtiles);
+        k_attention_dq<T, DP, NW><<<qtotal, NW * 64, 0, st>>>(s, a.g, a.q, a.k, a.v, a.out, a.lse, a.dq, a.stats, qtiles);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (ktotal) k_attention_dkv<T, DP, NW><<<(ktotal + 7) / 8 * 8, NW * 64, 0, st>>>(s, a.g, a.q, a.k, a.v, a.stats, a.dk, a.dv, ktiles);
+    if (ktotal) k_attention_dkv<T, DP, NW><<<ktotal, NW * 64, 0, st>>>(s, a.g, a.q, a.k, a.v, a.stats, a.dk, a.dv, ktiles);
     return hipGetLastError();
 }
 

@@ -18,7 +18,8 @@ constexpr int NW = 4, TS = 32;      // waves, slots of a wave's tile
 template <class T, int DP>
 __global__ __launch_bounds__(NW * 64, 2) void k_step(StepShape s, StepWork w)
 {
-    __shared__ __align__(16) char raw[NW * 2 * TS * DP * sizeof(T)];      // the waves' values; their outputs at the end
+    constexpr int TILE = Tile<DP>::size(TS);
+    __shared__ __align__(16) char raw[NW * 2 * TILE * sizeof(T)];      // the waves' values; their outputs at the end
     __shared__ float2 sums[NW][32];
     T *const lv = (T *)raw;
     const uint32_t group = s.q_heads / s.kv_heads, parts = (group + 31) / 32;
@@ -39,12 +40,12 @@ __global__ __launch_bounds__(NW * 64, 2) void k_step(StepShape s, StepWork w)
     const float c = s.scale * LOG2E;
     const ColRead<DP, T> cols(lane);
     const TileLoad<DP, TS, 1> tv(w.v.row, (int)s.head_dim / 8 - 1, 0, lane);
-    T *const mine = lv + wave * 2 * TS * DP;
+    T *const mine = lv + wave * 2 * TILE;
 
     f32x16 acc[DP / 32] = {};
     float m = LOWEST, l = 0.f;
     const auto fetch = [&](int at, int to) {      // slots at .. at + 31
-        tv.issue(mine + to * TS * DP, gv, at, len - 1, 0);
+        tv.issue(mine + to * TILE, gv, at, len - 1, 0);
         load_kept<DP>(kf, gk + (int64_t)min(at + r, len - 1) * w.k.row, s.head_dim, lane);
     };
     int at = c0 + wave * TS, buf = 0;
@@ -67,7 +68,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_step(StepShape s, StepWork w)
             for (int i = 0; i < 16; ++i) p[i] = (live >> (8 * (i / 4) + 4 * h + i % 4)) & 1 ? p[i] : -ATTN_INF;
             if (pos) {      // what an empty slot holds may be anything, and zero times it is not always zero
                 for (int n = lane; n < TS * DP / 8; n += 64)
-                    if (!((live >> (n / (DP / 8))) & 1)) ((s16x8 *)(mine + buf * TS * DP))[n] = s16x8{};
+                    if (!((live >> (n / (DP / 8))) & 1)) *(s16x8 *)(mine + buf * TILE + Tile<DP>::place(n / (DP / 8), n % (DP / 8))) = s16x8{};
             }
         }
         if (scores && r < n_rows) {
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_step(StepShape s, StepWork w)
         for (int t = 0; t < 2; ++t) {
             const auto pf = round8<T>(p, 8 * t);
 #pragma unroll
-            for (int d = 0; d < DP / 32; ++d) acc[d] = Elem<T>::mfma(cols.get(mine + buf * TS * DP, t, d), pf, acc[d]);
+            for (int d = 0; d < DP / 32; ++d) acc[d] = Elem<T>::mfma(cols.get(mine + buf * TILE, t, d), pf, acc[d]);
         }
     }
     // join the waves: their sums, then their outputs, each on the workgroup's maximum

@@ -55,44 +55,50 @@ __device__ __forceinline__ float half_sum(float x)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Rows in LDS: DP elements (DP / 8 chunks of 16 bytes) one after the other, chunk c of row r at place c ^ swz(r).  Eight
-// rows that follow each other, read at one chunk, and four rows read at two neighbouring chunks, then come from eight
-// different places: neither kind of read below has conflicts.
-__device__ __forceinline__ int swz(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
+// Rows in LDS.  An asynchronous load puts 64 times 16 bytes side by side, G rows of DP elements; such groups of rows stand
+// 16 bytes apart, and within one, chunk c (16 bytes) of row r stands at place c ^ swz(r).  LDS serves 256 bytes at a time
+// from 64 banks: 16 rows that follow each other, read at one chunk, or four rows at four neighbouring chunks, then come
+// from 16 different places, so neither kind of read below has conflicts (a layout whose places repeat after eight rows took
+// twice the LDS cycles).  The places of other groups are a constant away, and go into the instruction.
+template <int DP> struct Tile {
+    static constexpr int CH = DP / 8;            // chunks of a row
+    static constexpr int G = 64 / CH;            // rows of a group
+    static constexpr int GROUP = 64 * 8 + 8;     // elements from group to group
+    static constexpr int size(int rows) { return rows / G * GROUP; }
+    static __device__ __forceinline__ int swz(int row) { return DP == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2 | ((row >> 2) & 1) << 1; }
+    static __device__ __forceinline__ int place(int row, int chunk) { return row / G * GROUP + row % G * DP + (chunk ^ swz(row)) * 8; }
+};
 
 // ROWS rows from global memory into LDS, asynchronously, by NW waves.  Rows past `last` are copies of it and chunks past
 // the last one of a row copies of that one: padding is never read, and what stands in its place is part of the same row.
 // The compiler does not see these loads: it would wait for the ones just sent off before any read of LDS, as it cannot
 // tell the tiles apart.  tiles_arrive() waits for them.
 template <int DP, int ROWS, int NW> struct TileLoad {
-    static constexpr int CH = DP / 8, PER = ROWS * CH / 64 / NW;      // chunks of a row, instructions of a wave
-    static_assert(PER * 64 * NW == ROWS * CH, "whole instructions");
-    uint32_t off[PER];      // this lane's bytes of a whole tile
+    typedef Tile<DP> L;
+    static constexpr int PER = ROWS / L::G / NW;      // instructions of a wave
+    static_assert(PER * NW * L::G == ROWS, "whole instructions");
+    uint32_t off;           // this lane's bytes of the first instruction; the others are a number of rows further on
     uint32_t stride;        // bytes of a row (at most 2^25: 64 rows stay within 32 bits)
     int row0;
-    __device__ __forceinline__ static int chunk(int j, int lane, int wave, int last_chunk)
-    {
-        return min((lane % CH) ^ swz((wave * PER + j) * 64 / CH + lane / CH), last_chunk);
-    }
     __device__ __forceinline__ TileLoad(int64_t row_stride, int last_chunk, int wave, int lane)
     {
         stride = (uint32_t)row_stride * 2u;
-        row0 = wave * PER * 64 / CH + lane / CH;
-#pragma unroll
-        for (int j = 0; j < PER; ++j) off[j] = (uint32_t)(row0 + j * (64 / CH)) * stride + (uint32_t)chunk(j, lane, wave, last_chunk) * 16u;
+        row0 = wave * PER * L::G + lane / L::CH;
+        off = (uint32_t)row0 * stride + (uint32_t)min((lane % L::CH) ^ L::swz(lane / L::CH), last_chunk) * 16u;
     }
     // rows first .. first + ROWS - 1 of g; first <= last
     template <class T> __device__ __forceinline__ void issue(T *lds, const T *g, int first, int last, int wave) const
     {
         const char *base = (const char *)g + (int64_t)first * stride;
-        const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(ATTN_LDS void *)lds + (uint32_t)(wave * PER * 1024));
+        const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(ATTN_LDS void *)lds + (uint32_t)(wave * PER * L::GROUP * 2));
         const int left = last - first;
         if (left >= ROWS - 1) {
 #pragma unroll
-            for (int j = 0; j < PER; ++j) send(to + j * 1024u, off[j], base);
+            for (int j = 0; j < PER; ++j) send(to + j * (L::GROUP * 2u), off, base + (uint64_t)(j * L::G) * stride);
         } else {
 #pragma unroll
-            for (int j = 0; j < PER; ++j) send(to + j * 1024u, off[j] - (uint32_t)max(0, row0 + j * (64 / CH) - left) * stride, base);
+            for (int j = 0; j < PER; ++j)
+                send(to + j * (L::GROUP * 2u), off + (uint32_t)(min(row0 + j * L::G, left) - row0) * stride, base);
         }
     }
     // 16 bytes for every lane, from base + its offset, to LDS address `to` + 16 times the lane (the register that holds
@@ -102,6 +108,14 @@ template <int DP, int ROWS, int NW> struct TileLoad {
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
     }
 };
+
+// 64 floats from g + first on into LDS, by one wave; those past index `last` are copies of that one
+__device__ __forceinline__ void load_floats(float *lds, const float *g, int first, int last, int lane)
+{
+    const char *base = (const char *)(g + first);
+    const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(ATTN_LDS void *)lds);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(4u * (uint32_t)min(lane, last - first)), "s"(base) : "memory");
+}
 
 // what has been asked for has arrived in LDS, for every wave, and every wave is done with what it has read there
 __device__ __forceinline__ void tiles_arrive()
@@ -113,40 +127,50 @@ __device__ __forceinline__ void tiles_arrive()
 }
 
 // Operands out of a tile.  RowRead: A of a product over the elements of a row (lane l: row l % 32 of a block of 32).
-// The place of a chunk is an exclusive or; its two low bits are worked out once, the rest is an offset.
 template <int DP, class T> struct RowRead {
     int at[4];
     __device__ __forceinline__ explicit RowRead(int lane)
     {
-        const int r = lane & 31, h = lane >> 5;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) at[k] = r * DP + (((2 * k) | h) ^ swz(r)) * 8;
+        for (int i = 0; i < 4; ++i) at[i] = Tile<DP>::place(lane & 31, (DP == 128 ? 4 * i : 2 * i) | (lane >> 5));
     }
     // elements 16 k + 8 h .. of rows 32 block ..
     __device__ __forceinline__ typename Elem<T>::x8 get(const T *tile, int block, int k) const
     {
-        return *(const typename Elem<T>::x8 *)(tile + at[k & 3] + (k >> 2) * 64 + block * 32 * DP);
+        return *(const typename Elem<T>::x8 *)(tile + (DP == 128 ? at[k >> 1] + (k & 1) * 16 : at[k]) + Tile<DP>::size(32) * block);
     }
 };
 
 // ColRead: A of a product over the rows of the tile (lane l: element 32 d + l % 32 of rows 16 s .., in the order above)
 template <int DP, class T> struct ColRead {
-    int at[2];
+    int at[DP / 32];
     __device__ __forceinline__ explicit ColRead(int lane)
     {
-        const int g = lane >> 4, i = lane & 15, r = 4 * (g >> 1) + (i >> 2);
+        const int g = lane >> 4, i = lane & 15;
 #pragma unroll
-        for (int d = 0; d < 2; ++d) at[d] = r * DP + ((4 * d + 2 * (g & 1) + ((i & 3) >> 1)) ^ swz(r)) * 8 + (i & 1) * 4;
+        for (int d = 0; d < DP / 32; ++d) at[d] = Tile<DP>::place(4 * (g >> 1) + (i >> 2), 4 * d + 2 * (g & 1) + ((i & 3) >> 1)) + (i & 1) * 4;
     }
     __device__ __forceinline__ typename Elem<T>::x8 get(const T *tile, int s, int d) const
     {
-        T *p = const_cast<T *>(tile) + at[d & 1] + (d >> 1) * 64 + s * 16 * DP;
+        T *p = const_cast<T *>(tile) + at[d] + Tile<DP>::size(16) * s;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ATTN_LDS s16x4 *)p);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ATTN_LDS s16x4 *)(p + 8 * DP));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ATTN_LDS s16x4 *)(p + Tile<DP>::size(8)));
         const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         return __builtin_bit_cast(typename Elem<T>::x8, both);
     }
 };
+
+// The order of a run of N products with PER LDS reads each: reads stay AHEAD products in front of their use, where the
+// compiler, saving registers, would wait for each as it comes.
+template <int N, int PER, int AHEAD> __device__ __forceinline__ void reads_ahead()
+{
+    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * PER, 0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        if (i < N - AHEAD) __builtin_amdgcn_sched_group_barrier(0x100, PER, 0);
+    }
+}
 
 // B of a product over the elements of a row, straight from memory: lane l holds elements 16 k + 8 h .. of its row
 template <int DP, class T>
@@ -158,6 +182,15 @@ __device__ __forceinline__ void load_kept(typename Elem<T>::x8 (&f)[DP / 16], co
         typename Elem<T>::x8 z = {};
         f[k] = e < head_dim ? *(const typename Elem<T>::x8 *)(row + e) : z;
     }
+}
+
+// the same rows into a tile, as rows 32 block ..: zeros included where a row has fewer than DP elements
+template <int DP, class T>
+__device__ __forceinline__ void keep_in_lds(T *tile, int block, const typename Elem<T>::x8 *f, int lane)
+{
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k)
+        *(typename Elem<T>::x8 *)(tile + Tile<DP>::size(32) * block + Tile<DP>::place(lane & 31, 2 * k + (lane >> 5))) = f[k];
 }
 
 // eight values of C, from element `first` on, rounded to the nearest: B of the next product
@@ -215,14 +248,21 @@ __device__ __forceinline__ int row_hi(const AttnShape &s, const Span &p, int j)
     return s.window ? (int)min((int64_t)p.ql, (int64_t)j - p.off + s.window) : p.ql;
 }
 
-// Workgroups are dealt to the eight dies in turn, each with a cache of its own: the same work list, cut in eight pieces
-// that follow each other, so that the tiles of one head, which read the same rows, share a cache.  False: nothing to do.
-__device__ __forceinline__ bool work_item(uint32_t total, uint32_t &item)
+// Work of all tiles of the rows of `caches` key heads (times `group` query heads): tile by tile, key heads next to each
+// other.  Workgroups are dealt to the eight dies in turn, each with an L2 cache of its own, so with a multiple of eight key
+// heads (padded to one where there are many) all that reads one head's rows shares a die, at the same time; and where
+// tiles differ in length, all long ones come before all short ones, so that no unit is left with a long one at the end.
+struct Work {
+    uint32_t tile, b, g, kvh;
+};
+inline uint32_t padded_caches(uint32_t caches) { return caches < 32 ? caches : (caches + 7) / 8 * 8; }
+__device__ __forceinline__ bool work_item(const AttnShape &s, uint32_t group, Work &w)
 {
-    const uint32_t each = (total + 7) / 8;
-    const uint32_t n = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
-    item = n;
-    return (blockIdx.x >> 3) < each && n < total;
+    const uint32_t caches = s.batch * s.kv_heads, padded = caches < 32 ? caches : (caches + 7) / 8 * 8;
+    const uint32_t n = blockIdx.x / padded, c = blockIdx.x % padded;
+    w.tile = n / group, w.g = n % group;
+    w.b = c / s.kv_heads, w.kvh = c % s.kv_heads;
+    return c < caches;
 }
 
 }  // namespace lap

@@ -24,11 +24,14 @@ hipError_t launch_attention(const AttnShape &s, const Rows &q, const Rows &k, co
 struct AttnGrad {
     Rows g, q, k, v, out, dq, dk, dv;
     const float *lse;
-    float2 *stats;      // [batch, q_heads, q_len]: sums in base 2 (plus infinity: no key), delta
+    float *stats;       // sums in base 2 (plus infinity: no key) [batch, q_heads, q_len], then delta likewise
 };
 hipError_t launch_attention_grad(const AttnShape &s, const AttnGrad &a, hipStream_t st);
+// sums: [batch, kv_heads, weights_parts(s), k_len], unless that is one part
+uint32_t weights_blocks(const AttnShape &s);
+uint32_t weights_parts(const AttnShape &s);
 hipError_t launch_attention_weights(const AttnShape &s, const Rows &q, const Rows &k, const float *lse, const float *before, float *weights,
-                                    hipStream_t st);
+                                    float *sums, hipStream_t st);
 
 constexpr uint32_t MAX_GROUP = 256;      // query heads that share one key head, in attention_step.hip
 
