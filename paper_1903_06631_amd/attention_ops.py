@@ -10,8 +10,9 @@ ValueError here; the rest is LapError from the library.
 from __future__ import annotations
 
 import ctypes as C
-import math
 from typing import Optional
+
+from . import binding
 
 AT_FORWARD, AT_GRAD, AT_WEIGHTS, AT_STEP = range(4)
 
@@ -49,68 +50,85 @@ def declare(lib) -> None:
 
 
 def _lib():
-    from .binding import load_library
-    return load_library()
+    return binding._lib or binding.load_library()
 
 
-def _torch():
-    import torch
-    return torch
-
-
-def _done(rc: int, where: str, torch, device, sync: bool) -> None:
+def _done(rc: int, where: str, device, sync: bool) -> None:
     if rc:
-        from .binding import LapError
-        raise LapError(rc, where)
+        raise binding.LapError(rc, where)
     if sync:
-        torch.cuda.current_stream(device).synchronize()
+        binding._torch().cuda.current_stream(device).synchronize()
 
 
-def _check(ok: bool, what: str) -> None:
-    if not ok:
-        raise ValueError(what)
+# A call's arguments are looked at on every call, of a few microseconds each: the texts of refusals are put together only
+# where one is due.
+
+def _refuse(name: str, x, expected) -> None:
+    raise ValueError(f"{name}: {tuple(x.shape)} {x.dtype} on {x.device} with strides {x.stride()}, expected {expected}")
 
 
 def _rows(x, name: str, like, shape):
-    """lap_rows of x, which has to be a tensor of this shape and of like's type and device."""
-    _check(x.dtype == like.dtype and x.device == like.device, f"{name}: {x.dtype} on {x.device}, expected {like.dtype} on {like.device}")
-    _check(tuple(x.shape) == tuple(shape), f"{name}: shape {tuple(x.shape)}, expected {tuple(shape)}")
+    """lap_rows of x, which has to be a tensor of this shape and of like's type and device, elements of a row side by side."""
+    if x.dtype is not like.dtype or x.shape != shape or x.get_device() != like.get_device():
+        _refuse(name, x, f"{tuple(shape)} {like.dtype} on {like.device}")
     st = x.stride()
-    _check(st[-1] == 1 or x.numel() == 0, f"{name}: the elements of a row have to lie side by side")
-    return _Rows(x.data_ptr(), st[0], st[1], st[2] if len(shape) == 4 else 0)
+    if st[-1] != 1 and x.numel():
+        _refuse(name, x, "the elements of a row side by side")
+    return _Rows(x.data_ptr(), st[0], st[1], st[2] if len(st) == 4 else 0)
 
 
-def _plain(x, name: str, dtype, shape, device):
+def _plain(x, name: str, dtype, shape, index: int):
     """Address of a contiguous tensor of this type and shape, None for None."""
     if x is None:
         return None
-    _check(x.dtype == dtype and x.device == device and tuple(x.shape) == tuple(shape) and x.is_contiguous(),
-           f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+    if x.dtype is not dtype or x.shape != shape or x.get_device() != index or not x.is_contiguous():
+        _refuse(name, x, f"a contiguous {dtype} of {tuple(shape)} on GPU {index}")
     return x.data_ptr()
 
 
-def _type(torch, x) -> int:
-    _check(x.is_cuda, "tensors have to be on the GPU")
-    _check(x.dtype in (torch.bfloat16, torch.float16), f"{x.dtype}: expected torch.bfloat16 or torch.float16")
-    return 0 if x.dtype == torch.bfloat16 else 1
+def _type(torch, x, name: str) -> int:
+    if x.dtype is torch.bfloat16:
+        kind = 0
+    elif x.dtype is torch.float16:
+        kind = 1
+    else:
+        _refuse(name, x, "torch.bfloat16 or torch.float16")
+    if not x.is_cuda:
+        _refuse(name, x, "a tensor on the GPU")
+    return kind
+
+
+def _four(x, name: str):
+    if x.dim() != 4:
+        _refuse(name, x, "[batch, heads, length, head_dim]")
+    return x.shape
+
+
+def _scale(scale: Optional[float], d: int) -> float:
+    return float(scale) if scale is not None else d ** -0.5 if d else 0.0
 
 
 def _shape(torch, q, k, causal, window, scale, q_lens, k_lens):
-    _check(q.dim() == 4 and k.dim() == 4, "q and k are [batch, heads, length, head_dim]")
-    b, h, n, d = q.shape
-    kind = _type(torch, q)
-    _check(window >= 0, "window is 0 (none) or a number of keys")
-    return _Shape(kind, b, h, k.shape[1], n, k.shape[2], d, bool(causal), int(window),
-                  1.0 / math.sqrt(d) if scale is None and d else (scale or 0.0),
-                  _plain(q_lens, "q_lens", torch.int32, (b,), q.device), _plain(k_lens, "k_lens", torch.int32, (b,), q.device))
+    b, h, n, d = _four(q, "q")
+    _four(k, "k")
+    kind, index = _type(torch, q, "q"), q.get_device()
+    if window < 0:
+        raise ValueError("window is 0 (none) or a number of keys")
+    i32 = torch.int32
+    return _Shape(kind, b, h, k.shape[1], n, k.shape[2], d, 1 if causal else 0, window, _scale(scale, d),
+                  None if q_lens is None else _plain(q_lens, "q_lens", i32, (b,), index),
+                  None if k_lens is None else _plain(k_lens, "k_lens", i32, (b,), index))
 
 
 def _workspace(torch, ws, need: int, device):
+    """The workspace, its size and its address."""
     if ws is None:
-        ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    elif need:
-        _check(ws.dtype == torch.uint8 and ws.device == device and ws.is_contiguous(), "ws: expected contiguous torch.uint8 on the tensors' device")
-    return ws, (0 if ws is None else ws.numel()), (None if ws is None else ws.data_ptr())
+        if not need:
+            return None, 0, None
+        ws = torch.empty(need, dtype=torch.uint8, device=device)
+    elif ws.dtype is not torch.uint8 or ws.device != device or not ws.is_contiguous():
+        _refuse("ws", ws, f"a contiguous torch.uint8 on {device}")
+    return ws, ws.numel(), ws.data_ptr()
 
 
 def _stream(torch, device) -> int:
@@ -120,16 +138,16 @@ def _stream(torch, device) -> int:
 def attention(q, k, v, *, causal: bool = False, window: int = 0, scale: Optional[float] = None, q_lens=None, k_lens=None,
               out: Optional[dict] = None, ws=None, sync: bool = True):
     """lap_attention: returns dict(out like q, lse [batch, q_heads, q_len]).  scale None: 1 / sqrt(head_dim)."""
-    torch, lib = _torch(), _lib()
+    lib, torch = _lib(), binding._torch()
     s = _shape(torch, q, k, causal, window, scale, q_lens, k_lens)
     kv = (s.batch, s.kv_heads, s.k_len, s.head_dim)
     if out is None:
         out = dict(out=torch.empty_like(q), lse=torch.empty(q.shape[:3], dtype=torch.float32, device=q.device))
     ws, have, at = _workspace(torch, ws, lib.lap_attention_workspace_bytes(AT_FORWARD, s), q.device)
     rc = lib.lap_attention(s, _rows(q, "q", q, q.shape), _rows(k, "k", q, kv), _rows(v, "v", q, kv),
-                           _rows(out["out"], "out", q, q.shape), _plain(out["lse"], "lse", torch.float32, q.shape[:3], q.device),
+                           _rows(out["out"], "out", q, q.shape), _plain(out["lse"], "lse", torch.float32, q.shape[:3], q.get_device()),
                            at, have, _stream(torch, q.device))
-    _done(rc, "lap_attention", torch, q.device, sync)
+    _done(rc, "lap_attention", q.device, sync)
     return out
 
 
@@ -137,7 +155,7 @@ def attention_grad(dout, q, k, v, out, lse, *, causal: bool = False, window: int
                    k_lens=None, grads: Optional[dict] = None, ws=None, sync: bool = True):
     """lap_attention_grad: returns dict(dq, dk, dv); out and lse are attention's, the other arguments as there.  grads takes
     result tensors that the caller owns."""
-    torch, lib = _torch(), _lib()
+    lib, torch = _lib(), binding._torch()
     s = _shape(torch, q, k, causal, window, scale, q_lens, k_lens)
     kv = (s.batch, s.kv_heads, s.k_len, s.head_dim)
     if grads is None:
@@ -145,26 +163,26 @@ def attention_grad(dout, q, k, v, out, lse, *, causal: bool = False, window: int
                      dv=torch.empty(kv, dtype=q.dtype, device=q.device))
     ws, have, at = _workspace(torch, ws, lib.lap_attention_workspace_bytes(AT_GRAD, s), q.device)
     rc = lib.lap_attention_grad(s, _rows(dout, "dout", q, q.shape), _rows(q, "q", q, q.shape), _rows(k, "k", q, kv), _rows(v, "v", q, kv),
-                                _rows(out, "out", q, q.shape), _plain(lse, "lse", torch.float32, q.shape[:3], q.device),
+                                _rows(out, "out", q, q.shape), _plain(lse, "lse", torch.float32, q.shape[:3], q.get_device()),
                                 _rows(grads["dq"], "dq", q, q.shape), _rows(grads["dk"], "dk", q, kv), _rows(grads["dv"], "dv", q, kv),
                                 at, have, _stream(torch, q.device))
-    _done(rc, "lap_attention_grad", torch, q.device, sync)
+    _done(rc, "lap_attention_grad", q.device, sync)
     return grads
 
 
 def attention_weights(q, k, lse, *, before=None, causal: bool = False, window: int = 0, scale: Optional[float] = None, q_lens=None,
                       k_lens=None, weights=None, ws=None, sync: bool = True):
     """lap_attention_weights: returns dict(weights [batch, kv_heads, k_len]) = before (None: zeros) + what the keys receive."""
-    torch, lib = _torch(), _lib()
+    lib, torch = _lib(), binding._torch()
     s = _shape(torch, q, k, causal, window, scale, q_lens, k_lens)
     kv = (s.batch, s.kv_heads, s.k_len)
     if weights is None:
         weights = torch.empty(kv, dtype=torch.float32, device=q.device)
     ws, have, at = _workspace(torch, ws, lib.lap_attention_workspace_bytes(AT_WEIGHTS, s), q.device)
     rc = lib.lap_attention_weights(s, _rows(q, "q", q, q.shape), _rows(k, "k", q, kv + (s.head_dim,)),
-                                   _plain(lse, "lse", torch.float32, q.shape[:3], q.device), _plain(before, "before", torch.float32, kv, q.device),
-                                   _plain(weights, "weights", torch.float32, kv, q.device), at, have, _stream(torch, q.device))
-    _done(rc, "lap_attention_weights", torch, q.device, sync)
+                                   _plain(lse, "lse", torch.float32, q.shape[:3], q.get_device()), _plain(before, "before", torch.float32, kv, q.get_device()),
+                                   _plain(weights, "weights", torch.float32, kv, q.get_device()), at, have, _stream(torch, q.device))
+    _done(rc, "lap_attention_weights", q.device, sync)
     return dict(weights=weights)
 
 
@@ -173,69 +191,73 @@ def attention_step(q, k_cache, v_cache, weights=None, *, lens=None, positions=No
     """lap_attention_step: q [batch, q_heads, head_dim] of one token against caches [batch, kv_heads, slots, head_dim].  Returns
     dict(out like q, lse [batch, q_heads], weights = the given ones + this token's, a new tensor unless out holds one; None
     where none are given)."""
-    torch, lib = _torch(), _lib()
-    _check(q.dim() == 3 and k_cache.dim() == 4, "q is [batch, heads, head_dim], caches are [batch, heads, slots, head_dim]")
+    lib, torch = _lib(), binding._torch()
+    if q.dim() != 3:
+        _refuse("q", q, "[batch, heads, head_dim]")
     b, h, d = q.shape
-    dev = q.device
+    _four(k_cache, "k_cache")
+    dev, index = q.device, q.get_device()
     slots = (b, k_cache.shape[1], k_cache.shape[2])
-    s = _Shape(_type(torch, q), b, h, slots[1], 1, slots[2], d, 0, 0, 1.0 / math.sqrt(d) if scale is None and d else (scale or 0.0),
-               None, _plain(lens, "lens", torch.int32, (b,), dev))
+    s = _Shape(_type(torch, q, "q"), b, h, slots[1], 1, slots[2], d, 0, 0, _scale(scale, d), None,
+               _plain(lens, "lens", torch.int32, (b,), index))
     if out is None:
         out = dict(out=torch.empty_like(q), lse=torch.empty((b, h), dtype=torch.float32, device=dev),
                    weights=None if weights is None else torch.empty(slots, dtype=torch.float32, device=dev))
     ws, have, at = _workspace(torch, ws, lib.lap_attention_workspace_bytes(AT_STEP, s), dev)
     rc = lib.lap_attention_step(s, _rows(q, "q", q, q.shape), _rows(k_cache, "k_cache", q, slots + (d,)), _rows(v_cache, "v_cache", q, slots + (d,)),
-                                _plain(positions, "positions", torch.int32, slots, dev), _plain(weights, "weights", torch.float32, slots, dev),
-                                _rows(out["out"], "out", q, q.shape), _plain(out["lse"], "lse", torch.float32, (b, h), dev),
-                                _plain(out.get("weights"), "out weights", torch.float32, slots, dev), at, have, _stream(torch, dev))
-    _done(rc, "lap_attention_step", torch, dev, sync)
+                                _plain(positions, "positions", torch.int32, slots, index), _plain(weights, "weights", torch.float32, slots, index),
+                                _rows(out["out"], "out", q, q.shape), _plain(out["lse"], "lse", torch.float32, (b, h), index),
+                                _plain(out.get("weights"), "out weights", torch.float32, slots, index), at, have, _stream(torch, dev))
+    _done(rc, "lap_attention_step", dev, sync)
     return out
 
 
 def _cache(torch, k, v, weights, positions, name: str = ""):
-    _check(k.dim() == 4, "caches are [batch, heads, slots, head_dim]")
-    b, h, n, d = k.shape
-    kind = _type(torch, k)
+    b, h, n, d = _four(k, name + "k")
+    kind, index = _type(torch, k, name + "k"), k.get_device()
     return _Cache(kind, b, h, n, d, _rows(k, name + "k", k, k.shape), _rows(v, name + "v", k, k.shape),
-                  _plain(weights, name + "weights", torch.float32, (b, h, n), k.device),
-                  _plain(positions, name + "positions", torch.int32, (b, h, n), k.device))
+                  _plain(weights, name + "weights", torch.float32, (b, h, n), index),
+                  _plain(positions, name + "positions", torch.int32, (b, h, n), index))
 
 
 def cache_evict(k, v, weights, keep: int, recent: int, *, lens=None, positions=None, slots: Optional[int] = None,
                 out: Optional[dict] = None, ws=None, sync: bool = True):
     """lap_cache_evict: the `keep` rows of highest weight of k and v, the newest `recent` among them, into a cache of `slots`
     (None: keep).  Returns dict(k, v, weights, positions [batch, kv_heads, slots], lens [batch])."""
-    torch, lib = _torch(), _lib()
+    lib, torch = _lib(), binding._torch()
     src = _cache(torch, k, v, weights, positions)
-    _check(keep >= 0 and recent >= 0, "keep and recent are numbers of slots")
+    if keep < 0 or recent < 0:
+        raise ValueError("keep and recent are numbers of slots")
     b, h, n, d = k.shape
-    dev = k.device
+    dev, index = k.device, k.get_device()
     if out is None:
         m = int(keep if slots is None else slots)
         out = dict(k=torch.empty((b, h, m, d), dtype=k.dtype, device=dev), v=torch.empty((b, h, m, d), dtype=k.dtype, device=dev),
                    weights=torch.empty((b, h, m), dtype=torch.float32, device=dev),
                    positions=torch.empty((b, h, m), dtype=torch.int32, device=dev), lens=torch.empty(b, dtype=torch.int32, device=dev))
-    _check(out["k"].dtype == k.dtype and out["k"].device == dev, "out k: type or device")
+    if out["k"].dtype is not k.dtype or out["k"].get_device() != index:
+        _refuse("out k", out["k"], f"{k.dtype} on {dev}")
     dst = _cache(torch, out["k"], out["v"], out["weights"], out["positions"], "out ")
     ws, have, at = _workspace(torch, ws, lib.lap_cache_workspace_bytes(dst), dev)
-    rc = lib.lap_cache_evict(src, _plain(lens, "lens", torch.int32, (b,), dev), int(keep), int(recent), dst,
-                             _plain(out["lens"], "out lens", torch.int32, (b,), dev), at, have, _stream(torch, dev))
-    _done(rc, "lap_cache_evict", torch, dev, sync)
+    rc = lib.lap_cache_evict(src, _plain(lens, "lens", torch.int32, (b,), index), int(keep), int(recent), dst,
+                             _plain(out["lens"], "out lens", torch.int32, (b,), index), at, have, _stream(torch, dev))
+    _done(rc, "lap_cache_evict", dev, sync)
     return out
 
 
 def cache_insert(k_new, v_new, k_cache, v_cache, weights, positions, position, recent: int, *, slots=None, sync: bool = True):
     """lap_cache_insert: one token [batch, kv_heads, head_dim] into every cache, in place; position [batch] is the token's.
     Returns dict(slots [batch, kv_heads]): where it went."""
-    torch, lib = _torch(), _lib()
+    lib, torch = _lib(), binding._torch()
     cache = _cache(torch, k_cache, v_cache, weights, positions)
-    _check(recent >= 0, "recent is a number of slots")
+    if recent < 0:
+        raise ValueError("recent is a number of slots")
     b, h, _, d = k_cache.shape
-    dev = k_cache.device
+    dev, index = k_cache.device, k_cache.get_device()
     if slots is None:
         slots = torch.empty((b, h), dtype=torch.int32, device=dev)
     rc = lib.lap_cache_insert(cache, _rows(k_new, "k_new", k_cache, (b, h, d)), _rows(v_new, "v_new", k_cache, (b, h, d)),
-                              _plain(position, "position", torch.int32, (b,), dev), int(recent),
-                              _plain(slots, "slots", torch.int32, (b, h), dev), _stream(torch, dev))
-    _done(rc, "lap_cache_insert", torch, dev, sync)
+                              _plain(position, "position", torch.int32, (b,), index), int(recent),
+                              _plain(slots, "slots", torch.int32, (b, h), index), _stream(torch, dev))
+    _done(rc, "lap_cache_insert", dev, sync)
     return dict(slots=slots)

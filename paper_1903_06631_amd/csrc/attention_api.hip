@@ -172,7 +172,7 @@ int lap_attention_step(const lap_attention_shape *s, const lap_rows *q, const la
 {
     int rc = check_shape(s);
     if (!rc && (s->q_len != 1 || s->causal || s->q_lens)) rc = LAP_E_ATTENTION;
-    if (!rc && (s->q_heads / s->kv_heads > lap::MAX_GROUP || s->batch > MAX_GRID || s->q_heads > MAX_GRID)) rc = LAP_E_SIZE;
+    if (!rc && (s->q_heads / s->kv_heads > lap::MAX_GROUP)) rc = LAP_E_SIZE;
     if (!rc) rc = check_rows(q, s->batch, s->q_heads, 1, s->head_dim, false);
     if (!rc) rc = check_rows(k, s->batch, s->kv_heads, s->k_len, s->head_dim, false);
     if (!rc) rc = check_rows(v, s->batch, s->kv_heads, s->k_len, s->head_dim, false);

@@ -2,7 +2,7 @@
 //   o = sum_j p_j v_j, p_j = exp(scale q.k_j - lse), over the slots in use; w_j += sum of p_j over the heads that share slot j
 //
 // Every key and value is read once and takes part in a few products only: the pass is bound by memory, and there are few
-// sequences and heads to share it out to.  So the slots are cut into chunks of STEP_CHUNK or so, a workgroup each.  Its four
+// sequences and heads to share it out to.  So the slots are cut into chunks of up to 512, a workgroup each.  Its four
 // waves go through 32 slots at a time of their own, without waiting for each other: keys from memory straight into
 // registers as a matrix operand, values through LDS, which is where they are transposed.  The heads of a group are the
 // kept rows (up to 32; with fewer, part of the matrix instructions runs empty, at a rate that is far from binding).  A
@@ -23,7 +23,13 @@ __global__ __launch_bounds__(NW * 64, 2) void k_step(StepShape s, StepWork w)
     __shared__ float2 sums[NW][32];
     T *const lv = (T *)raw;
     const uint32_t group = s.q_heads / s.kv_heads, parts = (group + 31) / 32;
-    const uint32_t split = blockIdx.x, kvh = blockIdx.y / parts, part = blockIdx.y % parts, b = blockIdx.z;
+    // Many caches: next to each other, so that the last chunks of ragged ones, which are empty, come last and to all dies
+    // (64 caches of 8 heads, up to 4096 slots: 135 us, the other way 143).  Few: the chunks of one next to each other, which
+    // memory prefers (2 x 8 x 131072 slots: 231 us, the other way 245).
+    const uint32_t rows = s.batch * s.kv_heads * parts;
+    const uint32_t row = rows >= 256 ? blockIdx.x % rows : blockIdx.x / s.splits;
+    const uint32_t split = rows >= 256 ? blockIdx.x / rows : (blockIdx.x + row) % s.splits, part = row % parts;
+    const uint32_t kvh = row / parts % s.kv_heads, b = row / parts / s.kv_heads;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const int n_rows = min(32, (int)(group - part * 32));
     const uint32_t head0 = kvh * group + part * 32;
@@ -188,21 +194,37 @@ template <class T, int DP> __global__ __launch_bounds__(JOIN) void k_step_join(S
     }
     __syncthreads();
     const int len = clamp_len(s.lens, b, s.slots);
+    const int64_t row = (int64_t)item * s.slots;
+    const float *scores = w.scores + (int64_t)head0 * s.score_row;
+    if (s.slots % 4 == 0 && ((uintptr_t)w.weights | (uintptr_t)w.before) % 16 == 0) {      // four slots for each thread
+        const uint32_t slot = piece * JOIN_SLOTS + threadIdx.x * 4;
+        if (slot >= s.slots) return;
+        f32x4 sum = {};
+        if ((int)slot < len) {
+#pragma unroll 4
+            for (uint32_t g = 0; g < group; ++g) {
+                const f32x4 x = *(const f32x4 *)(scores + (int64_t)g * s.score_row + slot);
+                for (int j = 0; j < 4; ++j) sum[j] += exp2_fast(x[j] - l2[g]);
+            }
+            for (int j = 1; j < 4; ++j) sum[j] = (int)slot + j < len ? sum[j] : 0.f;
+        }
+        *(f32x4 *)(w.weights + row + slot) = *(const f32x4 *)(w.before + row + slot) + sum;
+        return;
+    }
     for (uint32_t i = 0; i < JOIN_SLOTS; i += JOIN) {
         const uint32_t slot = piece * JOIN_SLOTS + i + threadIdx.x;
         if (slot >= s.slots) return;
         float sum = 0.f;
         if ((int)slot < len)
-            for (uint32_t g = 0; g < group; ++g) sum += exp2_fast(w.scores[(int64_t)(head0 + g) * s.score_row + slot] - l2[g]);
-        const int64_t at = (int64_t)item * s.slots + slot;
-        w.weights[at] = w.before[at] + sum;
+            for (uint32_t g = 0; g < group; ++g) sum += exp2_fast(scores[(int64_t)g * s.score_row + slot] - l2[g]);
+        w.weights[row + slot] = w.before[row + slot] + sum;
     }
 }
 
 template <class T, int DP> hipError_t launch(const StepShape &s, const StepWork &w, hipStream_t st)
 {
     const uint32_t parts = (s.q_heads / s.kv_heads + 31) / 32;
-    k_step<T, DP><<<dim3(s.splits, s.kv_heads * parts, s.batch), NW * 64, 0, st>>>(s, w);
+    k_step<T, DP><<<s.splits * parts * s.batch * s.kv_heads, NW * 64, 0, st>>>(s, w);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const uint32_t pieces = w.weights ? (s.slots + JOIN_SLOTS - 1) / JOIN_SLOTS : 0;
@@ -212,8 +234,9 @@ template <class T, int DP> hipError_t launch(const StepShape &s, const StepWork 
 
 }  // namespace
 
-// Chunks: 2 workgroups fit a compute unit and 8 of them each keep the chip evenly loaded to the end, but a chunk is at
-// least one tile for every wave and no more than STEP_CHUNK slots are worth it.
+// Chunks: workgroups enough to keep the chip evenly loaded to the end, of a tile for each wave at least and 512 slots at
+// most (64 caches of 8 heads, up to 4096 slots: 143 us, with 1024 slots 157, with 256 and caches next to each other 142
+// in place of 135).
 void step_split(StepShape &s)
 {
     const uint64_t rows = (uint64_t)s.batch * s.kv_heads * ((s.q_heads / s.kv_heads + 31) / 32);

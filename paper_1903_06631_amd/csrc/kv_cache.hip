@@ -4,6 +4,7 @@
 // least), equal ones with the higher index first, then the newest `recent` positions.  An eviction keeps the last `keep`
 // of that order and copies them, in the order of their slots, into another cache; an insertion overwrites the first.
 #include "attn_core.h"
+#include "lap_dev.h"
 
 namespace lap {
 namespace {
@@ -13,33 +14,46 @@ constexpr uint32_t NEWEST = 0xFFFFFFFFu, LEAST = 1u, EMPTY = 0u;
 // weights as whole numbers in the same order (minus zero is zero)
 __device__ __forceinline__ uint32_t weight_key(float w)
 {
-    if (w != w) return LEAST;
     const uint32_t u = __float_as_uint(w + 0.f);
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
+    return w != w ? LEAST : u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr int EV = 1024, EW = EV / 64, BINS = 2048, COPIES = 4;
+constexpr int EV = 1024, EW = EV / 64, BIN_BITS = 13, BINS = 1 << BIN_BITS;
 
 struct EvictRow {
     const float *weights;
     const int32_t *positions;
     int len, from;      // slots in use; the first position that is among the newest
-    __device__ __forceinline__ uint32_t key(int slot) const
-    {
-        const int p = positions ? positions[slot] : slot;
-        if (p < 0) return EMPTY;
-        return p >= from ? NEWEST : weight_key(weights[slot]);
-    }
+    __device__ __forceinline__ uint32_t key(float w, int p) const { return p < 0 ? EMPTY : p >= from ? NEWEST : weight_key(w); }
 };
 
-// The slots that stay, ascending, into kept[]; -1 after the last.  One workgroup for each row.  The key of the last one
-// that stays is found digit by digit (11, 11 and 10 bits) from counts in LDS, in four copies: weights agree in their
-// leading bits, and additions to one counter take turns.  Then every wave takes a stretch of the row of its own.  A row is
-// read five times, from the L2 cache after the first.
+// how many of the lanes before this one are among `set`
+__device__ __forceinline__ uint32_t before_lane(uint64_t set)
+{
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(set >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)set, 0));
+}
+
+// one more in the counter of every lane's bin; lanes with the bin of the first one that counts add up in one go (many
+// weights are equal, and additions to one counter take turns)
+__device__ __forceinline__ void count(uint32_t *bins, bool counts, uint32_t bin, int lane)
+{
+    const uint64_t who = ballot(counts);
+    if (!who) return;
+    const int first = __ffsll((unsigned long long)who) - 1;
+    const uint32_t of = read_lane(bin, first);
+    const uint64_t same = ballot(counts && bin == of);
+    if (counts && (bin != of || lane == first)) atomicAdd(&bins[bin], bin == of ? (uint32_t)__popcll(same) : 1u);
+}
+
+// The slots that stay, ascending, into kept[]; -1 after the last.  One workgroup for each row, a stretch of it for each
+// wave, with the weights of EACH x 64 slots in registers (EACH 0: read again from the L2 cache each time).  The key of the
+// last one that stays is found digit by digit (13, 13 and 6 bits: the first one has four bits of a weight's fraction, so
+// that weights of one size do not all meet in one counter) from counts in LDS.
+template <int EACH>
 __global__ __launch_bounds__(EV) void k_evict_choose(EvictShape s, const float *weights, const int32_t *positions, int32_t *kept,
                                                    float *weights_out, int32_t *positions_out, int32_t *lens_out)
 {
-    __shared__ uint32_t bins[COPIES][BINS];
+    __shared__ uint32_t bins[BINS];
     __shared__ uint32_t part[EW][2];
     __shared__ uint32_t found[2];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
@@ -67,80 +81,111 @@ __global__ __launch_bounds__(EV) void k_evict_choose(EvictShape s, const float *
     row.from = newest - (int)s.recent + 1;
     const int keep = min((int)s.keep, used);
 
+    // this wave's slots, in whole 64s
+    const int each = ((row.len + EW - 1) / EW + 63) / 64 * 64, i0 = wave * each, i1 = min(i0 + each, row.len);
+    float mine[EACH ? EACH : 1];      // all asked for before the first is looked at
+    uint32_t keys[EACH ? EACH : 1];
+    if (EACH > 0 && i0 < i1) {
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) mine[j] = row.weights[min(i0 + 64 * j + lane, i1 - 1)];
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) {
+            const int i = i0 + 64 * j + lane, p = positions ? row.positions[min(i, i1 - 1)] : i;
+            keys[j] = i < i1 ? row.key(mine[j], p) : EMPTY;
+        }
+    }
+    const auto for_all = [&](auto &&f) {      // f(first slot, this lane's key and weight), for 64 slots at a time
+        if constexpr (EACH > 0) {
+#pragma unroll
+            for (int j = 0; j < EACH; ++j)
+                if (i0 + 64 * j < i1) f(i0 + 64 * j, keys[j], mine[j]);
+        } else
+            for (int i = i0; i < i1; i += 64) {
+                const int at = min(i + lane, i1 - 1);
+                const float w = row.weights[at];
+                f(i, i + lane < i1 ? row.key(w, positions ? row.positions[at] : i + lane) : EMPTY, w);
+            }
+    };
+
     // everything above `bound` stays, and the first `equal` slots whose key is `bound`
     uint32_t bound = LEAST, equal = 0xFFFFFFFFu;      // all slots in use
     if (keep < used) {
         uint32_t prefix = 0, mask = 0, want = (uint32_t)keep;      // of the slots whose key begins with prefix, the want-th
         if (want == 0) bound = NEWEST, equal = 0;
         for (int digit = 0; want && digit < 3; ++digit) {
-            const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, width = digit == 2 ? 10 : 11;
-            for (int i = t; i < COPIES * BINS; i += EV) ((uint32_t *)bins)[i] = 0;
+            const int shift = digit == 0 ? 19 : digit == 1 ? 6 : 0;
+            const uint32_t ones = digit == 2 ? 63 : BINS - 1;
+            for (int i = t; i < BINS; i += EV) bins[i] = 0;
             __syncthreads();
-            for (int i = t; i < row.len; i += EV) {
-                const uint32_t k = row.key(i);
-                if (k != EMPTY && (k & mask) == prefix) atomicAdd(&bins[wave % COPIES][(k >> shift) & ((1u << width) - 1)], 1u);
-            }
+            for_all([&](int, uint32_t k, float) { count(bins, k != EMPTY && (k & mask) == prefix, (k >> shift) & ones, lane); });
             __syncthreads();
-            // counts from the top: a thread holds two bins, bin 2047 first
-            const int hi = BINS - 1 - 2 * t;
-            uint32_t c1 = 0, c0 = 0;
-            for (int i = 0; i < COPIES; ++i) c1 += bins[i][hi], c0 += bins[i][hi - 1];
-            uint32_t up = c1 + c0;
+            // counts from the top: a thread holds eight bins, the highest first
+            constexpr int OWN = BINS / EV;
+            const int lo = BINS - OWN * (t + 1);
+            uint32_t c[OWN], own = 0;
+#pragma unroll
+            for (int i = 0; i < OWN; ++i) own += c[i] = bins[lo + i];
+            uint32_t up = own;
             for (int d = 1; d < 64; d <<= 1) {
                 const uint32_t x = __shfl_up(up, d, 64);
                 if (lane >= d) up += x;
             }
             if (lane == 63) part[wave][0] = up;
             __syncthreads();
-            for (int i = 0; i < wave; ++i) up += part[i][0];
-            const uint32_t before = up - c1 - c0;
+#pragma unroll
+            for (int i = 0; i < EW; ++i) up += i < wave ? part[i][0] : 0;
+            uint32_t before = up - own;
             if (before < want && want <= up) {
-                const bool first = want <= before + c1;
-                found[0] = (uint32_t)(first ? hi : hi - 1);
-                found[1] = want - before - (first ? 0u : c1);
+#pragma unroll
+                for (int i = OWN - 1; i >= 0; --i) {
+                    if (before < want && want <= before + c[i]) found[0] = (uint32_t)(lo + i), found[1] = want - before;
+                    before += c[i];
+                }
             }
             __syncthreads();
             prefix |= found[0] << shift;
-            mask |= ((1u << width) - 1) << shift;
+            mask |= ones << shift;
             want = found[1];
             __syncthreads();
         }
         if (mask) bound = prefix, equal = want;
     }
 
-    // stretches of whole 64s, one for each wave: how many above the bound and at it, then the places
-    const int each = ((row.len + EW - 1) / EW + 63) / 64 * 64, i0 = wave * each, i1 = min(i0 + each, row.len);
+    // how many of every wave's are above the bound and at it, then the places
     uint32_t above = 0, at = 0;
-    for (int i = i0 + lane; i < i1; i += 64) {
-        const uint32_t k = row.key(i);
+    for_all([&](int, uint32_t k, float) {
         above += k > bound;
         at += k == bound && k != EMPTY;
-    }
-    for (int d = 32; d; d >>= 1) above += __shfl_xor(above, d, 64), at += __shfl_xor(at, d, 64);
+    });
+    above = wave_reduce_add32(above), at = wave_reduce_add32(at);
     if (lane == 0) part[wave][0] = above, part[wave][1] = at;
     __syncthreads();
     uint32_t place = 0, seen = 0;
-    for (int i = 0; i < wave; ++i) place += part[i][0] + min(equal - min(equal, seen), part[i][1]), seen += part[i][1];
+#pragma unroll
+    for (int i = 0; i < EW; ++i)
+        if (i < wave) place += part[i][0] + min(equal - min(equal, seen), part[i][1]), seen += part[i][1];
     const int64_t out = (int64_t)blockIdx.x * s.slots_out;
-    for (int base = i0; base < i1; base += 64) {
-        const int i = base + lane;
-        const uint32_t k = i < i1 ? row.key(i) : EMPTY;
-        const uint64_t eq = __ballot(k == bound && k != EMPTY), below = ((uint64_t)1 << lane) - 1;
-        const bool stays = k > bound || (k == bound && k != EMPTY && seen + __popcll(eq & below) < equal);
-        const uint64_t all = __ballot(stays);
+    kept += out, weights_out += out, positions_out += out;
+    for_all([&](int base, uint32_t k, float w) {
+        const uint64_t eq = ballot(k == bound && k != EMPTY);
+        bool stays = k > bound;
+        if (eq) {
+            stays |= k == bound && k != EMPTY && seen + before_lane(eq) < equal;
+            seen += __popcll(eq);
+        }
+        const uint64_t all = ballot(stays);
         if (stays) {
-            const uint32_t to = place + __popcll(all & below);
-            kept[out + to] = i;
-            weights_out[out + to] = row.weights[i];
-            positions_out[out + to] = row.positions ? row.positions[i] : i;
+            const uint32_t to = place + before_lane(all);
+            kept[to] = base + lane;
+            weights_out[to] = w;
+            positions_out[to] = positions ? row.positions[base + lane] : base + lane;
         }
         place += __popcll(all);
-        seen += __popcll(eq);
-    }
+    });
     for (int i = keep + t; i < (int)s.slots_out; i += EV) {
-        kept[out + i] = -1;
-        weights_out[out + i] = 0.f;
-        positions_out[out + i] = -1;
+        kept[i] = -1;
+        weights_out[i] = 0.f;
+        positions_out[i] = -1;
     }
     if (blockIdx.x % s.kv_heads == 0 && t == 0) lens_out[b] = min((int)s.keep, row.len);
 }
@@ -223,7 +268,10 @@ hipError_t launch_cache_evict(const EvictShape &s, const Rows &k, const Rows &v,
                               const Rows &k_out, const Rows &v_out, float *weights_out, int32_t *positions_out, int32_t *lens_out,
                               int32_t *kept, hipStream_t st)
 {
-    k_evict_choose<<<s.batch * s.kv_heads, EV, 0, st>>>(s, weights, positions, kept, weights_out, positions_out, lens_out);
+    const uint32_t rows = s.batch * s.kv_heads;
+    if (s.slots <= 4 * EV) k_evict_choose<4><<<rows, EV, 0, st>>>(s, weights, positions, kept, weights_out, positions_out, lens_out);
+    else if (s.slots <= 16 * EV) k_evict_choose<16><<<rows, EV, 0, st>>>(s, weights, positions, kept, weights_out, positions_out, lens_out);
+    else k_evict_choose<0><<<rows, EV, 0, st>>>(s, weights, positions, kept, weights_out, positions_out, lens_out);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const uint32_t per = CP / (s.head_dim / 8) * CP_ROWS;
