@@ -8,14 +8,14 @@
 namespace lap {
 namespace {
 
-constexpr int KT = 64;      // keys of a tile
-
-template <class T, int DP, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnShape s, Rows q, Rows k, Rows v, Rows o, float *lse, uint32_t tiles)
+// QW blocks of 32 rows; their keys are dealt to KG waves each, NB blocks of 32 keys at a time.  Where rows are few, waves that
+// share them fill the units that would have none; they join their sums at the end.
+template <class T, int DP, int QW, int KG, int NB>
+__global__ __launch_bounds__(QW * KG * 64, 2) void k_attention(AttnShape s, Rows q, Rows k, Rows v, Rows o, float *lse, uint32_t tiles)
 {
-    constexpr int BQ = 32 * NW;
-    __shared__ __align__(16) T lk[2][Tile<DP>::size(KT)];
-    __shared__ __align__(16) T lv[2][Tile<DP>::size(KT)];
+    constexpr int NW = QW * KG, BQ = 32 * QW, KT = 32 * KG * NB;
+    __shared__ __align__(16) T tiles_kv[4][Tile<DP>::size(KT)];
+    T(*const lk)[Tile<DP>::size(KT)] = tiles_kv, (*const lv)[Tile<DP>::size(KT)] = tiles_kv + 2;
     const uint32_t group = s.q_heads / s.kv_heads;
     Work wk;
     if (!work_item(s, group, wk)) return;
@@ -24,7 +24,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnShape s, Rows q, R
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Span sp = span_of(s, b);
 
-    const int w0 = first + 32 * wave;               // this wave's rows
+    const int qw = wave % QW, kg = wave / QW;
+    const int w0 = first + 32 * qw;                 // this wave's rows
     const int row = w0 + (lane & 31);
     T *orow = (T *)o.data + (int64_t)b * o.batch + (int64_t)h * o.head + (int64_t)row * o.row;
     float *lrow = lse + ((int64_t)b * s.q_heads + h) * s.q_len + row;
@@ -59,17 +60,18 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnShape s, Rows q, R
                 tk.issue(lk[buf ^ 1], gk, kt + KT, last, wave);
                 tv.issue(lv[buf ^ 1], gv, kt + KT, last, wave);
             }
-            if (kt >= any_hi || kt + KT <= any_lo) continue;
-            f32x16 x[2] = {};
+            const int mine = kt + 32 * NB * kg;
+            if (mine >= any_hi || mine + 32 * NB <= any_lo) continue;
+            f32x16 x[NB] = {};
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+            for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
-                for (int d = 0; d < DP / 16; ++d) x[kb] = Elem<T>::mfma(rows.get(lk[buf], kb, d), qf[d], x[kb]);
-            reads_ahead<DP / 8, 1, 8>();
-            if (kt + KT > all_hi || kt < all_lo) {
-                const int at = kt + 4 * (lane >> 5);
+                for (int d = 0; d < DP / 16; ++d) x[kb] = Elem<T>::mfma(rows.get(lk[buf], NB * kg + kb, d), qf[d], x[kb]);
+            reads_ahead<NB * DP / 16, 1, NB * DP / 32>();
+            if (mine + 32 * NB > all_hi || mine < all_lo) {
+                const int at = mine + 4 * (lane >> 5);
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
+                for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int key = at + 32 * kb + 8 * (i / 4) + i % 4;
@@ -78,7 +80,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnShape s, Rows q, R
             }
             float top = x[0][0];
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+            for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) top = fmaxf(top, x[kb][i]);
             top = half_max(top);
@@ -96,7 +98,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnShape s, Rows q, R
             const float mc = m * c;
             float part = 0.f;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
+            for (int t = 0; t < 2 * NB; ++t) {
                 float p[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -105,12 +107,37 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnShape s, Rows q, R
                 }
                 const auto pf = round8<T>(p, 0);
 #pragma unroll
-                for (int d = 0; d < DP / 32; ++d) acc[d] = Elem<T>::mfma(cols.get(lv[buf], t, d), pf, acc[d]);
+                for (int d = 0; d < DP / 32; ++d) acc[d] = Elem<T>::mfma(cols.get(lv[buf], 2 * NB * kg + t, d), pf, acc[d]);
             }
             l += part;
         }
     }
     l = half_sum(l);
+    if constexpr (KG > 1) {
+        __shared__ float2 sums[KG][QW][32];
+        static_assert((KG - 1) * QW * DP / 2 * 64 * sizeof(float) <= sizeof(tiles_kv), "the sums fit where the tiles were");
+        float *const box = (float *)tiles_kv + qw * (DP / 2 * 64);
+        __syncthreads();
+        if (kg > 0) {
+            put_sums(box + (kg - 1) * QW * (DP / 2 * 64), acc, lane);
+            if (lane < 32) sums[kg][qw][lane] = make_float2(m, l);
+        }
+        __syncthreads();
+        if (kg > 0) return;
+        const float c = s.scale * LOG2E;
+#pragma unroll 1
+        for (int g = 1; g < KG; ++g) {
+            const float2 other = sums[g][qw][lane & 31];
+            const float up = fmaxf(m, other.x), by = exp2_fast((m - up) * c), times = exp2_fast((other.x - up) * c);
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[d][i] *= by;
+            add_sums(box + (g - 1) * QW * (DP / 2 * 64), acc, times, lane);
+            l = l * by + other.y * times;
+            m = up;
+        }
+    }
     if (row < (int)s.q_len) {
         const bool some = row < sp.ql && l != 0.f;      // (a sum that is not a number is some)
         if (!some)
@@ -121,14 +148,23 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnShape s, Rows q, R
     }
 }
 
+template <class T, int DP, int QW, int KG, int NB>
+hipError_t launch_as(const AttnShape &s, const Rows &q, const Rows &k, const Rows &v, const Rows &out, float *lse, hipStream_t st)
+{
+    const uint32_t tiles = (s.q_len + 32 * QW - 1) / (32 * QW);
+    const uint32_t total = padded_caches(s.batch * s.kv_heads) * (s.q_heads / s.kv_heads) * tiles;
+    k_attention<T, DP, QW, KG, NB><<<total, QW * KG * 64, 0, st>>>(s, q, k, v, out, lse, tiles);
+    return hipGetLastError();
+}
+
 template <class T, int DP>
 hipError_t launch(const AttnShape &s, const Rows &q, const Rows &k, const Rows &v, const Rows &out, float *lse, hipStream_t st)
 {
-    constexpr int NW = 4;
-    const uint32_t tiles = (s.q_len + 32 * NW - 1) / (32 * NW);
-    const uint32_t total = padded_caches(s.batch * s.kv_heads) * (s.q_heads / s.kv_heads) * tiles;
-    k_attention<T, DP, NW><<<total, NW * 64, 0, st>>>(s, q, k, v, out, lse, tiles);
-    return hipGetLastError();
+    switch (share_of((uint64_t)s.batch * s.q_heads * ((s.q_len + 127) / 128))) {
+    case Share::FOUR: return launch_as<T, DP, 4, 1, 2>(s, q, k, v, out, lse, st);
+    case Share::FOUR_BY_TWO: return launch_as<T, DP, 4, 2, 2>(s, q, k, v, out, lse, st);
+    default: return launch_as<T, DP, 2, 4, 1>(s, q, k, v, out, lse, st);
+    }
 }
 
 }  // namespace

@@ -11,16 +11,14 @@
 namespace lap {
 namespace {
 
-constexpr int KT = 64;      // keys of a tile of the first kernel
-constexpr int QT = 32;      // rows of a tile of the second
-
-template <class T, int DP, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void k_attention_dq(AttnShape s, Rows g, Rows q, Rows k, Rows v, Rows o, const float *lse,
+// QW blocks of 32 rows, the keys of each dealt to KG waves, a block of 32 at a time of KT
+template <class T, int DP, int QW, int KG, int KT>
+__global__ __launch_bounds__(QW * KG * 64, 2) void k_attention_dq(AttnShape s, Rows g, Rows q, Rows k, Rows v, Rows o, const float *lse,
                                                           Rows dq, float *stats, uint32_t tiles)
 {
-    constexpr int BQ = 32 * NW;
-    __shared__ __align__(16) T lk[2][Tile<DP>::size(KT)];
-    __shared__ __align__(16) T lv[2][Tile<DP>::size(KT)];
+    constexpr int NW = QW * KG, BQ = 32 * QW;
+    __shared__ __align__(16) T tiles_kv[4][Tile<DP>::size(KT)];
+    T(*const lk)[Tile<DP>::size(KT)] = tiles_kv, (*const lv)[Tile<DP>::size(KT)] = tiles_kv + 2;
     const uint32_t group = s.q_heads / s.kv_heads;
     Work wk;
     if (!work_item(s, group, wk)) return;
@@ -29,7 +27,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_dq(AttnShape s, Rows g
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Span sp = span_of(s, b);
 
-    const int w0 = first + 32 * wave;
+    const int qw = wave % QW, kg = wave / QW;
+    const int w0 = first + 32 * qw;
     const int row = w0 + (lane & 31);
     T *drow = (T *)dq.data + (int64_t)b * dq.batch + (int64_t)h * dq.head + (int64_t)row * dq.row;
     const int64_t at = ((int64_t)b * s.q_heads + h) * s.q_len;
@@ -55,7 +54,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_dq(AttnShape s, Rows g
         }
         // a row without keys gets probabilities of zero
         const float sum = lse[at + used], l2 = sum == -ATTN_INF ? ATTN_INF : sum * LOG2E;
-        if (row < sp.ql && lane < 32) {
+        if (row < sp.ql && lane < 32 && kg == 0) {
             stats[at + row] = l2;
             stats[(int64_t)s.batch * s.q_heads * s.q_len + at + row] = delta;
         }
@@ -81,10 +80,10 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_dq(AttnShape s, Rows g
                     tk.issue(lk[buf ^ 1], gk, kt + KT, sp.kl - 1, wave);
                     tv.issue(lv[buf ^ 1], gv, kt + KT, sp.kl - 1, wave);
                 }
-                if (kt >= any_hi || kt + KT <= any_lo) continue;
-                const bool whole = kt + KT <= all_hi && kt >= all_lo;
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
+                for (int n = 0; n < KT / 32 / KG; ++n) {
+                    const int kb = KT / 32 / KG * kg + n, at = kt + 32 * kb;
+                    if (at >= any_hi || at + 32 <= any_lo) continue;
                     f32x16 x = {}, y = {};
 #pragma unroll
                     for (int d = 0; d < DP / 16; ++d) x = Elem<T>::mfma(rows.get(lk[buf], kb, d), qf[d], x);
@@ -93,8 +92,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_dq(AttnShape s, Rows g
                     float ds[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) ds[i] = exp2_fast(__builtin_fmaf(x[i], c, -l2)) * (y[i] - delta);
-                    if (!whole) {
-                        const int key0 = kt + 4 * (lane >> 5) + 32 * kb;
+                    if (at + 32 > all_hi || at < all_lo) {
+                        const int key0 = at + 4 * (lane >> 5);
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const int key = key0 + 8 * (i / 4) + i % 4;
@@ -111,6 +110,16 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_dq(AttnShape s, Rows g
             }
         }
     }
+    if constexpr (KG > 1) {
+        static_assert((KG - 1) * QW * DP / 2 * 64 * sizeof(float) <= sizeof(tiles_kv), "the sums fit where the tiles were");
+        float *const box = (float *)tiles_kv + qw * (DP / 2 * 64);
+        __syncthreads();
+        if (kg > 0) put_sums(box + (kg - 1) * QW * (DP / 2 * 64), acc, lane);
+        __syncthreads();
+        if (kg > 0) return;
+#pragma unroll
+        for (int n = 1; n < KG; ++n) add_sums(box + (n - 1) * QW * (DP / 2 * 64), acc, 1.f, lane);
+    }
     if (row < (int)s.q_len) {
         if (row >= sp.ql)
 #pragma unroll
@@ -119,19 +128,20 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_dq(AttnShape s, Rows g
     }
 }
 
-template <class T, int DP, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void k_attention_dkv(AttnShape s, Rows g, Rows q, Rows k, Rows v, const float *stats, Rows dk,
+// KW blocks of 32 keys, the rows of each dealt to RG waves, a block of 32 at a time
+template <class T, int DP, int KW, int RG>
+__global__ __launch_bounds__(KW * RG * 64, 2) void k_attention_dkv(AttnShape s, Rows g, Rows q, Rows k, Rows v, const float *stats, Rows dk,
                                                            Rows dv, uint32_t tiles)
 {
-    constexpr int BK = 32 * NW;
-    __shared__ __align__(16) T lq[2][Tile<DP>::size(QT)];
-    __shared__ __align__(16) T lg[2][Tile<DP>::size(QT)];
+    constexpr int NW = KW * RG, BK = 32 * KW, QT = 32 * RG;
+    __shared__ __align__(16) T tiles_qg[4][Tile<DP>::size(QT)];
+    T(*const lq)[Tile<DP>::size(QT)] = tiles_qg, (*const lg)[Tile<DP>::size(QT)] = tiles_qg + 2;
     // The values of the kept rows are read from here: in registers they and the sums of two waves on a SIMD do not fit, and
     // what the compiler then keeps in memory has to be waited for together with the next tile (8 x 16 heads x 2048 tokens x
     // 128: both passes 566 us; with 26 registers in memory 753, with one wave on a SIMD 668).
     __shared__ __align__(16) T lkept[Tile<DP>::size(BK)];
-    __shared__ __align__(16) float lst[2][2][64];
-    static_assert(QT <= 64, "a wave fetches the numbers of 64 rows at once");
+    constexpr int PARTS = (QT + 63) / 64;      // a wave fetches the numbers of 64 rows at once
+    __shared__ __align__(16) float lst[2][2][64 * PARTS];
     Work wk;
     if (!work_item(s, 1, wk)) return;
     const uint32_t b = wk.b, kvh = wk.kvh;
@@ -140,7 +150,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_dkv(AttnShape s, Rows 
     const Span sp = span_of(s, b);
     const uint32_t group = s.q_heads / s.kv_heads;
 
-    const int w0 = first + 32 * wave;
+    const int kw = wave % KW, rg = wave / KW;
+    const int w0 = first + 32 * kw;
     const int key = w0 + (lane & 31);
     f32x16 ak[DP / 32] = {}, av[DP / 32] = {};
     const int end = min(first + BK, sp.kl);
@@ -150,7 +161,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_dkv(AttnShape s, Rows 
         const int used = min(key, sp.kl - 1);
         typename Elem<T>::x8 kf[DP / 16];
         load_kept<DP>(kf, (const T *)v.data + (int64_t)b * v.batch + (int64_t)kvh * v.head + (int64_t)used * v.row, s.head_dim, lane);
-        keep_in_lds<DP>(lkept, wave, kf, lane);
+        if (rg == 0) keep_in_lds<DP>(lkept, kw, kf, lane);
         load_kept<DP>(kf, (const T *)k.data + (int64_t)b * k.batch + (int64_t)kvh * k.head + (int64_t)used * k.row, s.head_dim, lane);
         const int hi = row_hi(s, sp, used), lo = row_lo(s, sp, used);
         const int w_last = min(w0 + 31, sp.kl - 1), w_first = min(w0, sp.kl - 1);
@@ -170,7 +181,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_dkv(AttnShape s, Rows 
         const auto issue = [&](int to) {
             tq.issue(lq[to], gq, next, sp.ql - 1, wave);
             tg.issue(lg[to], gg, next, sp.ql - 1, wave);
-            if (wave < 2) load_floats(lst[to][wave], gs + wave * to_delta, next, sp.ql - 1, lane);
+            if (wave < 2 * PARTS) load_floats(lst[to][wave / PARTS], gs + wave / PARTS * to_delta, next, sp.ql - 1, wave % PARTS, lane);
             next += QT;
             if (next >= r1) next = r0, gq += q.head, gg += g.head, gs += s.q_len;
         };
@@ -181,43 +192,56 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_dkv(AttnShape s, Rows 
             if (n + 1 < count) issue(buf ^ 1);
             const int tile = qt;
             qt = qt + QT >= r1 ? r0 : qt + QT;
+            const int at = tile + 32 * rg;
+            if (at >= any_hi || at + 32 <= any_lo) continue;
+            f32x16 x = {}, y = {};
 #pragma unroll
-            for (int qb = 0; qb < QT / 32; ++qb) {
-                const int at = tile + 32 * qb;
-                if (at >= any_hi || at + 32 <= any_lo) continue;
-                f32x16 x = {}, y = {};
+            for (int d = 0; d < DP / 16; ++d) x = Elem<T>::mfma(rows.get(lq[buf], rg, d), kf[d], x);
 #pragma unroll
-                for (int d = 0; d < DP / 16; ++d) x = Elem<T>::mfma(rows.get(lq[buf], qb, d), kf[d], x);
+            for (int d = 0; d < DP / 16; ++d) y = Elem<T>::mfma(rows.get(lg[buf], rg, d), rows.get(lkept, kw, d), y);
+            const float *const l2 = lst[buf][0] + 32 * rg + 4 * (lane >> 5), *const delta = lst[buf][1] + 32 * rg + 4 * (lane >> 5);
+            float p[16], ds[16];
 #pragma unroll
-                for (int d = 0; d < DP / 16; ++d) y = Elem<T>::mfma(rows.get(lg[buf], qb, d), rows.get(lkept, wave, d), y);
-                const float *const l2 = lst[buf][0] + 32 * qb + 4 * (lane >> 5), *const delta = lst[buf][1] + 32 * qb + 4 * (lane >> 5);
-                float p[16], ds[16];
+            for (int i = 0; i < 16; ++i) {
+                p[i] = exp2_fast(__builtin_fmaf(x[i], c, -l2[8 * (i / 4) + i % 4]));
+                ds[i] = p[i] * (y[i] - delta[8 * (i / 4) + i % 4]);
+            }
+            if (at + 32 > all_hi || at < all_lo) {
+                const int row0 = at + 4 * (lane >> 5);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    p[i] = exp2_fast(__builtin_fmaf(x[i], c, -l2[8 * (i / 4) + i % 4]));
-                    ds[i] = p[i] * (y[i] - delta[8 * (i / 4) + i % 4]);
+                    const int row = row0 + 8 * (i / 4) + i % 4;
+                    const bool in = row < hi && row >= lo;
+                    p[i] = in ? p[i] : 0.f;
+                    ds[i] = in ? ds[i] : 0.f;
                 }
-                if (at + 32 > all_hi || at < all_lo) {
-                    const int row0 = at + 4 * (lane >> 5);
+            }
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int row = row0 + 8 * (i / 4) + i % 4;
-                        const bool in = row < hi && row >= lo;
-                        p[i] = in ? p[i] : 0.f;
-                        ds[i] = in ? ds[i] : 0.f;
-                    }
-                }
+            for (int t = 0; t < 2; ++t) {
+                const auto pf = round8<T>(p, 8 * t), df = round8<T>(ds, 8 * t);
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const auto pf = round8<T>(p, 8 * t), df = round8<T>(ds, 8 * t);
-#pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) {
-                        av[d] = Elem<T>::mfma(cols.get(lg[buf], 2 * qb + t, d), pf, av[d]);
-                        ak[d] = Elem<T>::mfma(cols.get(lq[buf], 2 * qb + t, d), df, ak[d]);
-                    }
+                for (int d = 0; d < DP / 32; ++d) {
+                    av[d] = Elem<T>::mfma(cols.get(lg[buf], 2 * rg + t, d), pf, av[d]);
+                    ak[d] = Elem<T>::mfma(cols.get(lq[buf], 2 * rg + t, d), df, ak[d]);
                 }
             }
         }
+    }
+    if constexpr (RG > 1) {
+        static_assert((RG - 1) * KW * DP / 2 * 64 * sizeof(float) <= sizeof(tiles_qg), "the sums fit where the tiles were");
+        float *const box = (float *)tiles_qg + kw * (DP / 2 * 64);
+        __syncthreads();
+        if (rg > 0) put_sums(box + (rg - 1) * KW * (DP / 2 * 64), ak, lane);
+        __syncthreads();
+        if (rg == 0)
+#pragma unroll
+            for (int n = 1; n < RG; ++n) add_sums(box + (n - 1) * KW * (DP / 2 * 64), ak, 1.f, lane);
+        __syncthreads();
+        if (rg > 0) put_sums(box + (rg - 1) * KW * (DP / 2 * 64), av, lane);
+        __syncthreads();
+        if (rg > 0) return;
+#pragma unroll
+        for (int n = 1; n < RG; ++n) add_sums(box + (n - 1) * KW * (DP / 2 * 64), av, 1.f, lane);
     }
     if (key < (int)s.k_len) {
         if (key >= sp.kl)
@@ -228,20 +252,32 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_dkv(AttnShape s, Rows 
     }
 }
 
+template <class T, int DP, int QW, int KG, int KT> hipError_t launch_dq(const AttnShape &s, const AttnGrad &a, hipStream_t st)
+{
+    const uint32_t tiles = (s.q_len + 32 * QW - 1) / (32 * QW);
+    const uint32_t total = padded_caches(s.batch * s.kv_heads) * (s.q_heads / s.kv_heads) * tiles;
+    k_attention_dq<T, DP, QW, KG, KT><<<total, QW * KG * 64, 0, st>>>(s, a.g, a.q, a.k, a.v, a.out, a.lse, a.dq, a.stats, tiles);
+    return hipGetLastError();
+}
+template <class T, int DP, int KW, int RG> hipError_t launch_dkv(const AttnShape &s, const AttnGrad &a, hipStream_t st)
+{
+    const uint32_t tiles = (s.k_len + 32 * KW - 1) / (32 * KW), total = padded_caches(s.batch * s.kv_heads) * tiles;
+    k_attention_dkv<T, DP, KW, RG><<<total, KW * RG * 64, 0, st>>>(s, a.g, a.q, a.k, a.v, a.stats, a.dk, a.dv, tiles);
+    return hipGetLastError();
+}
+
 template <class T, int DP>
 hipError_t launch(const AttnShape &s, const AttnGrad &a, hipStream_t st)
 {
-    constexpr int NW = 4;
-    const uint32_t caches = padded_caches(s.batch * s.kv_heads);
-    const uint32_t qtiles = (s.q_len + 32 * NW - 1) / (32 * NW), qtotal = caches * (s.q_heads / s.kv_heads) * qtiles;
-    const uint32_t ktiles = (s.k_len + 32 * NW - 1) / (32 * NW), ktotal = caches * ktiles;
-    if (qtotal) {
-        k_attention_dq<T, DP, NW><<<qtotal, NW * 64, 0, st>>>(s, a.g, a.q, a.k, a.v, a.out, a.lse, a.dq, a.stats, qtiles);
-        const hipError_t e = hipGetLastError();
+    if (s.q_len) {
+        const Share share = share_of((uint64_t)s.batch * s.q_heads * ((s.q_len + 127) / 128));
+        const hipError_t e = share == Share::FOUR ? launch_dq<T, DP, 4, 1, 64>(s, a, st) : share == Share::FOUR_BY_TWO ? launch_dq<T, DP, 4, 2, 64>(s, a, st)
+                                                                                                                         : launch_dq<T, DP, 2, 4, 128>(s, a, st);
         if (e != hipSuccess) return e;
     }
-    if (ktotal) k_attention_dkv<T, DP, NW><<<ktotal, NW * 64, 0, st>>>(s, a.g, a.q, a.k, a.v, a.stats, a.dk, a.dv, ktiles);
-    return hipGetLastError();
+    if (!s.k_len) return hipSuccess;
+    const Share share = share_of((uint64_t)s.batch * s.kv_heads * ((s.k_len + 127) / 128));
+    return share == Share::FOUR ? launch_dkv<T, DP, 4, 1>(s, a, st) : share == Share::FOUR_BY_TWO ? launch_dkv<T, DP, 4, 2>(s, a, st) : launch_dkv<T, DP, 2, 4>(s, a, st);
 }
 
 }  // namespace

@@ -55,7 +55,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_weights(AttnShape s, R
         int next = r0 + n0 % per * QT;      // rows of the next tile to ask for
         const auto issue = [&](int to) {
             tq.issue(lq[to], gq, next, sp.ql - 1, wave);
-            if (wave == 0) load_floats(lst[to], gs, next, sp.ql - 1, lane);
+            if (wave == 0) load_floats(lst[to], gs, next, sp.ql - 1, 0, lane);
             next += QT;
             if (next >= r1) next = r0, gq += q.head, gs += s.q_len;
         };

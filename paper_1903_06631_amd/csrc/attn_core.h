@@ -109,12 +109,13 @@ template <int DP, int ROWS, int NW> struct TileLoad {
     }
 };
 
-// 64 floats from g + first on into LDS, by one wave; those past index `last` are copies of that one
-__device__ __forceinline__ void load_floats(float *lds, const float *g, int first, int last, int lane)
+// Floats from g + first on into LDS, 64 of them by one wave, the part-th 64 of a tile; those past index `last` are copies of
+// that one (first <= last)
+__device__ __forceinline__ void load_floats(float *lds, const float *g, int first, int last, int part, int lane)
 {
     const char *base = (const char *)(g + first);
-    const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(ATTN_LDS void *)lds);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(4u * (uint32_t)min(lane, last - first)), "s"(base) : "memory");
+    const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(ATTN_LDS void *)(lds + 64 * part));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(4u * (uint32_t)min(64 * part + lane, last - first)), "s"(base) : "memory");
 }
 
 // what has been asked for has arrived in LDS, for every wave, and every wave is done with what it has read there
@@ -193,6 +194,22 @@ __device__ __forceinline__ void keep_in_lds(T *tile, int block, const typename E
         *(typename Elem<T>::x8 *)(tile + Tile<DP>::size(32) * block + Tile<DP>::place(lane & 31, 2 * k + (lane >> 5))) = f[k];
 }
 
+// A wave's sums through LDS to the wave that adds them up: N times 16 numbers of each lane, lanes side by side
+template <int N> __device__ __forceinline__ void put_sums(float *box, const f32x16 (&c)[N], int lane)
+{
+#pragma unroll
+    for (int d = 0; d < N; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) box[(16 * d + i) * 64 + lane] = c[d][i];
+}
+template <int N> __device__ __forceinline__ void add_sums(const float *box, f32x16 (&c)[N], float times, int lane)
+{
+#pragma unroll
+    for (int d = 0; d < N; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) c[d][i] = __builtin_fmaf(box[(16 * d + i) * 64 + lane], times, c[d][i]);
+}
+
 // eight values of C, from element `first` on, rounded to the nearest: B of the next product
 template <class T, int N>
 __device__ __forceinline__ typename Elem<T>::x8 round8(const float (&x)[N], int first)
@@ -218,6 +235,15 @@ __device__ __forceinline__ void store_kept(T *row, const f32x16 (&c)[DP / 32], f
             if (e < head_dim) *(typename Elem<T>::x4 *)(row + e) = x;
         }
 }
+
+// How the waves of a workgroup share its work out, by the number of its blocks of 128 kept rows: few leave units empty, so
+// more waves take part in each.  Times in us, one sequence of 2048 tokens x 128, causal, forward and backward:
+//   heads (16 blocks each)                       2         12        20        32        48        64
+//   4 blocks of 32 rows, a wave each          41  137    42  139   44  145   50  161   64  196   82  260
+//   4 blocks of 32 rows, two waves each       35  106    35  108   38  114   48  149   76  231   99  301
+//   2 blocks of 32 rows, four waves each      25   70    29   84   48  138   67  196  102  296  138  400
+enum class Share { FOUR, FOUR_BY_TWO, TWO_BY_FOUR };
+inline Share share_of(uint64_t blocks) { return blocks > 512 ? Share::FOUR : blocks > 256 ? Share::FOUR_BY_TWO : Share::TWO_BY_FOUR; }
 
 // ---- who sees whom ------------------------------------------------------------------------------------------------
 

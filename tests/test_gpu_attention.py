@@ -68,6 +68,11 @@ CASES = [
     (HF, 96, 2, 2, 0, 50, False, 0, None, None, "bhnd"),
     (BF, 64, 2, 2, 50, 0, True, 0, None, None, "bhnd"),
     (HF, 128, 5, 5, 513, 640, True, 0, None, None, "bhnd"),
+    # as many blocks of rows or keys as take another sharing of the waves, and fewer key heads than those by far
+    (BF, 128, 66, 33, 130, 140, True, 0, [130, 0, 77, 64], [140, 140, 5, 129], "bhnd"),
+    (HF, 64, 140, 70, 150, 170, True, 40, [150, 128, 1, 97], [170, 128, 64, 33], "bnhd"),
+    (BF, 72, 132, 132, 129, 70, True, 0, [129, 128, 65, 2], [70, 64, 33, 70], "bhnd"),
+    (BF, 64, 8, 1, 1100, 1300, True, 0, None, None, "bhnd"),          # the weights' rows in parts
 ]
 
 
