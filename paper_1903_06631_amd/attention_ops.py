@@ -32,7 +32,14 @@ class _Cache(C.Structure):
                 ("head_dim", C.c_uint32), ("k", _Rows), ("v", _Rows), ("weights", C.c_void_p), ("positions", C.c_void_p)]
 
 
+torch = None      # set when the library is loaded, which loads torch first
+
+
 def declare(lib) -> None:
+    global torch, _stream
+    import torch
+    # the handle alone, where torch has a call for it: a stream object takes 2 us to make
+    _stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
     p, rows, shape, cache = C.c_void_p, C.POINTER(_Rows), C.POINTER(_Shape), C.POINTER(_Cache)
     ws = [p, C.c_size_t, p]
     lib.lap_attention_workspace_bytes.restype = C.c_size_t
@@ -53,11 +60,11 @@ def _lib():
     return binding._lib or binding.load_library()
 
 
-def _done(rc: int, where: str, device, sync: bool) -> None:
+def _done(rc: int, where: str, index: int, sync: bool) -> None:
     if rc:
         raise binding.LapError(rc, where)
     if sync:
-        binding._torch().cuda.current_stream(device).synchronize()
+        torch.cuda.current_stream(index).synchronize()
 
 
 # A call's arguments are looked at on every call, of a few microseconds each: the texts of refusals are put together only
@@ -86,7 +93,7 @@ def _plain(x, name: str, dtype, shape, index: int):
     return x.data_ptr()
 
 
-def _type(torch, x, name: str) -> int:
+def _type(x, name: str) -> int:
     if x.dtype is torch.bfloat16:
         kind = 0
     elif x.dtype is torch.float16:
@@ -108,10 +115,10 @@ def _scale(scale: Optional[float], d: int) -> float:
     return float(scale) if scale is not None else d ** -0.5 if d else 0.0
 
 
-def _shape(torch, q, k, causal, window, scale, q_lens, k_lens):
+def _shape(q, k, causal, window, scale, q_lens, k_lens):
     b, h, n, d = _four(q, "q")
     _four(k, "k")
-    kind, index = _type(torch, q, "q"), q.get_device()
+    kind, index = _type(q, "q"), q.get_device()
     if window < 0:
         raise ValueError("window is 0 (none) or a number of keys")
     i32 = torch.int32
@@ -120,34 +127,31 @@ def _shape(torch, q, k, causal, window, scale, q_lens, k_lens):
                   None if k_lens is None else _plain(k_lens, "k_lens", i32, (b,), index))
 
 
-def _workspace(torch, ws, need: int, device):
+def _workspace(ws, need: int, index: int):
     """The workspace, its size and its address."""
     if ws is None:
         if not need:
             return None, 0, None
-        ws = torch.empty(need, dtype=torch.uint8, device=device)
-    elif ws.dtype is not torch.uint8 or ws.device != device or not ws.is_contiguous():
-        _refuse("ws", ws, f"a contiguous torch.uint8 on {device}")
+        ws = torch.empty(need, dtype=torch.uint8, device=index)
+    elif ws.dtype is not torch.uint8 or ws.get_device() != index or not ws.is_contiguous():
+        _refuse("ws", ws, f"a contiguous torch.uint8 on GPU {index}")
     return ws, ws.numel(), ws.data_ptr()
-
-
-def _stream(torch, device) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
 
 
 def attention(q, k, v, *, causal: bool = False, window: int = 0, scale: Optional[float] = None, q_lens=None, k_lens=None,
               out: Optional[dict] = None, ws=None, sync: bool = True):
     """lap_attention: returns dict(out like q, lse [batch, q_heads, q_len]).  scale None: 1 / sqrt(head_dim)."""
-    lib, torch = _lib(), binding._torch()
-    s = _shape(torch, q, k, causal, window, scale, q_lens, k_lens)
+    lib = _lib()
+    s, index = _shape(q, k, causal, window, scale, q_lens, k_lens), q.get_device()
     kv = (s.batch, s.kv_heads, s.k_len, s.head_dim)
     if out is None:
-        out = dict(out=torch.empty_like(q), lse=torch.empty(q.shape[:3], dtype=torch.float32, device=q.device))
-    ws, have, at = _workspace(torch, ws, lib.lap_attention_workspace_bytes(AT_FORWARD, s), q.device)
+        out = dict(out=torch.empty_like(q), lse=torch.empty(q.shape[:3], dtype=torch.float32, device=index))
+    ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_FORWARD, s), index)
     rc = lib.lap_attention(s, _rows(q, "q", q, q.shape), _rows(k, "k", q, kv), _rows(v, "v", q, kv),
-                           _rows(out["out"], "out", q, q.shape), _plain(out["lse"], "lse", torch.float32, q.shape[:3], q.get_device()),
-                           at, have, _stream(torch, q.device))
-    _done(rc, "lap_attention", q.device, sync)
+                           _rows(out["out"], "out", q, q.shape), _plain(out["lse"], "lse", torch.float32, q.shape[:3], index),
+                           at, have, _stream(index))
+    if rc or sync:
+        _done(rc, "lap_attention", index, sync)
     return out
 
 
@@ -155,34 +159,36 @@ def attention_grad(dout, q, k, v, out, lse, *, causal: bool = False, window: int
                    k_lens=None, grads: Optional[dict] = None, ws=None, sync: bool = True):
     """lap_attention_grad: returns dict(dq, dk, dv); out and lse are attention's, the other arguments as there.  grads takes
     result tensors that the caller owns."""
-    lib, torch = _lib(), binding._torch()
-    s = _shape(torch, q, k, causal, window, scale, q_lens, k_lens)
+    lib = _lib()
+    s, index = _shape(q, k, causal, window, scale, q_lens, k_lens), q.get_device()
     kv = (s.batch, s.kv_heads, s.k_len, s.head_dim)
     if grads is None:
-        grads = dict(dq=torch.empty_like(q), dk=torch.empty(kv, dtype=q.dtype, device=q.device),
-                     dv=torch.empty(kv, dtype=q.dtype, device=q.device))
-    ws, have, at = _workspace(torch, ws, lib.lap_attention_workspace_bytes(AT_GRAD, s), q.device)
+        grads = dict(dq=torch.empty_like(q), dk=torch.empty(kv, dtype=q.dtype, device=index),
+                     dv=torch.empty(kv, dtype=q.dtype, device=index))
+    ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_GRAD, s), index)
     rc = lib.lap_attention_grad(s, _rows(dout, "dout", q, q.shape), _rows(q, "q", q, q.shape), _rows(k, "k", q, kv), _rows(v, "v", q, kv),
-                                _rows(out, "out", q, q.shape), _plain(lse, "lse", torch.float32, q.shape[:3], q.get_device()),
+                                _rows(out, "out", q, q.shape), _plain(lse, "lse", torch.float32, q.shape[:3], index),
                                 _rows(grads["dq"], "dq", q, q.shape), _rows(grads["dk"], "dk", q, kv), _rows(grads["dv"], "dv", q, kv),
-                                at, have, _stream(torch, q.device))
-    _done(rc, "lap_attention_grad", q.device, sync)
+                                at, have, _stream(index))
+    if rc or sync:
+        _done(rc, "lap_attention_grad", index, sync)
     return grads
 
 
 def attention_weights(q, k, lse, *, before=None, causal: bool = False, window: int = 0, scale: Optional[float] = None, q_lens=None,
                       k_lens=None, weights=None, ws=None, sync: bool = True):
     """lap_attention_weights: returns dict(weights [batch, kv_heads, k_len]) = before (None: zeros) + what the keys receive."""
-    lib, torch = _lib(), binding._torch()
-    s = _shape(torch, q, k, causal, window, scale, q_lens, k_lens)
+    lib = _lib()
+    s, index = _shape(q, k, causal, window, scale, q_lens, k_lens), q.get_device()
     kv = (s.batch, s.kv_heads, s.k_len)
     if weights is None:
-        weights = torch.empty(kv, dtype=torch.float32, device=q.device)
-    ws, have, at = _workspace(torch, ws, lib.lap_attention_workspace_bytes(AT_WEIGHTS, s), q.device)
+        weights = torch.empty(kv, dtype=torch.float32, device=index)
+    ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_WEIGHTS, s), index)
     rc = lib.lap_attention_weights(s, _rows(q, "q", q, q.shape), _rows(k, "k", q, kv + (s.head_dim,)),
-                                   _plain(lse, "lse", torch.float32, q.shape[:3], q.get_device()), _plain(before, "before", torch.float32, kv, q.get_device()),
-                                   _plain(weights, "weights", torch.float32, kv, q.get_device()), at, have, _stream(torch, q.device))
-    _done(rc, "lap_attention_weights", q.device, sync)
+                                   _plain(lse, "lse", torch.float32, q.shape[:3], index), _plain(before, "before", torch.float32, kv, index),
+                                   _plain(weights, "weights", torch.float32, kv, index), at, have, _stream(index))
+    if rc or sync:
+        _done(rc, "lap_attention_weights", index, sync)
     return dict(weights=weights)
 
 
@@ -191,30 +197,31 @@ def attention_step(q, k_cache, v_cache, weights=None, *, lens=None, positions=No
     """lap_attention_step: q [batch, q_heads, head_dim] of one token against caches [batch, kv_heads, slots, head_dim].  Returns
     dict(out like q, lse [batch, q_heads], weights = the given ones + this token's, a new tensor unless out holds one; None
     where none are given)."""
-    lib, torch = _lib(), binding._torch()
+    lib = _lib()
     if q.dim() != 3:
         _refuse("q", q, "[batch, heads, head_dim]")
     b, h, d = q.shape
     _four(k_cache, "k_cache")
-    dev, index = q.device, q.get_device()
+    index = q.get_device()
     slots = (b, k_cache.shape[1], k_cache.shape[2])
-    s = _Shape(_type(torch, q, "q"), b, h, slots[1], 1, slots[2], d, 0, 0, _scale(scale, d), None,
+    s = _Shape(_type(q, "q"), b, h, slots[1], 1, slots[2], d, 0, 0, _scale(scale, d), None,
                _plain(lens, "lens", torch.int32, (b,), index))
     if out is None:
-        out = dict(out=torch.empty_like(q), lse=torch.empty((b, h), dtype=torch.float32, device=dev),
-                   weights=None if weights is None else torch.empty(slots, dtype=torch.float32, device=dev))
-    ws, have, at = _workspace(torch, ws, lib.lap_attention_workspace_bytes(AT_STEP, s), dev)
+        out = dict(out=torch.empty_like(q), lse=torch.empty((b, h), dtype=torch.float32, device=index),
+                   weights=None if weights is None else torch.empty(slots, dtype=torch.float32, device=index))
+    ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_STEP, s), index)
     rc = lib.lap_attention_step(s, _rows(q, "q", q, q.shape), _rows(k_cache, "k_cache", q, slots + (d,)), _rows(v_cache, "v_cache", q, slots + (d,)),
                                 _plain(positions, "positions", torch.int32, slots, index), _plain(weights, "weights", torch.float32, slots, index),
                                 _rows(out["out"], "out", q, q.shape), _plain(out["lse"], "lse", torch.float32, (b, h), index),
-                                _plain(out.get("weights"), "out weights", torch.float32, slots, index), at, have, _stream(torch, dev))
-    _done(rc, "lap_attention_step", dev, sync)
+                                _plain(out.get("weights"), "out weights", torch.float32, slots, index), at, have, _stream(index))
+    if rc or sync:
+        _done(rc, "lap_attention_step", index, sync)
     return out
 
 
-def _cache(torch, k, v, weights, positions, name: str = ""):
+def _cache(k, v, weights, positions, name: str = ""):
     b, h, n, d = _four(k, name + "k")
-    kind, index = _type(torch, k, name + "k"), k.get_device()
+    kind, index = _type(k, name + "k"), k.get_device()
     return _Cache(kind, b, h, n, d, _rows(k, name + "k", k, k.shape), _rows(v, name + "v", k, k.shape),
                   _plain(weights, name + "weights", torch.float32, (b, h, n), index),
                   _plain(positions, name + "positions", torch.int32, (b, h, n), index))
@@ -224,40 +231,42 @@ def cache_evict(k, v, weights, keep: int, recent: int, *, lens=None, positions=N
                 out: Optional[dict] = None, ws=None, sync: bool = True):
     """lap_cache_evict: the `keep` rows of highest weight of k and v, the newest `recent` among them, into a cache of `slots`
     (None: keep).  Returns dict(k, v, weights, positions [batch, kv_heads, slots], lens [batch])."""
-    lib, torch = _lib(), binding._torch()
-    src = _cache(torch, k, v, weights, positions)
+    lib = _lib()
+    src = _cache(k, v, weights, positions)
     if keep < 0 or recent < 0:
         raise ValueError("keep and recent are numbers of slots")
     b, h, n, d = k.shape
-    dev, index = k.device, k.get_device()
+    index = k.get_device()
     if out is None:
         m = int(keep if slots is None else slots)
-        out = dict(k=torch.empty((b, h, m, d), dtype=k.dtype, device=dev), v=torch.empty((b, h, m, d), dtype=k.dtype, device=dev),
-                   weights=torch.empty((b, h, m), dtype=torch.float32, device=dev),
-                   positions=torch.empty((b, h, m), dtype=torch.int32, device=dev), lens=torch.empty(b, dtype=torch.int32, device=dev))
+        out = dict(k=torch.empty((b, h, m, d), dtype=k.dtype, device=index), v=torch.empty((b, h, m, d), dtype=k.dtype, device=index),
+                   weights=torch.empty((b, h, m), dtype=torch.float32, device=index),
+                   positions=torch.empty((b, h, m), dtype=torch.int32, device=index), lens=torch.empty(b, dtype=torch.int32, device=index))
     if out["k"].dtype is not k.dtype or out["k"].get_device() != index:
-        _refuse("out k", out["k"], f"{k.dtype} on {dev}")
-    dst = _cache(torch, out["k"], out["v"], out["weights"], out["positions"], "out ")
-    ws, have, at = _workspace(torch, ws, lib.lap_cache_workspace_bytes(dst), dev)
+        _refuse("out k", out["k"], f"{k.dtype} on GPU {index}")
+    dst = _cache(out["k"], out["v"], out["weights"], out["positions"], "out ")
+    ws, have, at = _workspace(ws, lib.lap_cache_workspace_bytes(dst), index)
     rc = lib.lap_cache_evict(src, _plain(lens, "lens", torch.int32, (b,), index), int(keep), int(recent), dst,
-                             _plain(out["lens"], "out lens", torch.int32, (b,), index), at, have, _stream(torch, dev))
-    _done(rc, "lap_cache_evict", dev, sync)
+                             _plain(out["lens"], "out lens", torch.int32, (b,), index), at, have, _stream(index))
+    if rc or sync:
+        _done(rc, "lap_cache_evict", index, sync)
     return out
 
 
 def cache_insert(k_new, v_new, k_cache, v_cache, weights, positions, position, recent: int, *, slots=None, sync: bool = True):
     """lap_cache_insert: one token [batch, kv_heads, head_dim] into every cache, in place; position [batch] is the token's.
     Returns dict(slots [batch, kv_heads]): where it went."""
-    lib, torch = _lib(), binding._torch()
-    cache = _cache(torch, k_cache, v_cache, weights, positions)
+    lib = _lib()
+    cache = _cache(k_cache, v_cache, weights, positions)
     if recent < 0:
         raise ValueError("recent is a number of slots")
     b, h, _, d = k_cache.shape
-    dev, index = k_cache.device, k_cache.get_device()
+    index = k_cache.get_device()
     if slots is None:
-        slots = torch.empty((b, h), dtype=torch.int32, device=dev)
+        slots = torch.empty((b, h), dtype=torch.int32, device=index)
     rc = lib.lap_cache_insert(cache, _rows(k_new, "k_new", k_cache, (b, h, d)), _rows(v_new, "v_new", k_cache, (b, h, d)),
                               _plain(position, "position", torch.int32, (b,), index), int(recent),
-                              _plain(slots, "slots", torch.int32, (b, h), index), _stream(torch, dev))
-    _done(rc, "lap_cache_insert", dev, sync)
+                              _plain(slots, "slots", torch.int32, (b, h), index), _stream(index))
+    if rc or sync:
+        _done(rc, "lap_cache_insert", index, sync)
     return dict(slots=slots)

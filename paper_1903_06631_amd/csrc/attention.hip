@@ -2,7 +2,9 @@
 // of the sum of exp(scale q_i.k_j) over the keys that row i sees.
 //
 // One pass over the keys with a running maximum m and sum l for every row: a tile of keys gives s = K Q^T, p = 2^(c s - c m)
-// with c = scale log2(e), l += sum p, O^T += V^T P^T.  Nothing of the size queries x keys is ever stored.
+// with c = scale log2(e), l += sum p, O^T += V^T P^T.  Nothing of the size queries x keys is ever stored.  Where there are few
+// rows and many keys, the keys are cut into parts, a workgroup each, which leave m, l and O in the workspace for a second
+// kernel to join.
 #include "attn_core.h"
 
 namespace lap {
@@ -11,15 +13,16 @@ namespace {
 // QW blocks of 32 rows; their keys are dealt to KG waves each, NB blocks of 32 keys at a time.  Where rows are few, waves that
 // share them fill the units that would have none; they join their sums at the end.
 template <class T, int DP, int QW, int KG, int NB>
-__global__ __launch_bounds__(QW * KG * 64, 2) void k_attention(AttnShape s, Rows q, Rows k, Rows v, Rows o, float *lse, uint32_t tiles)
+__global__ __launch_bounds__(QW * KG * 64, 2) void k_attention(AttnShape s, Rows q, Rows k, Rows v, Rows o, float *lse, uint32_t tiles,
+                                                                     uint32_t parts, float *outs, float2 *out_sums)
 {
     constexpr int NW = QW * KG, BQ = 32 * QW, KT = 32 * KG * NB;
     __shared__ __align__(16) T tiles_kv[4][Tile<DP>::size(KT)];
     T(*const lk)[Tile<DP>::size(KT)] = tiles_kv, (*const lv)[Tile<DP>::size(KT)] = tiles_kv + 2;
     const uint32_t group = s.q_heads / s.kv_heads;
     Work wk;
-    if (!work_item(s, group, wk)) return;
-    const uint32_t b = wk.b, h = wk.kvh * group + wk.g;
+    if (!work_item(s, group * parts, wk)) return;
+    const uint32_t b = wk.b, h = wk.kvh * group + wk.g % group, part = wk.g / group;
     const int first = (int)(tiles - 1 - wk.tile) * BQ;      // the longest rows of a causal head first
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Span sp = span_of(s, b);
@@ -33,8 +36,13 @@ __global__ __launch_bounds__(QW * KG * 64, 2) void k_attention(AttnShape s, Rows
     f32x16 acc[DP / 32] = {};
     float m = LOWEST, l = 0.f;
     const int end = min(first + BQ, sp.ql);         // rows in use
-    const int k0 = first < sp.ql ? key_lo(s, sp, first) / KT * KT : 0;
-    const int k1 = first < sp.ql ? key_hi(s, sp, end - 1) : 0;
+    int k0 = first < sp.ql ? key_lo(s, sp, first) / KT * KT : 0;
+    int k1 = first < sp.ql ? key_hi(s, sp, end - 1) : 0;
+    if (parts > 1 && k0 < k1) {      // this part's share of the tiles
+        const int64_t n = (k1 - k0 + KT - 1) / KT;
+        k1 = min(k1, k0 + (int)(n * (part + 1) / parts) * KT);
+        k0 += (int)(n * part / parts) * KT;
+    }
     if (k0 < k1) {
         const int used = min(row, sp.ql - 1);       // padding takes the last row's part and is thrown away
         const int last_chunk = (int)s.head_dim / 8 - 1, last = sp.kl - 1;
@@ -138,6 +146,17 @@ __global__ __launch_bounds__(QW * KG * 64, 2) void k_attention(AttnShape s, Rows
             m = up;
         }
     }
+    if (parts > 1) {
+        if (row >= sp.ql) return;
+        const int64_t at = (((int64_t)b * s.q_heads + h) * s.q_len + row) * parts + part;
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *(f32x4 *)(outs + at * DP + 32 * d + 2 * i + 4 * (lane >> 5)) = f32x4{acc[d][i], acc[d][i + 1], acc[d][i + 2], acc[d][i + 3]};
+        if (lane < 32) out_sums[at] = make_float2(m, l);
+        return;
+    }
     if (row < (int)s.q_len) {
         const bool some = row < sp.ql && l != 0.f;      // (a sum that is not a number is some)
         if (!some)
@@ -148,32 +167,86 @@ __global__ __launch_bounds__(QW * KG * 64, 2) void k_attention(AttnShape s, Rows
     }
 }
 
-template <class T, int DP, int QW, int KG, int NB>
-hipError_t launch_as(const AttnShape &s, const Rows &q, const Rows &k, const Rows &v, const Rows &out, float *lse, hipStream_t st)
+// A wave joins the parts of a row.
+template <class T, int DP>
+__global__ __launch_bounds__(256) void k_attention_join(AttnShape s, Rows o, float *lse, uint32_t parts, const float *outs, const float2 *sums)
 {
-    const uint32_t tiles = (s.q_len + 32 * QW - 1) / (32 * QW);
-    const uint32_t total = padded_caches(s.batch * s.kv_heads) * (s.q_heads / s.kv_heads) * tiles;
-    k_attention<T, DP, QW, KG, NB><<<total, QW * KG * 64, 0, st>>>(s, q, k, v, out, lse, tiles);
+    const int lane = threadIdx.x & 63;
+    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (at >= (int64_t)s.batch * s.q_heads * s.q_len) return;
+    const uint32_t row = (uint32_t)(at % s.q_len), h = (uint32_t)(at / s.q_len % s.q_heads), b = (uint32_t)(at / s.q_len / s.q_heads);
+    constexpr int N = DP / 64;      // elements of a lane
+    const float c = s.scale * LOG2E;
+    float m = LOWEST, l = 0.f, y[N] = {};
+    if ((int)row < span_of(s, b).ql) {
+        for (uint32_t i = 0; i < parts; ++i) m = fmaxf(m, sums[at * parts + i].x);
+#pragma unroll 4
+        for (uint32_t i = 0; i < parts; ++i) {
+            const float2 x = sums[at * parts + i];
+            const float by = exp2_fast((x.x - m) * c);
+            l += x.y * by;
+#pragma unroll
+            for (int j = 0; j < N; ++j) y[j] += outs[(at * parts + i) * DP + lane * N + j] * by;
+        }
+    }
+    const bool some = l != 0.f;
+    T *to = (T *)o.data + (int64_t)b * o.batch + (int64_t)h * o.head + (int64_t)row * o.row + lane * N;
+    typedef T TN __attribute__((ext_vector_type(N)));
+    TN z;
+#pragma unroll
+    for (int j = 0; j < N; ++j) z[j] = (T)(some ? y[j] / l : 0.f);
+    if (lane * N < (int)s.head_dim) *(TN *)to = z;
+    if (lane == 0) lse[at] = some ? m * s.scale + __logf(l) : -ATTN_INF;
+}
+
+template <class T, int DP, int QW, int KG, int NB>
+hipError_t launch_as(const AttnShape &s, const Rows &q, const Rows &k, const Rows &v, const Rows &out, float *lse, void *ws, hipStream_t st)
+{
+    const uint32_t tiles = (s.q_len + 32 * QW - 1) / (32 * QW), parts = forward_parts(s);
+    const uint32_t total = padded_caches(s.batch * s.kv_heads) * (s.q_heads / s.kv_heads) * tiles * parts;
+    const uint64_t rows = (uint64_t)s.batch * s.q_heads * s.q_len;
+    float *outs = (float *)ws;
+    float2 *sums = (float2 *)(outs + rows * parts * DP);
+    k_attention<T, DP, QW, KG, NB><<<total, QW * KG * 64, 0, st>>>(s, q, k, v, out, lse, tiles, parts, outs, sums);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || parts == 1) return e;
+    k_attention_join<T, DP><<<(uint32_t)((rows + 3) / 4), 256, 0, st>>>(s, out, lse, parts, outs, sums);
     return hipGetLastError();
 }
 
 template <class T, int DP>
-hipError_t launch(const AttnShape &s, const Rows &q, const Rows &k, const Rows &v, const Rows &out, float *lse, hipStream_t st)
+hipError_t launch(const AttnShape &s, const Rows &q, const Rows &k, const Rows &v, const Rows &out, float *lse, void *ws, hipStream_t st)
 {
     switch (share_of((uint64_t)s.batch * s.q_heads * ((s.q_len + 127) / 128))) {
-    case Share::FOUR: return launch_as<T, DP, 4, 1, 2>(s, q, k, v, out, lse, st);
-    case Share::FOUR_BY_TWO: return launch_as<T, DP, 4, 2, 2>(s, q, k, v, out, lse, st);
-    default: return launch_as<T, DP, 2, 4, 1>(s, q, k, v, out, lse, st);
+    case Share::FOUR: return launch_as<T, DP, 4, 1, 2>(s, q, k, v, out, lse, ws, st);
+    case Share::FOUR_BY_TWO: return launch_as<T, DP, 4, 2, 2>(s, q, k, v, out, lse, ws, st);
+    default: return launch_as<T, DP, 2, 4, 1>(s, q, k, v, out, lse, ws, st);
     }
 }
 
 }  // namespace
 
-hipError_t launch_attention(const AttnShape &s, const Rows &q, const Rows &k, const Rows &v, const Rows &out, float *lse, hipStream_t st)
+// Parts of the keys: as many as workgroups of 64 rows (the last of the sharings above) leave units for, of four tiles of 128
+// keys at least.  Of 17 rows on 12000 keys, two sequences of 16 heads, 25 us (in one part 111); 500 rows on 8000 keys 52 us
+// (77); twice as many parts, which units then take in turn, 30 and 60 us; two tiles to a part in place of four 26 us where
+// that is 19 (2 heads of 2048 rows, causal; one part 25).
+uint32_t forward_parts(const AttnShape &s)
+{
+    const uint64_t groups = (uint64_t)s.batch * s.q_heads * ((s.q_len + 63) / 64);
+    const uint64_t want = groups ? 256 / groups : 0, most = s.k_len / 512;
+    return (uint32_t)(want < 2 || most < 2 ? 1 : want > most ? most : want);
+}
+size_t forward_workspace(const AttnShape &s)
+{
+    const uint32_t parts = forward_parts(s);
+    return parts == 1 ? 0 : (size_t)s.batch * s.q_heads * s.q_len * parts * ((s.head_dim <= 64 ? 64 : 128) * sizeof(float) + sizeof(float2));
+}
+
+hipError_t launch_attention(const AttnShape &s, const Rows &q, const Rows &k, const Rows &v, const Rows &out, float *lse, void *ws, hipStream_t st)
 {
     if (s.half)
-        return s.head_dim <= 64 ? launch<_Float16, 64>(s, q, k, v, out, lse, st) : launch<_Float16, 128>(s, q, k, v, out, lse, st);
-    return s.head_dim <= 64 ? launch<__bf16, 64>(s, q, k, v, out, lse, st) : launch<__bf16, 128>(s, q, k, v, out, lse, st);
+        return s.head_dim <= 64 ? launch<_Float16, 64>(s, q, k, v, out, lse, ws, st) : launch<_Float16, 128>(s, q, k, v, out, lse, ws, st);
+    return s.head_dim <= 64 ? launch<__bf16, 64>(s, q, k, v, out, lse, ws, st) : launch<__bf16, 128>(s, q, k, v, out, lse, ws, st);
 }
 
 }  // namespace lap

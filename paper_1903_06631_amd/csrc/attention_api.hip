@@ -106,6 +106,7 @@ size_t lap_attention_workspace_bytes(int which_call, const lap_attention_shape *
 {
     if (check_shape(s)) return 0;
     switch (which_call) {
+    case LAP_AT_FORWARD: return up(lap::forward_workspace(shape_of(s)));
     case LAP_AT_GRAD: return ws_grad(s);
     case LAP_AT_WEIGHTS: return ws_weights(s);
     case LAP_AT_STEP: return ws_step(s);
@@ -128,9 +129,9 @@ int lap_attention(const lap_attention_shape *s, const lap_rows *q, const lap_row
     if (!rc) rc = check_rows(v, s->batch, s->kv_heads, s->k_len, s->head_dim, false);
     if (!rc) rc = check_rows(out, s->batch, s->q_heads, s->q_len, s->head_dim, true);
     if (!rc && s->q_len && !lse) rc = LAP_E_NULL;
-    if (!rc) rc = check_ws(ws, ws_bytes, lap_attention_workspace_bytes(LAP_AT_FORWARD, s));
+    if (!rc) rc = check_ws(ws, ws_bytes, up(lap::forward_workspace(shape_of(s))));
     if (rc || !s->q_len) return rc;
-    LAP_HIP(lap::launch_attention(shape_of(s), rows_of(q), rows_of(k), rows_of(v), rows_of(out), lse, (hipStream_t)hip_stream));
+    LAP_HIP(lap::launch_attention(shape_of(s), rows_of(q), rows_of(k), rows_of(v), rows_of(out), lse, ws, (hipStream_t)hip_stream));
     return LAP_OK;
 }
 

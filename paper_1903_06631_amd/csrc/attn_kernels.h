@@ -19,7 +19,9 @@ struct AttnShape {
     bool half;      // IEEE binary16, else bfloat16
 };
 
-hipError_t launch_attention(const AttnShape &s, const Rows &q, const Rows &k, const Rows &v, const Rows &out, float *lse, hipStream_t st);
+uint32_t forward_parts(const AttnShape &s);
+size_t forward_workspace(const AttnShape &s);
+hipError_t launch_attention(const AttnShape &s, const Rows &q, const Rows &k, const Rows &v, const Rows &out, float *lse, void *ws, hipStream_t st);
 
 struct AttnGrad {
     Rows g, q, k, v, out, dq, dk, dv;

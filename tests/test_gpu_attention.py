@@ -68,6 +68,10 @@ CASES = [
     (HF, 96, 2, 2, 0, 50, False, 0, None, None, "bhnd"),
     (BF, 64, 2, 2, 50, 0, True, 0, None, None, "bhnd"),
     (HF, 128, 5, 5, 513, 640, True, 0, None, None, "bhnd"),
+    # few rows on many keys: the keys in parts, some of them with nothing for a row
+    (BF, 128, 4, 2, 70, 2200, True, 0, [70, 0, 33], [2200, 100, 1], "bhnd"),
+    (HF, 64, 2, 1, 33, 3001, False, 0, [33, 1], [3001, 0], "gaps"),
+    (BF, 104, 2, 2, 65, 2100, True, 300, None, None, "bnhd"),
     # as many blocks of rows or keys as take another sharing of the waves, and fewer key heads than those by far
     (BF, 128, 66, 33, 130, 140, True, 0, [130, 0, 77, 64], [140, 140, 5, 129], "bhnd"),
     (HF, 64, 140, 70, 150, 170, True, 40, [150, 128, 1, 97], [170, 128, 64, 33], "bnhd"),
