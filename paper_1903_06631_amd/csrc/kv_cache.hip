@@ -233,11 +233,20 @@ __global__ __launch_bounds__(IN) void k_insert(InsertShape s, Rows k_new, Rows v
     float *w = weights + (int64_t)blockIdx.x * s.slots;
     int32_t *pos = positions + (int64_t)blockIdx.x * s.slots;
     uint64_t least = ~0ull;
-    for (uint32_t i = t; i < s.slots; i += IN) {
-        const int p = pos[i];
-        const uint64_t hi = p < 0 ? EMPTY : (int64_t)p > (int64_t)at - (int64_t)s.recent ? NEWEST : weight_key(w[i]);
-        const uint64_t x = hi << 32 | (p < 0 ? i : ~i);
-        least = x < least ? x : least;
+    for (uint32_t first = t; first < s.slots; first += 8 * IN) {      // eight at a time; past the end the last one again
+        int p[8];
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[j] = pos[min(first + j * IN, s.slots - 1)];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = w[min(first + j * IN, s.slots - 1)];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t i = min(first + j * IN, s.slots - 1);
+            const uint32_t key = p[j] < 0 ? EMPTY : (int64_t)p[j] > (int64_t)at - (int64_t)s.recent ? NEWEST : weight_key(x[j]);
+            const uint64_t y = (uint64_t)key << 32 | (p[j] < 0 ? i : ~i);
+            least = y < least ? y : least;
+        }
     }
     for (int d = 32; d; d >>= 1) {
         const uint64_t x = __shfl_xor((unsigned long long)least, d, 64);
