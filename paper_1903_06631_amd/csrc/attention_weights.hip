@@ -82,8 +82,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_weights(AttnShape s, R
                 float l2[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float l = lst[buf][32 * qb + 8 * (i / 4) + 4 * (lane >> 5) + i % 4];
-                    l2[i] = l == -ATTN_INF ? -ATTN_INF : -l * LOG2E;      // a row without keys gives nothing
+                    // minus infinity: a row without keys, or whose scores are all below what counts, far below this
+                    l2[i] = -LOG2E * fmaxf(lst[buf][32 * qb + 8 * (i / 4) + 4 * (lane >> 5) + i % 4], -1e20f);
                 }
                 const bool whole = at + 32 <= all_hi && at >= all_lo;
 #pragma unroll

@@ -55,7 +55,7 @@ __global__ __launch_bounds__(EV) void k_evict_choose(EvictShape s, const float *
 {
     __shared__ uint32_t bins[BINS];
     __shared__ uint32_t part[EW][2];
-    __shared__ uint32_t found[2];
+    __shared__ uint32_t found[3];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const uint32_t b = blockIdx.x / s.kv_heads;
     EvictRow row;
@@ -138,7 +138,7 @@ __global__ __launch_bounds__(EV) void k_evict_choose(EvictShape s, const float *
             if (before < want && want <= up) {
 #pragma unroll
                 for (int i = OWN - 1; i >= 0; --i) {
-                    if (before < want && want <= before + c[i]) found[0] = (uint32_t)(lo + i), found[1] = want - before;
+                    if (before < want && want <= before + c[i]) found[0] = (uint32_t)(lo + i), found[1] = want - before, found[2] = c[i];
                     before += c[i];
                 }
             }
@@ -146,7 +146,12 @@ __global__ __launch_bounds__(EV) void k_evict_choose(EvictShape s, const float *
             prefix |= found[0] << shift;
             mask |= ones << shift;
             want = found[1];
+            const bool all = want == found[2];      // all that begin like this: nothing left to tell apart (prefix is not 0: if the least stay, all do)
             __syncthreads();
+            if (all) {
+                prefix -= 1, want = 0;
+                break;
+            }
         }
         if (mask) bound = prefix, equal = want;
     }
