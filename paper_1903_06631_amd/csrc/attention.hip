@@ -217,7 +217,7 @@ hipError_t launch_as(const AttnShape &s, const Rows &q, const Rows &k, const Row
 template <class T, int DP>
 hipError_t launch(const AttnShape &s, const Rows &q, const Rows &k, const Rows &v, const Rows &out, float *lse, void *ws, hipStream_t st)
 {
-    switch (share_of((uint64_t)s.batch * s.q_heads * ((s.q_len + 127) / 128))) {
+    switch (share_of(s, s.q_heads, s.q_len)) {
     case Share::FOUR: return launch_as<T, DP, 4, 1, 2>(s, q, k, v, out, lse, ws, st);
     case Share::FOUR_BY_TWO: return launch_as<T, DP, 4, 2, 2>(s, q, k, v, out, lse, ws, st);
     default: return launch_as<T, DP, 2, 4, 1>(s, q, k, v, out, lse, ws, st);

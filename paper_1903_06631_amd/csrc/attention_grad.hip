@@ -270,13 +270,13 @@ template <class T, int DP>
 hipError_t launch(const AttnShape &s, const AttnGrad &a, hipStream_t st)
 {
     if (s.q_len) {
-        const Share share = share_of((uint64_t)s.batch * s.q_heads * ((s.q_len + 127) / 128));
+        const Share share = share_of(s, s.q_heads, s.q_len);
         const hipError_t e = share == Share::FOUR ? launch_dq<T, DP, 4, 1, 64>(s, a, st) : share == Share::FOUR_BY_TWO ? launch_dq<T, DP, 4, 2, 64>(s, a, st)
                                                                                                                          : launch_dq<T, DP, 2, 4, 128>(s, a, st);
         if (e != hipSuccess) return e;
     }
     if (!s.k_len) return hipSuccess;
-    const Share share = share_of((uint64_t)s.batch * s.kv_heads * ((s.k_len + 127) / 128));
+    const Share share = share_of(s, s.kv_heads, s.k_len);
     return share == Share::FOUR ? launch_dkv<T, DP, 4, 1>(s, a, st) : share == Share::FOUR_BY_TWO ? launch_dkv<T, DP, 4, 2>(s, a, st) : launch_dkv<T, DP, 2, 4>(s, a, st);
 }
 

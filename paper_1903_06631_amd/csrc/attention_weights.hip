@@ -4,6 +4,8 @@
 // A workgroup keeps keys and streams the rows of their heads; a lane adds up the probabilities of one key for each block of
 // 32 that its wave keeps.  Where that makes too few workgroups, or under a causal mask too few to share out long and short
 // ones, the rows are cut into parts, whose sums a second kernel adds in order.
+#include <algorithm>
+
 #include "attn_core.h"
 
 namespace lap {
@@ -153,15 +155,17 @@ uint32_t weights_blocks(const AttnShape &s)
 {
     return (uint64_t)s.batch * s.kv_heads * ((s.k_len + 127) / 128) * (s.q_heads / s.kv_heads) * ((s.q_len + 255) / 256) >= 512 ? 2 : 1;
 }
-// Parts of the rows: enough for 2048 workgroups (that call: 558 us, with 1024 of them 582, with 4096 561), if each has 1024
-// rows at least: an additional kernel takes 4 us.
+// Parts of the rows: enough for 2048 workgroups (2 x 32 heads x 8192 tokens: 558 us, with 1024 of them 582, with 4096 561), of
+// 512 rows each at least (16 x 16 heads on 4 x 600 tokens: 28 us, with 256 rows 33); where that leaves fewer than 512
+// workgroups, as many as that, of 256 rows at least (8 heads of 1500 tokens: 16 us, with 512 rows 26, with 1024 40).
 uint32_t weights_parts(const AttnShape &s)
 {
     const uint32_t keys = 32 * NW * weights_blocks(s);
-    const uint64_t groups = (uint64_t)s.batch * s.kv_heads * ((s.k_len + keys - 1) / keys);
-    const uint64_t most = (uint64_t)(s.q_heads / s.kv_heads) * s.q_len / 1024;
-    const uint64_t want = (2048 + groups - 1) / groups;
-    return (uint32_t)(want < 1 || most < 1 ? 1 : want > most ? most : want);
+    const uint64_t groups = (uint64_t)s.batch * s.kv_heads * ((s.k_len + keys - 1) / keys), rows = (uint64_t)(s.q_heads / s.kv_heads) * s.q_len;
+    if (!groups) return 1;
+    uint64_t parts = std::min((2048 + groups - 1) / groups, rows / 512);
+    if (groups * parts < 512) parts = std::min((512 + groups - 1) / groups, rows / 256);
+    return (uint32_t)std::max<uint64_t>(parts, 1);
 }
 
 hipError_t launch_attention_weights(const AttnShape &s, const Rows &q, const Rows &k, const float *lse, const float *before, float *weights,

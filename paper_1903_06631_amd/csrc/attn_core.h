@@ -237,13 +237,23 @@ __device__ __forceinline__ void store_kept(T *row, const f32x16 (&c)[DP / 32], f
 }
 
 // How the waves of a workgroup share its work out, by the number of its blocks of 128 kept rows: few leave units empty, so
-// more waves take part in each.  Times in us, one sequence of 2048 tokens x 128, causal, forward and backward:
-//   heads (16 blocks each)                       2         12        20        32        48        64
+// more waves take part in each.  Times in us, forward and backward, one sequence of 2048 tokens x 128 with so many heads (16
+// blocks each).  Under a causal mask, long tiles first:
+//                                                 2         12        20        32        48        64
 //   4 blocks of 32 rows, a wave each          41  137    42  139   44  145   50  161   64  196   82  260
 //   4 blocks of 32 rows, two waves each       35  106    35  108   38  114   48  149   76  231   99  301
 //   2 blocks of 32 rows, four waves each      25   70    29   84   48  138   67  196  102  296  138  400
+// Without, equal tiles, which units take in whole rounds:
+//                                                 6          9        15        20        32
+//   4 blocks of 32 rows, a wave each          42  139    43  141   44  145   62  188   75  232
+//   4 blocks of 32 rows, two waves each       35  107    36  109   41  125   72  227   81  252
+//   2 blocks of 32 rows, four waves each      25   72    51  145   55  161   78  227  105  310
 enum class Share { FOUR, FOUR_BY_TWO, TWO_BY_FOUR };
-inline Share share_of(uint64_t blocks) { return blocks > 512 ? Share::FOUR : blocks > 256 ? Share::FOUR_BY_TWO : Share::TWO_BY_FOUR; }
+inline Share share_of(const AttnShape &s, uint32_t heads, uint32_t len)
+{
+    const uint64_t blocks = (uint64_t)s.batch * heads * ((len + 127) / 128), round = s.causal ? 256 : 128;
+    return blocks > 2 * round ? Share::FOUR : blocks > round ? Share::FOUR_BY_TWO : Share::TWO_BY_FOUR;
+}
 
 // ---- who sees whom ------------------------------------------------------------------------------------------------
 
