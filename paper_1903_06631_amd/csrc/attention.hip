@@ -40,8 +40,8 @@ __global__ __launch_bounds__(QW * KG * 64, 2) void k_attention(AttnShape s, Rows
     int k1 = first < sp.ql ? key_hi(s, sp, end - 1) : 0;
     if (parts > 1 && k0 < k1) {      // this part's share of the tiles
         const int64_t n = (k1 - k0 + KT - 1) / KT;
-        k1 = min(k1, k0 + (int)(n * (part + 1) / parts) * KT);
-        k0 += (int)(n * part / parts) * KT;
+        k1 = uniform(min(k1, k0 + (int)(n * (part + 1) / parts) * KT));
+        k0 = uniform(k0 + (int)(n * part / parts) * KT);
     }
     if (k0 < k1) {
         const int used = min(row, sp.ql - 1);       // padding takes the last row's part and is thrown away

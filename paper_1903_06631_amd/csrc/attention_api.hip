@@ -74,7 +74,8 @@ lap::StepShape step_of(const lap_attention_shape *s)
 }
 inline size_t padded_dim(const lap_attention_shape *s) { return s->head_dim <= 64 ? 64 : 128; }
 
-size_t ws_grad(const lap_attention_shape *s) { return up((size_t)s->batch * s->q_heads * s->q_len * 2 * sizeof(float)); }
+size_t ws_stats(const lap_attention_shape *s) { return up((size_t)s->batch * s->q_heads * s->q_len * 2 * sizeof(float)); }
+size_t ws_grad(const lap_attention_shape *s) { return ws_stats(s) + up(lap::grad_sums(shape_of(s))); }
 size_t ws_weights(const lap_attention_shape *s)
 {
     const uint32_t parts = lap::weights_parts(shape_of(s));
@@ -151,7 +152,7 @@ int lap_attention_grad(const lap_attention_shape *s, const lap_rows *dout, const
     if (!rc) rc = check_ws(ws, ws_bytes, ws_grad(s));
     if (rc || (!s->q_len && !s->k_len)) return rc;
     LAP_HIP(lap::launch_attention_grad(shape_of(s), {rows_of(dout), rows_of(q), rows_of(k), rows_of(v), rows_of(out), rows_of(dq),
-                                                     rows_of(dk), rows_of(dv), lse, (float *)ws}, (hipStream_t)hip_stream));
+                                                     rows_of(dk), rows_of(dv), lse, (float *)ws, (float *)((char *)ws + ws_stats(s))}, (hipStream_t)hip_stream));
     return LAP_OK;
 }
 

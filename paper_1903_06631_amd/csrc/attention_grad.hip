@@ -5,7 +5,11 @@
 // Two kernels, each with its sums in registers from the first product to the last, added in a fixed order: one keeps
 // query rows and streams keys (dq; it also leaves delta and the sums in base 2 in the workspace), the other keeps keys and
 // streams the rows of every query head that shares them (dk and dv).  Scores and g.v are computed in both, seven products
-// in place of five: the price for results that do not depend on the order in which workgroups finish.
+// in place of five: the price for results that do not depend on the order in which workgroups finish.  Where there are few
+// keys and many rows, the second kernel's rows are cut into parts, whose sums a third adds in order.
+#include <algorithm>
+#include <cmath>
+
 #include "attn_core.h"
 
 namespace lap {
@@ -131,7 +135,7 @@ __global__ __launch_bounds__(QW * KG * 64, 2) void k_attention_dq(AttnShape s, R
 // KW blocks of 32 keys, the rows of each dealt to RG waves, a block of 32 at a time
 template <class T, int DP, int KW, int RG>
 __global__ __launch_bounds__(KW * RG * 64, 2) void k_attention_dkv(AttnShape s, Rows g, Rows q, Rows k, Rows v, const float *stats, Rows dk,
-                                                           Rows dv, uint32_t tiles)
+                                                                Rows dv, uint32_t parts, float *sums)
 {
     constexpr int NW = KW * RG, BK = 32 * KW, QT = 32 * RG;
     __shared__ __align__(16) T tiles_qg[4][Tile<DP>::size(QT)];
@@ -143,7 +147,7 @@ __global__ __launch_bounds__(KW * RG * 64, 2) void k_attention_dkv(AttnShape s, 
     constexpr int PARTS = (QT + 63) / 64;      // a wave fetches the numbers of 64 rows at once
     __shared__ __align__(16) float lst[2][2][64 * PARTS];
     Work wk;
-    if (!work_item(s, 1, wk)) return;
+    if (!work_item(s, RG > 2 ? parts : 1, wk)) return;
     const uint32_t b = wk.b, kvh = wk.kvh;
     const int first = (int)wk.tile * BK;      // the first keys of a causal head are seen by the most rows
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -157,7 +161,13 @@ __global__ __launch_bounds__(KW * RG * 64, 2) void k_attention_dkv(AttnShape s, 
     const int end = min(first + BK, sp.kl);
     const int r0 = first < sp.kl ? row_lo(s, sp, first) / QT * QT : 0;
     const int r1 = first < sp.kl ? row_hi(s, sp, end - 1) : 0;
-    if (r0 < r1) {
+    const int per = r0 < r1 ? (r1 - r0 + QT - 1) / QT : 0;      // tiles of a head, of which this part takes n0 .. n1 - 1
+    int n0 = 0, n1 = per * (int)group, head0 = (int)(kvh * group), begin = r0;
+    if constexpr (RG > 2) {      // (the few workgroups of the others are enough)
+        n0 = uniform((int)((int64_t)n1 * wk.g / parts)), n1 = uniform((int)((int64_t)n1 * (wk.g + 1) / parts));
+        if (per) head0 = uniform(head0 + n0 / per), begin = uniform(r0 + n0 % per * QT);
+    }
+    if (n0 < n1) {
         const int used = min(key, sp.kl - 1);
         typename Elem<T>::x8 kf[DP / 16];
         load_kept<DP>(kf, (const T *)v.data + (int64_t)b * v.batch + (int64_t)kvh * v.head + (int64_t)used * v.row, s.head_dim, lane);
@@ -172,12 +182,11 @@ __global__ __launch_bounds__(KW * RG * 64, 2) void k_attention_dkv(AttnShape s, 
         const RowRead<DP, T> rows(lane);
         const ColRead<DP, T> cols(lane);
         const TileLoad<DP, QT, NW> tq(q.row, last_chunk, wave, lane), tg(g.row, last_chunk, wave, lane);
-        const int per = (r1 - r0 + QT - 1) / QT, count = per * (int)group;
-        const T *gq = (const T *)q.data + (int64_t)b * q.batch + (int64_t)kvh * group * q.head;
-        const T *gg = (const T *)g.data + (int64_t)b * g.batch + (int64_t)kvh * group * g.head;
-        const float *gs = stats + ((int64_t)b * s.q_heads + (int64_t)kvh * group) * s.q_len;
+        const T *gq = (const T *)q.data + (int64_t)b * q.batch + head0 * q.head;
+        const T *gg = (const T *)g.data + (int64_t)b * g.batch + head0 * g.head;
+        const float *gs = stats + ((int64_t)b * s.q_heads + head0) * s.q_len;
         const int64_t to_delta = (int64_t)s.batch * s.q_heads * s.q_len;
-        int next = r0;      // rows and head of the next tile to ask for
+        int next = begin;      // rows and head of the next tile to ask for
         const auto issue = [&](int to) {
             tq.issue(lq[to], gq, next, sp.ql - 1, wave);
             tg.issue(lg[to], gg, next, sp.ql - 1, wave);
@@ -185,11 +194,11 @@ __global__ __launch_bounds__(KW * RG * 64, 2) void k_attention_dkv(AttnShape s, 
             next += QT;
             if (next >= r1) next = r0, gq += q.head, gg += g.head, gs += s.q_len;
         };
+        int buf = 0, qt = next;
         issue(0);
-        int buf = 0, qt = r0;
-        for (int n = 0; n < count; ++n, buf ^= 1) {
+        for (int n = n0; n < n1; ++n, buf ^= 1) {
             tiles_arrive();
-            if (n + 1 < count) issue(buf ^ 1);
+            if (n + 1 < n1) issue(buf ^ 1);
             const int tile = qt;
             qt = qt + QT >= r1 ? r0 : qt + QT;
             const int at = tile + 32 * rg;
@@ -243,6 +252,18 @@ __global__ __launch_bounds__(KW * RG * 64, 2) void k_attention_dkv(AttnShape s, 
 #pragma unroll
         for (int n = 1; n < RG; ++n) add_sums(box + (n - 1) * KW * (DP / 2 * 64), av, 1.f, lane);
     }
+    if (RG > 2 && parts > 1) {      // [part][batch, kv_heads, k_len][dk, dv][DP]
+        if (key >= sp.kl) return;
+        float *to = sums + (((int64_t)wk.g * s.batch * s.kv_heads + (int64_t)b * s.kv_heads + kvh) * s.k_len + key) * 2 * DP + 4 * (lane >> 5);
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                *(f32x4 *)(to + 32 * d + 2 * i) = f32x4{ak[d][i], ak[d][i + 1], ak[d][i + 2], ak[d][i + 3]};
+                *(f32x4 *)(to + DP + 32 * d + 2 * i) = f32x4{av[d][i], av[d][i + 1], av[d][i + 2], av[d][i + 3]};
+            }
+        return;
+    }
     if (key < (int)s.k_len) {
         if (key >= sp.kl)
 #pragma unroll
@@ -250,6 +271,29 @@ __global__ __launch_bounds__(KW * RG * 64, 2) void k_attention_dkv(AttnShape s, 
         store_kept<DP>((T *)dk.data + (int64_t)b * dk.batch + (int64_t)kvh * dk.head + (int64_t)key * dk.row, ak, s.scale, s.head_dim, lane);
         store_kept<DP>((T *)dv.data + (int64_t)b * dv.batch + (int64_t)kvh * dv.head + (int64_t)key * dv.row, av, 1.f, s.head_dim, lane);
     }
+}
+
+// Eight elements of a key's dk or dv for each thread: the parts in order, rounded once.
+template <class T, int DP> __global__ __launch_bounds__(256) void k_dkv_join(AttnShape s, Rows dk, Rows dv, uint32_t parts, const float *sums)
+{
+    constexpr int ACROSS = 2 * DP / 8;
+    const int64_t at = (int64_t)blockIdx.x * (256 / ACROSS) + threadIdx.x / ACROSS, all = (int64_t)s.batch * s.kv_heads * s.k_len;
+    if (at >= all) return;
+    const uint32_t e = threadIdx.x % ACROSS * 8 % DP, key = (uint32_t)(at % s.k_len);
+    const bool second = threadIdx.x % ACROSS >= DP / 8;
+    const uint32_t h = (uint32_t)(at / s.k_len % s.kv_heads), b = (uint32_t)(at / s.k_len / s.kv_heads);
+    if (e >= s.head_dim) return;
+    f32x4 y[2] = {};
+    if ((int)key < span_of(s, b).kl) {
+        const f32x4 *from = (const f32x4 *)(sums + (at * 2 + second) * DP + e);
+        for (uint32_t i = 0; i < parts; ++i, from += all * 2 * DP / 4) y[0] += from[0], y[1] += from[1];
+    }
+    const float by = second ? 1.f : s.scale;
+    typename Elem<T>::x8 z;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) z[j] = (T)(y[j / 4][j % 4] * by);
+    const Rows &to = second ? dv : dk;
+    *(typename Elem<T>::x8 *)((T *)to.data + (int64_t)b * to.batch + (int64_t)h * to.head + (int64_t)key * to.row + e) = z;
 }
 
 template <class T, int DP, int QW, int KG, int KT> hipError_t launch_dq(const AttnShape &s, const AttnGrad &a, hipStream_t st)
@@ -261,8 +305,12 @@ template <class T, int DP, int QW, int KG, int KT> hipError_t launch_dq(const At
 }
 template <class T, int DP, int KW, int RG> hipError_t launch_dkv(const AttnShape &s, const AttnGrad &a, hipStream_t st)
 {
-    const uint32_t tiles = (s.k_len + 32 * KW - 1) / (32 * KW), total = padded_caches(s.batch * s.kv_heads) * tiles;
-    k_attention_dkv<T, DP, KW, RG><<<total, KW * RG * 64, 0, st>>>(s, a.g, a.q, a.k, a.v, a.stats, a.dk, a.dv, tiles);
+    const uint32_t tiles = (s.k_len + 32 * KW - 1) / (32 * KW), parts = grad_parts(s), total = padded_caches(s.batch * s.kv_heads) * tiles * parts;
+    k_attention_dkv<T, DP, KW, RG><<<total, KW * RG * 64, 0, st>>>(s, a.g, a.q, a.k, a.v, a.stats, a.dk, a.dv, parts, a.sums);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || parts == 1) return e;
+    const uint64_t rows = (uint64_t)s.batch * s.kv_heads * s.k_len, per = 256 / (2 * DP / 8);
+    k_dkv_join<T, DP><<<(uint32_t)((rows + per - 1) / per), 256, 0, st>>>(s, a.dk, a.dv, parts, a.sums);
     return hipGetLastError();
 }
 
@@ -281,6 +329,30 @@ hipError_t launch(const AttnShape &s, const AttnGrad &a, hipStream_t st)
 }
 
 }  // namespace
+
+// Parts of the rows that the second kernel streams: where there are few keys and many rows (query heads that share a key
+// head are rows too), the number that ends first by this estimate, in us: a workgroup's 64 keys take 2.2 for each 128
+// rows, 256 workgroups at a time; under a causal mask half of that on the average, the longest first; every part's sums are
+// written and read once at 5 TB/s, by a kernel more.  Backward passes, causal, 8 heads on one x 2048 tokens 80 us (in one part
+// 255), 16 on 2 x 4096 tokens 274 (542); all keys visible, 2 sequences of 5013 tokens, 4 heads on one 444 (469).
+uint32_t grad_parts(const AttnShape &s)
+{
+    if (!s.k_len || !s.q_len || share_of(s, s.kv_heads, s.k_len) != Share::TWO_BY_FOUR) return 1;
+    const double groups = (double)s.batch * s.kv_heads * ((s.k_len + 63) / 64), rows = (double)(s.q_heads / s.kv_heads) * s.q_len;
+    const double whole = rows / 128 * 2.2, sums = groups * 64 * 2 * (s.head_dim <= 64 ? 64 : 128) * 8 / 5e6;
+    uint32_t best = 1;
+    double least = 0;
+    for (uint32_t p = 1; p <= 16 && (p == 1 || rows / p >= 512); ++p) {
+        const double time = (s.causal ? std::max(groups * whole / 512, whole / p) : std::ceil(groups * p / 256) * whole / p) + (p > 1 ? 6 + p * sums : 0);
+        if (p == 1 || time < least) best = p, least = time;
+    }
+    return best;
+}
+size_t grad_sums(const AttnShape &s)
+{
+    const uint32_t parts = grad_parts(s);
+    return parts == 1 ? 0 : (size_t)parts * s.batch * s.kv_heads * s.k_len * 2 * (s.head_dim <= 64 ? 64 : 128) * sizeof(float);
+}
 
 hipError_t launch_attention_grad(const AttnShape &s, const AttnGrad &a, hipStream_t st)
 {

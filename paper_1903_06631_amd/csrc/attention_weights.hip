@@ -35,7 +35,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_weights(AttnShape s, R
     const int r0 = first < sp.kl ? row_lo(s, sp, first) / QT * QT : 0;
     const int r1 = first < sp.kl ? row_hi(s, sp, end - 1) : 0;
     const int per = r0 < r1 ? (r1 - r0 + QT - 1) / QT : 0;
-    const int n0 = (int)((int64_t)per * group * wk.g / parts), n1 = (int)((int64_t)per * group * (wk.g + 1) / parts);
+    const int n0 = uniform((int)((int64_t)per * group * wk.g / parts)), n1 = uniform((int)((int64_t)per * group * (wk.g + 1) / parts));
     if (n0 < n1) {
         typename Elem<T>::x8 kf[KB][DP / 16];
         int hi[KB], lo[KB];
@@ -51,10 +51,10 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_weights(AttnShape s, R
         const float c = s.scale * LOG2E;
         const RowRead<DP, T> rows(lane);
         const TileLoad<DP, QT, NW> tq(q.row, (int)s.head_dim / 8 - 1, wave, lane);
-        const int64_t head0 = (int64_t)kvh * group + n0 / per;
+        const int64_t head0 = uniform((int)(kvh * group) + n0 / per);
         const T *gq = (const T *)q.data + (int64_t)b * q.batch + head0 * q.head;
         const float *gs = lse + ((int64_t)b * s.q_heads + head0) * s.q_len;
-        int next = r0 + n0 % per * QT;      // rows of the next tile to ask for
+        int next = uniform(r0 + n0 % per * QT);      // rows of the next tile to ask for
         const auto issue = [&](int to) {
             tq.issue(lq[to], gq, next, sp.ql - 1, wave);
             if (wave == 0) load_floats(lst[to], gs, next, sp.ql - 1, 0, lane);

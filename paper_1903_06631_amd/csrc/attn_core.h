@@ -41,6 +41,8 @@ constexpr float LN2 = 0.6931471805599453f;
 constexpr float LOWEST = -1e30f;      // running maximum of a row that has seen no key
 #define ATTN_INF __builtin_inff()
 
+// a number that all lanes hold alike, told to the compiler (divisions leave theirs in vector registers)
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // the larger of a lane's value and its partner's in the other half of the wave (and the same for a sum)

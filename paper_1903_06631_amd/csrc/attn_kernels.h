@@ -27,7 +27,10 @@ struct AttnGrad {
     Rows g, q, k, v, out, dq, dk, dv;
     const float *lse;
     float *stats;       // sums in base 2 (plus infinity: no key) [batch, q_heads, q_len], then delta likewise
+    float *sums;        // grad_sums(s) bytes
 };
+uint32_t grad_parts(const AttnShape &s);
+size_t grad_sums(const AttnShape &s);
 hipError_t launch_attention_grad(const AttnShape &s, const AttnGrad &a, hipStream_t st);
 // sums: [batch, kv_heads, weights_parts(s), k_len], unless that is one part
 uint32_t weights_blocks(const AttnShape &s);

@@ -76,7 +76,10 @@ CASES = [
     (BF, 128, 66, 33, 130, 140, True, 0, [130, 0, 77, 64], [140, 140, 5, 129], "bhnd"),
     (HF, 64, 140, 70, 150, 170, True, 40, [150, 128, 1, 97], [170, 128, 64, 33], "bnhd"),
     (BF, 72, 132, 132, 129, 70, True, 0, [129, 128, 65, 2], [70, 64, 33, 70], "bhnd"),
-    (BF, 64, 8, 1, 1100, 1300, True, 0, None, None, "bhnd"),          # the weights' rows in parts
+    # many rows on few keys: the rows in parts, for the weights and for the keys' gradients
+    (BF, 64, 8, 1, 1100, 1300, True, 0, None, None, "bhnd"),
+    (HF, 120, 8, 2, 900, 333, False, 0, [900, 17], [333, 0], "gaps"),
+    (BF, 128, 12, 2, 400, 400, True, 50, [400, 100, 1], [400, 50, 7], "bhnd"),
 ]
 
 
