@@ -5,6 +5,8 @@
 // with c = scale log2(e), l += sum p, O^T += V^T P^T.  Nothing of the size queries x keys is ever stored.  Where there are few
 // rows and many keys, the keys are cut into parts, a workgroup each, which leave m, l and O in the workspace for a second
 // kernel to join.
+#include <type_traits>
+
 #include "attn_core.h"
 
 namespace lap {
@@ -33,8 +35,16 @@ __global__ __launch_bounds__(QW * KG * 64, 2) void k_attention(AttnShape s, Rows
     T *orow = (T *)o.data + (int64_t)b * o.batch + (int64_t)h * o.head + (int64_t)row * o.row;
     float *lrow = lse + ((int64_t)b * s.q_heads + h) * s.q_len + row;
 
-    f32x16 acc[DP / 32] = {};
-    float m = LOWEST, l = 0.f;
+    f32x16 acc[DP / 32];
+    float m, l;
+    __shared__ int again;
+    if (threadIdx.x == 0) again = 0;
+    const auto clear = [&] {
+        m = LOWEST, l = 0.f;
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) acc[d] = f32x16{};
+    };
+    clear();
     const int end = min(first + BQ, sp.ql);         // rows in use
     int k0 = first < sp.ql ? key_lo(s, sp, first) / KT * KT : 0;
     int k1 = first < sp.ql ? key_hi(s, sp, end - 1) : 0;
@@ -49,7 +59,6 @@ __global__ __launch_bounds__(QW * KG * 64, 2) void k_attention(AttnShape s, Rows
         const T *gk = (const T *)k.data + (int64_t)b * k.batch + (int64_t)wk.kvh * k.head;
         const T *gv = (const T *)v.data + (int64_t)b * v.batch + (int64_t)wk.kvh * v.head;
         const TileLoad<DP, KT, NW> tk(k.row, last_chunk, wave, lane), tv(v.row, last_chunk, wave, lane);
-        tk.issue(lk[0], gk, k0, last, wave);
         typename Elem<T>::x8 qf[DP / 16];
         load_kept<DP>(qf, (const T *)q.data + (int64_t)b * q.batch + (int64_t)h * q.head + (int64_t)used * q.row, s.head_dim, lane);
         const int hi = key_hi(s, sp, used), lo = key_lo(s, sp, used);
@@ -60,64 +69,105 @@ __global__ __launch_bounds__(QW * KG * 64, 2) void k_attention(AttnShape s, Rows
         const RowRead<DP, T> rows(lane);
         const ColRead<DP, T> cols(lane);
 
-        tv.issue(lv[0], gv, k0, last, wave);
-        int buf = 0;
-        for (int kt = k0; kt < k1; kt += KT, buf ^= 1) {
-            tiles_arrive();
-            if (kt + KT < k1) {
-                tk.issue(lk[buf ^ 1], gk, kt + KT, last, wave);
-                tv.issue(lv[buf ^ 1], gv, kt + KT, last, wave);
-            }
-            const int mine = kt + 32 * NB * kg;
-            if (mine >= any_hi || mine + 32 * NB <= any_lo) continue;
-            f32x16 x[NB] = {};
-#pragma unroll
-            for (int kb = 0; kb < NB; ++kb)
-#pragma unroll
-                for (int d = 0; d < DP / 16; ++d) x[kb] = Elem<T>::mfma(rows.get(lk[buf], NB * kg + kb, d), qf[d], x[kb]);
-            reads_ahead<NB * DP / 16, 1, NB * DP / 32>();
-            if (mine + 32 * NB > all_hi || mine < all_lo) {
-                const int at = mine + 4 * (lane >> 5);
+        const auto pass = [&](auto careful) {
+            constexpr bool care = decltype(careful)::value;
+            bool odd = false;      // blocks have been left out
+            tk.issue(lk[0], gk, k0, last, wave);
+            tv.issue(lv[0], gv, k0, last, wave);
+            int buf = 0;
+            for (int kt = k0; kt < k1; kt += KT, buf ^= 1) {
+                tiles_arrive();
+                if (kt + KT < k1) {
+                    tk.issue(lk[buf ^ 1], gk, kt + KT, last, wave);
+                    tv.issue(lv[buf ^ 1], gv, kt + KT, last, wave);
+                }
+                const int mine = kt + 32 * NB * kg;
+                if (mine >= any_hi || mine + 32 * NB <= any_lo) continue;
+                f32x16 x[NB] = {};
 #pragma unroll
                 for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int key = at + 32 * kb + 8 * (i / 4) + i % 4;
-                        x[kb][i] = key < hi && key >= lo ? x[kb][i] : -ATTN_INF;
-                    }
-            }
-            float top = x[0][0];
+                    for (int d = 0; d < DP / 16; ++d) x[kb] = Elem<T>::mfma(rows.get(lk[buf], NB * kg + kb, d), qf[d], x[kb]);
+                reads_ahead<NB * DP / 16, 1, NB * DP / 32>();
+                bool finite = true;
+                if (mine + 32 * NB > all_hi || mine < all_lo) {
 #pragma unroll
-            for (int kb = 0; kb < NB; ++kb)
+                    for (int kb = 0; kb < NB; ++kb)
+                        if (care) finite &= block_is_finite<DP>(lv[buf], NB * kg + kb, lane);
+                    const int at = mine + 4 * (lane >> 5);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, x[kb][i]);
-            top = half_max(top);
-            // The sums stay on an old maximum until a score passes it by a factor of 2^8: what is rounded to 16 bits keeps
-            // its relative error, and rows seldom come to that more than once or twice.
-            if (__ballot((top - m) * c > 8.f)) {
-                const float up = fmaxf(m, top), by = exp2_fast((m - up) * c);
-                m = up;
-                l *= by;
+                    for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
-                for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[d][i] *= by;
-            }
-            const float mc = m * c;
-            float part = 0.f;
-#pragma unroll
-            for (int t = 0; t < 2 * NB; ++t) {
-                float p[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    p[i] = exp2_fast(__builtin_fmaf(x[t / 2][8 * (t % 2) + i], c, -mc));
-                    part += p[i];
+                        for (int i = 0; i < 16; ++i) {
+                            const int key = at + 32 * kb + 8 * (i / 4) + i % 4;
+                            x[kb][i] = key < hi && key >= lo ? x[kb][i] : -ATTN_INF;
+                        }
                 }
-                const auto pf = round8<T>(p, 0);
+                float top = x[0][0];
 #pragma unroll
-                for (int d = 0; d < DP / 32; ++d) acc[d] = Elem<T>::mfma(cols.get(lv[buf], 2 * NB * kg + t, d), pf, acc[d]);
+                for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) top = fmaxf(top, x[kb][i]);
+                top = half_max(top);
+                // The sums stay on an old maximum until a score passes it by a factor of 2^8: what is rounded to 16 bits keeps
+                // its relative error, and rows seldom come to that more than once or twice.
+                if (__ballot((top - m) * c > 8.f)) {
+                    const float up = fmaxf(m, top), by = exp2_fast((m - up) * c);
+                    m = up;
+                    l *= by;
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[d][i] *= by;
+                }
+                const float mc = m * c;
+                float part = 0.f;
+                if (!finite) {
+                    odd = true;
+#pragma unroll
+                    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) l += exp2_fast(__builtin_fmaf(x[kb][i], c, -mc));
+                    continue;
+                }
+#pragma unroll
+                for (int t = 0; t < 2 * NB; ++t) {
+                    float p[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        p[i] = exp2_fast(__builtin_fmaf(x[t / 2][8 * (t % 2) + i], c, -mc));
+                        part += p[i];
+                    }
+                    const auto pf = round8<T>(p, 0);
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d) acc[d] = Elem<T>::mfma(cols.get(lv[buf], 2 * NB * kg + t, d), pf, acc[d]);
+                }
+                l += part;
             }
-            l += part;
+            if constexpr (care) {
+                if (!odd) return;
+                const T *const qrow = (const T *)q.data + (int64_t)b * q.batch + (int64_t)h * q.head + (int64_t)used * q.row;
+#pragma unroll 1
+                for (int kt = k0; kt < k1; kt += KT) {
+                    const int mine = kt + 32 * NB * kg;
+                    if (mine >= any_hi || mine + 32 * NB <= any_lo || (mine + 32 * NB <= all_hi && mine >= all_lo)) continue;
+                    bool finite = true;
+                    for (int kb = 0; kb < NB; ++kb) finite &= rows_are_finite(gv, v.row, mine + 32 * kb, last, s.head_dim, lane);
+                    if (finite) continue;
+#pragma unroll 1
+                    for (int key = max(mine, lo); key < min(mine + 32 * NB, hi); ++key) {
+                        const float x = dot(qrow, gk + (int64_t)key * k.row, s.head_dim);
+                        add_row<DP>(acc, gv + (int64_t)key * v.row, exp2_fast((x - m) * c), s.head_dim, lane);
+                    }
+                }
+            }
+        };
+        pass(std::false_type());
+        if (!sums_are_numbers(acc) && lane == 0) again = 1;
+        __syncthreads();
+        if (again) {
+            clear();
+            pass(std::true_type());
         }
     }
     l = half_sum(l);

@@ -9,6 +9,7 @@
 // keys and many rows, the second kernel's rows are cut into parts, whose sums a third adds in order.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "attn_core.h"
 
@@ -37,6 +38,8 @@ __global__ __launch_bounds__(QW * KG * 64, 2) void k_attention_dq(AttnShape s, R
     T *drow = (T *)dq.data + (int64_t)b * dq.batch + (int64_t)h * dq.head + (int64_t)row * dq.row;
     const int64_t at = ((int64_t)b * s.q_heads + h) * s.q_len;
 
+    __shared__ int again;
+    if (threadIdx.x == 0) again = 0;
     f32x16 acc[DP / 32] = {};
     const int end = min(first + BQ, sp.ql);
     const int k0 = first < sp.ql ? key_lo(s, sp, first) / KT * KT : 0;
@@ -75,42 +78,77 @@ __global__ __launch_bounds__(QW * KG * 64, 2) void k_attention_dq(AttnShape s, R
             const RowRead<DP, T> rows(lane);
             const ColRead<DP, T> cols(lane);
             const TileLoad<DP, KT, NW> tk(k.row, last_chunk, wave, lane), tv(v.row, last_chunk, wave, lane);
-            tk.issue(lk[0], gk, k0, sp.kl - 1, wave);
-            tv.issue(lv[0], gv, k0, sp.kl - 1, wave);
-            int buf = 0;
-            for (int kt = k0; kt < k1; kt += KT, buf ^= 1) {
-                tiles_arrive();
-                if (kt + KT < k1) {
-                    tk.issue(lk[buf ^ 1], gk, kt + KT, sp.kl - 1, wave);
-                    tv.issue(lv[buf ^ 1], gv, kt + KT, sp.kl - 1, wave);
-                }
+            const auto pass = [&](auto careful) {
+                constexpr bool care = decltype(careful)::value;
+                bool odd = false;      // blocks have been left out
+                tk.issue(lk[0], gk, k0, sp.kl - 1, wave);
+                tv.issue(lv[0], gv, k0, sp.kl - 1, wave);
+                int buf = 0;
+                for (int kt = k0; kt < k1; kt += KT, buf ^= 1) {
+                    tiles_arrive();
+                    if (kt + KT < k1) {
+                        tk.issue(lk[buf ^ 1], gk, kt + KT, sp.kl - 1, wave);
+                        tv.issue(lv[buf ^ 1], gv, kt + KT, sp.kl - 1, wave);
+                    }
 #pragma unroll
-                for (int n = 0; n < KT / 32 / KG; ++n) {
-                    const int kb = KT / 32 / KG * kg + n, at = kt + 32 * kb;
-                    if (at >= any_hi || at + 32 <= any_lo) continue;
-                    f32x16 x = {}, y = {};
+                    for (int n = 0; n < KT / 32 / KG; ++n) {
+                        const int kb = KT / 32 / KG * kg + n, at = kt + 32 * kb;
+                        if (at >= any_hi || at + 32 <= any_lo) continue;
+                        f32x16 x = {}, y = {};
 #pragma unroll
-                    for (int d = 0; d < DP / 16; ++d) x = Elem<T>::mfma(rows.get(lk[buf], kb, d), qf[d], x);
+                        for (int d = 0; d < DP / 16; ++d) x = Elem<T>::mfma(rows.get(lk[buf], kb, d), qf[d], x);
 #pragma unroll
-                    for (int d = 0; d < DP / 16; ++d) y = Elem<T>::mfma(rows.get(lv[buf], kb, d), gf[d], y);
-                    float ds[16];
+                        for (int d = 0; d < DP / 16; ++d) y = Elem<T>::mfma(rows.get(lv[buf], kb, d), gf[d], y);
+                        float ds[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) ds[i] = exp2_fast(__builtin_fmaf(x[i], c, -l2)) * (y[i] - delta);
-                    if (at + 32 > all_hi || at < all_lo) {
-                        const int key0 = at + 4 * (lane >> 5);
+                        for (int i = 0; i < 16; ++i) ds[i] = exp2_fast(__builtin_fmaf(x[i], c, -l2)) * (y[i] - delta);
+                        if (at + 32 > all_hi || at < all_lo) {
+                            const int key0 = at + 4 * (lane >> 5);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int key = key0 + 8 * (i / 4) + i % 4;
-                            ds[i] = key < hi && key >= lo ? ds[i] : 0.f;
+                            for (int i = 0; i < 16; ++i) {
+                                const int key = key0 + 8 * (i / 4) + i % 4;
+                                ds[i] = key < hi && key >= lo ? ds[i] : 0.f;
+                            }
+                            if (care && !block_is_finite<DP>(lk[buf], kb, lane)) {
+                                odd = true;
+                                continue;
+                            }
+                        }
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) {
+                            const auto df = round8<T>(ds, 8 * t);
+#pragma unroll
+                            for (int d = 0; d < DP / 32; ++d) acc[d] = Elem<T>::mfma(cols.get(lk[buf], 2 * kb + t, d), df, acc[d]);
                         }
                     }
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        const auto df = round8<T>(ds, 8 * t);
-#pragma unroll
-                        for (int d = 0; d < DP / 32; ++d) acc[d] = Elem<T>::mfma(cols.get(lk[buf], 2 * kb + t, d), df, acc[d]);
-                    }
                 }
+                if constexpr (care) {
+                    if (!odd) return;
+                    const T *const qrow = (const T *)q.data + (int64_t)b * q.batch + (int64_t)h * q.head + (int64_t)used * q.row;
+                    const T *const grow = (const T *)g.data + (int64_t)b * g.batch + (int64_t)h * g.head + (int64_t)used * g.row;
+#pragma unroll 1
+                    for (int kt = k0; kt < k1; kt += KT)
+#pragma unroll 1
+                        for (int n = 0; n < KT / 32 / KG; ++n) {
+                            const int at = kt + 32 * (KT / 32 / KG * kg + n);
+                            if (at >= any_hi || at + 32 <= any_lo || (at + 32 <= all_hi && at >= all_lo)) continue;
+                            if (rows_are_finite(gk, k.row, at, sp.kl - 1, s.head_dim, lane)) continue;
+#pragma unroll 1
+                            for (int key = max(at, lo); key < min(at + 32, hi); ++key) {
+                                const T *const krow = gk + (int64_t)key * k.row;
+                                const float p = exp2_fast(__builtin_fmaf(dot(qrow, krow, s.head_dim), c, -l2));
+                                add_row<DP>(acc, krow, p * (dot(grow, gv + (int64_t)key * v.row, s.head_dim) - delta), s.head_dim, lane);
+                            }
+                        }
+                }
+            };
+            pass(std::false_type());
+            if (!sums_are_numbers(acc) && lane == 0) again = 1;
+            __syncthreads();
+            if (again) {
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d) acc[d] = f32x16{};
+                pass(std::true_type());
             }
         }
     }
@@ -157,6 +195,8 @@ __global__ __launch_bounds__(KW * RG * 64, 2) void k_attention_dkv(AttnShape s, 
     const int kw = wave % KW, rg = wave / KW;
     const int w0 = first + 32 * kw;
     const int key = w0 + (lane & 31);
+    __shared__ int again;
+    if (threadIdx.x == 0) again = 0;
     f32x16 ak[DP / 32] = {}, av[DP / 32] = {};
     const int end = min(first + BK, sp.kl);
     const int r0 = first < sp.kl ? row_lo(s, sp, first) / QT * QT : 0;
@@ -182,58 +222,96 @@ __global__ __launch_bounds__(KW * RG * 64, 2) void k_attention_dkv(AttnShape s, 
         const RowRead<DP, T> rows(lane);
         const ColRead<DP, T> cols(lane);
         const TileLoad<DP, QT, NW> tq(q.row, last_chunk, wave, lane), tg(g.row, last_chunk, wave, lane);
-        const T *gq = (const T *)q.data + (int64_t)b * q.batch + head0 * q.head;
-        const T *gg = (const T *)g.data + (int64_t)b * g.batch + head0 * g.head;
-        const float *gs = stats + ((int64_t)b * s.q_heads + head0) * s.q_len;
         const int64_t to_delta = (int64_t)s.batch * s.q_heads * s.q_len;
-        int next = begin;      // rows and head of the next tile to ask for
-        const auto issue = [&](int to) {
-            tq.issue(lq[to], gq, next, sp.ql - 1, wave);
-            tg.issue(lg[to], gg, next, sp.ql - 1, wave);
-            if (wave < 2 * PARTS) load_floats(lst[to][wave / PARTS], gs + wave / PARTS * to_delta, next, sp.ql - 1, wave % PARTS, lane);
-            next += QT;
-            if (next >= r1) next = r0, gq += q.head, gg += g.head, gs += s.q_len;
-        };
-        int buf = 0, qt = next;
-        issue(0);
-        for (int n = n0; n < n1; ++n, buf ^= 1) {
-            tiles_arrive();
-            if (n + 1 < n1) issue(buf ^ 1);
-            const int tile = qt;
-            qt = qt + QT >= r1 ? r0 : qt + QT;
-            const int at = tile + 32 * rg;
-            if (at >= any_hi || at + 32 <= any_lo) continue;
-            f32x16 x = {}, y = {};
+        const auto pass = [&](auto careful) {
+            constexpr bool care = decltype(careful)::value;
+            bool odd = false;      // blocks have been left out
+            const T *gq = (const T *)q.data + (int64_t)b * q.batch + head0 * q.head;
+            const T *gg = (const T *)g.data + (int64_t)b * g.batch + head0 * g.head;
+            const float *gs = stats + ((int64_t)b * s.q_heads + head0) * s.q_len;
+            int next = begin;      // rows and head of the next tile to ask for
+            const auto issue = [&](int to) {
+                tq.issue(lq[to], gq, next, sp.ql - 1, wave);
+                tg.issue(lg[to], gg, next, sp.ql - 1, wave);
+                if (wave < 2 * PARTS) load_floats(lst[to][wave / PARTS], gs + wave / PARTS * to_delta, next, sp.ql - 1, wave % PARTS, lane);
+                next += QT;
+                if (next >= r1) next = r0, gq += q.head, gg += g.head, gs += s.q_len;
+            };
+            int buf = 0, qt = next;
+            issue(0);
+            for (int n = n0; n < n1; ++n, buf ^= 1) {
+                tiles_arrive();
+                if (n + 1 < n1) issue(buf ^ 1);
+                const int tile = qt;
+                qt = qt + QT >= r1 ? r0 : qt + QT;
+                const int at = tile + 32 * rg;
+                if (at >= any_hi || at + 32 <= any_lo) continue;
+                f32x16 x = {}, y = {};
 #pragma unroll
-            for (int d = 0; d < DP / 16; ++d) x = Elem<T>::mfma(rows.get(lq[buf], rg, d), kf[d], x);
+                for (int d = 0; d < DP / 16; ++d) x = Elem<T>::mfma(rows.get(lq[buf], rg, d), kf[d], x);
 #pragma unroll
-            for (int d = 0; d < DP / 16; ++d) y = Elem<T>::mfma(rows.get(lg[buf], rg, d), rows.get(lkept, kw, d), y);
-            const float *const l2 = lst[buf][0] + 32 * rg + 4 * (lane >> 5), *const delta = lst[buf][1] + 32 * rg + 4 * (lane >> 5);
-            float p[16], ds[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                p[i] = exp2_fast(__builtin_fmaf(x[i], c, -l2[8 * (i / 4) + i % 4]));
-                ds[i] = p[i] * (y[i] - delta[8 * (i / 4) + i % 4]);
-            }
-            if (at + 32 > all_hi || at < all_lo) {
-                const int row0 = at + 4 * (lane >> 5);
+                for (int d = 0; d < DP / 16; ++d) y = Elem<T>::mfma(rows.get(lg[buf], rg, d), rows.get(lkept, kw, d), y);
+                const float *const l2 = lst[buf][0] + 32 * rg + 4 * (lane >> 5), *const delta = lst[buf][1] + 32 * rg + 4 * (lane >> 5);
+                float p[16], ds[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int row = row0 + 8 * (i / 4) + i % 4;
-                    const bool in = row < hi && row >= lo;
-                    p[i] = in ? p[i] : 0.f;
-                    ds[i] = in ? ds[i] : 0.f;
+                    p[i] = exp2_fast(__builtin_fmaf(x[i], c, -l2[8 * (i / 4) + i % 4]));
+                    ds[i] = p[i] * (y[i] - delta[8 * (i / 4) + i % 4]);
+                }
+                if (at + 32 > all_hi || at < all_lo) {
+                    const int row0 = at + 4 * (lane >> 5);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int row = row0 + 8 * (i / 4) + i % 4;
+                        const bool in = row < hi && row >= lo;
+                        p[i] = in ? p[i] : 0.f;
+                        ds[i] = in ? ds[i] : 0.f;
+                    }
+                    if (care && (!block_is_finite<DP>(lq[buf], rg, lane) || !block_is_finite<DP>(lg[buf], rg, lane))) {
+                        odd = true;
+                        continue;
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const auto pf = round8<T>(p, 8 * t), df = round8<T>(ds, 8 * t);
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d) {
+                        av[d] = Elem<T>::mfma(cols.get(lg[buf], 2 * rg + t, d), pf, av[d]);
+                        ak[d] = Elem<T>::mfma(cols.get(lq[buf], 2 * rg + t, d), df, ak[d]);
+                    }
                 }
             }
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const auto pf = round8<T>(p, 8 * t), df = round8<T>(ds, 8 * t);
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d) {
-                    av[d] = Elem<T>::mfma(cols.get(lg[buf], 2 * rg + t, d), pf, av[d]);
-                    ak[d] = Elem<T>::mfma(cols.get(lq[buf], 2 * rg + t, d), df, ak[d]);
+            if constexpr (care) {
+                if (!odd) return;
+                const T *const krow = (const T *)k.data + (int64_t)b * k.batch + (int64_t)kvh * k.head + (int64_t)used * k.row;
+                const T *const vrow = (const T *)v.data + (int64_t)b * v.batch + (int64_t)kvh * v.head + (int64_t)used * v.row;
+#pragma unroll 1
+                for (int n = n0; n < n1; ++n) {
+                    const int at = r0 + n % per * QT + 32 * rg;
+                    if (at >= any_hi || at + 32 <= any_lo || (at + 32 <= all_hi && at >= all_lo)) continue;
+                    const int64_t head = (int64_t)kvh * group + n / per;
+                    const T *const q0 = (const T *)q.data + (int64_t)b * q.batch + head * q.head;
+                    const T *const g0 = (const T *)g.data + (int64_t)b * g.batch + head * g.head;
+                    const float *const st = stats + ((int64_t)b * s.q_heads + head) * s.q_len;
+                    if (rows_are_finite(q0, q.row, at, sp.ql - 1, s.head_dim, lane) && rows_are_finite(g0, g.row, at, sp.ql - 1, s.head_dim, lane)) continue;
+#pragma unroll 1
+                    for (int row = max(at, lo); row < min(at + 32, hi); ++row) {
+                        const T *const qrow = q0 + (int64_t)row * q.row, *const grow = g0 + (int64_t)row * g.row;
+                        const float p = exp2_fast(__builtin_fmaf(dot(qrow, krow, s.head_dim), c, -st[row]));
+                        add_row<DP>(av, grow, p, s.head_dim, lane);
+                        add_row<DP>(ak, qrow, p * (dot(grow, vrow, s.head_dim) - st[to_delta + row]), s.head_dim, lane);
+                    }
                 }
             }
+        };
+        pass(std::false_type());
+        if (!(sums_are_numbers(ak) && sums_are_numbers(av)) && lane == 0) again = 1;
+        __syncthreads();
+        if (again) {
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) ak[d] = av[d] = f32x16{};
+            pass(std::true_type());
         }
     }
     if constexpr (RG > 1) {

@@ -196,6 +196,68 @@ __device__ __forceinline__ void keep_in_lds(T *tile, int block, const typename E
         *(typename Elem<T>::x8 *)(tile + Tile<DP>::size(32) * block + Tile<DP>::place(lane & 31, 2 * k + (lane >> 5))) = f[k];
 }
 
+// Hidden pairs have weight zero, but zero times infinity is not a number, and so then is the sum.  A workgroup whose sums are
+// all numbers is done.  One with a sum that is not (which pairs that are seen may have made so too) runs again with care:
+// where some pairs of a block of 32 rows are hidden, the block is looked over, one with a value that is not finite is left
+// out, and after the loop its rows are added one by one, from memory, to the sums of the kept rows that see them.  The look
+// at the sums takes 1 to 3 % of a call; a look at every such block in the first place took 1 to 13 %.
+template <int N> __device__ __forceinline__ bool sums_are_numbers(const f32x16 (&c)[N])
+{
+    float x[4] = {};      // infinities count as well
+#pragma unroll
+    for (int d = 0; d < N; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i % 4] = __builtin_fmaf(c[d][i], 0.f, x[i % 4]);
+    return __ballot(!((x[0] + x[1]) + (x[2] + x[3]) == 0.f)) == 0;
+}
+template <int DP, class T> __device__ __forceinline__ bool block_is_finite(const T *tile, int block, int lane)
+{
+    typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+    constexpr unsigned short MAGNITUDE = 0x7FFF, TOP = __is_same(T, __bf16) ? 0x7F80 : 0x7C00;
+    u16x8 most = {};
+#pragma unroll
+    for (int j = 0; j < 32 * DP / 8 / 64; ++j) {
+        const u16x8 x = *(const u16x8 *)(tile + Tile<DP>::size(32) * block + j * Tile<DP>::GROUP + lane * 8) & MAGNITUDE;
+        most = __builtin_elementwise_max(most, x);
+    }
+    bool fine = true;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) fine &= most[j] < TOP;
+    return __ballot(!fine) == 0;
+}
+// The same of rows first .. first + 31 in memory, those past `last` as copies of it.
+template <class T> __device__ __forceinline__ bool rows_are_finite(const T *g, int64_t stride, int first, int last, uint32_t head_dim, int lane)
+{
+    const T *row = g + (int64_t)min(first + (lane & 31), last) * stride;
+    bool fine = true;
+#pragma unroll 1
+    for (uint32_t e = 0; e < head_dim; ++e) fine &= __builtin_fabsf((float)row[e]) < ATTN_INF;
+    return __ballot(!fine) == 0;
+}
+template <class T> __device__ __forceinline__ float dot(const T *a, const T *b, uint32_t head_dim)
+{
+    float x = 0.f;
+#pragma unroll 1
+    for (uint32_t e = 0; e < head_dim; ++e) x = __builtin_fmaf((float)a[e], (float)b[e], x);
+    return x;
+}
+// a row in memory times its weight added to the sums of a kept row
+template <int DP, class T>
+__device__ __forceinline__ void add_row(f32x16 (&c)[DP / 32], const T *row, float weight, uint32_t head_dim, int lane)
+{
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const uint32_t e = 32 * d + 2 * i + 4 * (lane >> 5);
+            if (e < head_dim) {
+                const auto x = *(const typename Elem<T>::x4 *)(row + e);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) c[d][i + j] = __builtin_fmaf((float)x[j], weight, c[d][i + j]);
+            }
+        }
+}
+
 // A wave's sums through LDS to the wave that adds them up: N times 16 numbers of each lane, lanes side by side
 template <int N> __device__ __forceinline__ void put_sums(float *box, const f32x16 (&c)[N], int lane)
 {

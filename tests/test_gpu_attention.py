@@ -150,15 +150,42 @@ def test_scale_and_large_scores(lap):
         within(got["out"], want.out, want.out_bound, f"out at {scale}")
 
 
-def test_a_row_that_is_not_finite_stays_with_those_that_see_it(lap):
+@pytest.mark.parametrize("kind,d,heads,kv,n,window", [(BF, 128, 2, 2, 200, 0), (HF, 64, 4, 2, 333, 50), (BF, 72, 300, 150, 150, 0), (HF, 128, 700, 700, 130, 33)])
+def test_what_is_not_finite_reaches_only_rows_that_see_it(lap, kind, d, heads, kv, n, window):
+    """Keys, values, queries and gradients with infinities and not-a-numbers in places that a causal mask hides from part of
+    the rows: those are within the bounds of the same call without them, wherever the places fall in a tile."""
     gen = torch.Generator().manual_seed(6)
-    q, k, v = (rows(gen, 2, 1, 200, 64, BF) for _ in range(3))
-    clean = lap.attention(q, k, v, causal=True)["out"]
+    q, g = rows(gen, 1, heads, n, d, kind), rows(gen, 1, heads, n, d, kind)
+    k, v = rows(gen, 1, kv, n, d, kind), rows(gen, 1, kv, n, d, kind)
+    mask = dict(causal=True, window=window)
+    want = ref.Case(q, k, v, **mask)
+    see = want.see[0, 0]
+    clean = lap.attention(q, k, v, **mask)
+    bad_keys = [n // 2 + 3, n - 1]
     k2, v2 = k.clone(), v.clone()
-    k2[0, 0, 150], v2[0, 0, 199] = math.inf, math.nan
-    got = lap.attention(q, k2, v2, causal=True)["out"]
-    assert torch.equal(got[1], clean[1]) and torch.equal(got[0, 0, :128], clean[0, 0, :128])      # rows of earlier tiles
-    assert torch.isnan(got[0, 0, 199]).any()
+    k2[:, :, bad_keys[0]], v2[:, :, bad_keys[0], 5:9], v2[:, :, bad_keys[1]] = math.inf, math.nan, -math.inf
+    got = lap.attention(q, k2, v2, **mask)
+    fine = ~see[:, bad_keys].any(1)
+    assert fine.any() and not fine.all()
+    within(got["lse"][:, :, fine], want.lse[:, :, fine], want.lse_bound[:, :, fine], "lse")
+    within(got["out"][:, :, fine], want.out[:, :, fine], want.out_bound[:, :, fine], "out")
+    assert not torch.isfinite(got["out"][:, :, ~fine.cuda()]).all(-1).any()      # and the others show it
+    exact = want.grads(g, clean["out"])
+    grads = lap.attention_grad(g, q, k2, v2, clean["out"], clean["lse"], **mask)
+    within(grads["dq"][:, :, fine], exact["dq"][0][:, :, fine], exact["dq"][1][:, :, fine], "dq")
+    # rows that only part of the keys is seen from
+    bad_rows = [0, n // 2 - 2]
+    q2, g2 = q.clone(), g.clone()
+    q2[:, :, bad_rows[0]], g2[:, :, bad_rows[1], 1] = math.nan, math.inf
+    grads = lap.attention_grad(g2, q2, k, v, clean["out"], clean["lse"], **mask)
+    fine = ~see[bad_rows].any(0)
+    assert fine.any() and not fine.all()
+    for name in ("dk", "dv"):
+        within(grads[name][:, :, fine], exact[name][0][:, :, fine], exact[name][1][:, :, fine], name)
+    w = lap.attention_weights(q2, k, clean["lse"], **mask)["weights"]
+    value, bound = want.weights()
+    fine = ~see[0]
+    within(w[:, :, fine], value[:, :, fine], bound[:, :, fine], "weights")
 
 
 def test_broadcast_keys_and_their_gradient(lap):
