@@ -54,6 +54,9 @@ def test_rows_and_pointers(lib):
         assert forward(lib, out=rows(**bad)) == -10, bad
     assert forward(lib, lse=None) == -1
     assert lib.lap_attention(shape(), None, rows(), rows(), rows(), FAKE, None, 0, None) == -1
+    few = shape(batch=1, k_len=3000)      # few rows on many keys: the keys in parts, joined in a workspace
+    assert lib.lap_attention_workspace_bytes(0, shape()) == 0 and lib.lap_attention_workspace_bytes(0, few) > 0
+    assert forward(lib, few) == -3
     assert forward(lib, shape(q_len=0), q=rows(data=None), out=rows(data=None), lse=None) == 0      # nothing to do
 
 
@@ -74,7 +77,8 @@ def test_gradient(lib):
 def test_weights(lib):
     call = lambda s=None, q=None, k=None, lse=FAKE, w=FAKE: lib.lap_attention_weights(s or shape(), q or rows(), k or rows(), lse, None, w, None, 0, None)
     assert call(lse=None) == -1 and call(w=None) == -1 and call(q=rows(data=None)) == -1 and call(k=rows(data=FAKE + 2)) == -10
-    assert call(shape(scale=-1.0)) == -9 and call(shape(k_len=0), k=rows(data=None), w=None) == 0
+    assert call(shape(batch=1, q_heads=8, kv_heads=1, q_len=2000)) == -3      # the rows in parts, no workspace
+    assert call(shape(scale=2e6)) == -9 and call(shape(k_len=0), k=rows(data=None), w=None) == 0
 
 
 def test_step(lib):

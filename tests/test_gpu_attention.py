@@ -243,6 +243,12 @@ def test_step(lap, case):
     assert plain["weights"] is None and torch.equal(plain["out"], got["out"]) and torch.equal(plain["lse"], got["lse"])
 
 
+def test_step_without_slots(lap):
+    q, empty = torch.ones(2, 4, 64, dtype=BF, device="cuda"), torch.empty(2, 2, 0, 64, dtype=BF, device="cuda")
+    got = lap.attention_step(q, empty, empty, torch.empty(2, 2, 0, device="cuda"))
+    assert not got["out"].any() and (got["lse"] == -math.inf).all() and got["weights"].numel() == 0
+
+
 def test_step_agrees_with_the_last_row_of_a_prompt(lap):
     gen = torch.Generator().manual_seed(3)
     q, k, v = rows(gen, 2, 8, 300, 128, BF), rows(gen, 2, 2, 300, 128, BF), rows(gen, 2, 2, 300, 128, BF)

@@ -90,6 +90,12 @@ def test_an_evicted_cache_can_be_evicted_again(lap):
     assert all(torch.equal(a[x], b[x]) for x in a)
 
 
+def test_evict_from_nothing(lap):
+    k = torch.empty(2, 3, 0, 64, dtype=torch.bfloat16, device="cuda")
+    got = lap.cache_evict(k, k, torch.empty(2, 3, 0, device="cuda"), 5, 2)
+    assert (got["positions"] == -1).all() and not got["lens"].any() and not got["k"].any() and not got["weights"].any()
+
+
 @pytest.mark.parametrize("n,recent,kind", [(1, 1, "plain"), (5, 2, "ties"), (300, 0, "odd"), (1000, 17, "ties"), (4099, 1000, "odd")])
 def test_insert_many_tokens(lap, n, recent, kind):
     """Into caches that fill up and then drop a slot for each token; one sequence sits out now and then."""
