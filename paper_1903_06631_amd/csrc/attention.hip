@@ -15,7 +15,7 @@ namespace {
 // QW blocks of 32 rows; their keys are dealt to KG waves each, NB blocks of 32 keys at a time.  Where rows are few, waves that
 // share them fill the units that would have none; they join their sums at the end.
 template <class T, int DP, int QW, int KG, int NB>
-__global__ __launch_bounds__(QW * KG * 64, 2) void k_attention(AttnShape s, Rows q, Rows k, Rows v, Rows o, float *lse, uint32_t tiles,
+__global__ __launch_bounds__(QW * KG * 64, NB == 1 && KG == 1 ? 3 : 2) void k_attention(AttnShape s, Rows q, Rows k, Rows v, Rows o, float *lse, uint32_t tiles,
                                                                      uint32_t parts, float *outs, float2 *out_sums)
 {
     constexpr int NW = QW * KG, BQ = 32 * QW, KT = 32 * KG * NB;
@@ -268,7 +268,11 @@ template <class T, int DP>
 hipError_t launch(const AttnShape &s, const Rows &q, const Rows &k, const Rows &v, const Rows &out, float *lse, void *ws, hipStream_t st)
 {
     switch (share_of(s, s.q_heads, s.q_len)) {
-    case Share::FOUR: return launch_as<T, DP, 4, 1, 2>(s, q, k, v, out, lse, ws, st);
+    case Share::FOUR:
+        // 32 keys a tile leave registers for a third wave on a SIMD, where there are that many (3104 blocks of 128
+        // rows: 1325 us for 32 heads of 12345 rows, with 64 keys 1360; 640 blocks: 61 us and 54)
+        if ((uint64_t)s.batch * s.q_heads * ((s.q_len + 127) / 128) > 1024) return launch_as<T, DP, 4, 1, 1>(s, q, k, v, out, lse, ws, st);
+        return launch_as<T, DP, 4, 1, 2>(s, q, k, v, out, lse, ws, st);
     case Share::FOUR_BY_TWO: return launch_as<T, DP, 4, 2, 2>(s, q, k, v, out, lse, ws, st);
     default: return launch_as<T, DP, 2, 4, 1>(s, q, k, v, out, lse, ws, st);
     }

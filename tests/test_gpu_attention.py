@@ -76,6 +76,7 @@ CASES = [
     (BF, 128, 66, 33, 130, 140, True, 0, [130, 0, 77, 64], [140, 140, 5, 129], "bhnd"),
     (HF, 64, 140, 70, 150, 170, True, 40, [150, 128, 1, 97], [170, 128, 64, 33], "bnhd"),
     (BF, 72, 132, 132, 129, 70, True, 0, [129, 128, 65, 2], [70, 64, 33, 70], "bhnd"),
+    (HF, 128, 86, 43, 130, 137, True, 0, [130, 129, 33, 64], [137, 130, 137, 65], "bhnd"),
     # many rows on few keys: the rows in parts, for the weights and for the keys' gradients
     (BF, 64, 8, 1, 1100, 1300, True, 0, None, None, "bhnd"),
     (HF, 120, 8, 2, 900, 333, False, 0, [900, 17], [333, 0], "gaps"),
