@@ -7,7 +7,9 @@
 // registers as a matrix operand, values through LDS, which is where they are transposed.  The heads of a group are the
 // kept rows (up to 32; with fewer, part of the matrix instructions runs empty, at a rate that is far from binding).  A
 // second kernel joins the chunks' sums and outputs; the weights need the joined sums, so the first one leaves the scores
-// (4 bytes for each slot and head beside the slot's 4 head_dim).
+// (4 bytes for each slot and head beside the slot's 4 head_dim).  Measured: 2 caches of 8 heads x 131072 slots x 128, 4 query heads
+// each, 216 + 16 us, the first kernel at 5.1 TB/s (a copy of 2 GiB: 4.9); 64 ragged caches of up to 4096 slots 123 + 12 us; one
+// of 16 heads x 1000 slots 6.2 + 3.5 us.
 #include "attn_core.h"
 
 namespace lap {
