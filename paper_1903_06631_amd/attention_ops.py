@@ -74,10 +74,10 @@ def _refuse(name: str, x, expected) -> None:
     raise ValueError(f"{name}: {tuple(x.shape)} {x.dtype} on {x.device} with strides {x.stride()}, expected {expected}")
 
 
-def _rows(x, name: str, like, shape):
-    """lap_rows of x, which has to be a tensor of this shape and of like's type and device, elements of a row side by side."""
-    if x.dtype is not like.dtype or x.shape != shape or x.get_device() != like.get_device():
-        _refuse(name, x, f"{tuple(shape)} {like.dtype} on {like.device}")
+def _rows(x, name: str, dtype, shape, index: int):
+    """lap_rows of x, which has to be a tensor of this type and shape on this GPU, elements of a row side by side."""
+    if x.dtype is not dtype or x.shape != shape or x.get_device() != index:
+        _refuse(name, x, f"{tuple(shape)} {dtype} on GPU {index}")
     st = x.stride()
     if st[-1] != 1 and x.numel():
         _refuse(name, x, "the elements of a row side by side")
@@ -116,15 +116,18 @@ def _scale(scale: Optional[float], d: int) -> float:
 
 
 def _shape(q, k, causal, window, scale, q_lens, k_lens):
-    b, h, n, d = _four(q, "q")
-    _four(k, "k")
+    """lap_attention_shape, the type, the shapes of queries and keys, the GPU."""
+    qs, ks = _four(q, "q"), _four(k, "k")
+    b, h, n, d = qs
+    _, kv, m, _ = ks
     kind, index = _type(q, "q"), q.get_device()
     if window < 0:
         raise ValueError("window is 0 (none) or a number of keys")
     i32 = torch.int32
-    return _Shape(kind, b, h, k.shape[1], n, k.shape[2], d, 1 if causal else 0, window, _scale(scale, d),
-                  None if q_lens is None else _plain(q_lens, "q_lens", i32, (b,), index),
-                  None if k_lens is None else _plain(k_lens, "k_lens", i32, (b,), index))
+    s = _Shape(kind, b, h, kv, n, m, d, 1 if causal else 0, window, _scale(scale, d),
+               None if q_lens is None else _plain(q_lens, "q_lens", i32, (b,), index),
+               None if k_lens is None else _plain(k_lens, "k_lens", i32, (b,), index))
+    return s, q.dtype, qs, (b, kv, m, d), index
 
 
 def _workspace(ws, need: int, index: int):
@@ -142,13 +145,12 @@ def attention(q, k, v, *, causal: bool = False, window: int = 0, scale: Optional
               out: Optional[dict] = None, ws=None, sync: bool = True):
     """lap_attention: returns dict(out like q, lse [batch, q_heads, q_len]).  scale None: 1 / sqrt(head_dim)."""
     lib = _lib()
-    s, index = _shape(q, k, causal, window, scale, q_lens, k_lens), q.get_device()
-    kv = (s.batch, s.kv_heads, s.k_len, s.head_dim)
+    s, t, qs, kv, index = _shape(q, k, causal, window, scale, q_lens, k_lens)
     if out is None:
-        out = dict(out=torch.empty_like(q), lse=torch.empty(q.shape[:3], dtype=torch.float32, device=index))
+        out = dict(out=torch.empty_like(q), lse=torch.empty(qs[:3], dtype=torch.float32, device=index))
     ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_FORWARD, s), index)
-    rc = lib.lap_attention(s, _rows(q, "q", q, q.shape), _rows(k, "k", q, kv), _rows(v, "v", q, kv),
-                           _rows(out["out"], "out", q, q.shape), _plain(out["lse"], "lse", torch.float32, q.shape[:3], index),
+    rc = lib.lap_attention(s, _rows(q, "q", t, qs, index), _rows(k, "k", t, kv, index), _rows(v, "v", t, kv, index),
+                           _rows(out["out"], "out", t, qs, index), _plain(out["lse"], "lse", torch.float32, qs[:3], index),
                            at, have, _stream(index))
     if rc or sync:
         _done(rc, "lap_attention", index, sync)
@@ -160,15 +162,15 @@ def attention_grad(dout, q, k, v, out, lse, *, causal: bool = False, window: int
     """lap_attention_grad: returns dict(dq, dk, dv); out and lse are attention's, the other arguments as there.  grads takes
     result tensors that the caller owns."""
     lib = _lib()
-    s, index = _shape(q, k, causal, window, scale, q_lens, k_lens), q.get_device()
-    kv = (s.batch, s.kv_heads, s.k_len, s.head_dim)
+    s, t, qs, kv, index = _shape(q, k, causal, window, scale, q_lens, k_lens)
     if grads is None:
-        grads = dict(dq=torch.empty_like(q), dk=torch.empty(kv, dtype=q.dtype, device=index),
-                     dv=torch.empty(kv, dtype=q.dtype, device=index))
+        grads = dict(dq=torch.empty_like(q), dk=torch.empty(kv, dtype=t, device=index),
+                     dv=torch.empty(kv, dtype=t, device=index))
     ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_GRAD, s), index)
-    rc = lib.lap_attention_grad(s, _rows(dout, "dout", q, q.shape), _rows(q, "q", q, q.shape), _rows(k, "k", q, kv), _rows(v, "v", q, kv),
-                                _rows(out, "out", q, q.shape), _plain(lse, "lse", torch.float32, q.shape[:3], index),
-                                _rows(grads["dq"], "dq", q, q.shape), _rows(grads["dk"], "dk", q, kv), _rows(grads["dv"], "dv", q, kv),
+    rc = lib.lap_attention_grad(s, _rows(dout, "dout", t, qs, index), _rows(q, "q", t, qs, index), _rows(k, "k", t, kv, index),
+                                _rows(v, "v", t, kv, index), _rows(out, "out", t, qs, index),
+                                _plain(lse, "lse", torch.float32, qs[:3], index), _rows(grads["dq"], "dq", t, qs, index),
+                                _rows(grads["dk"], "dk", t, kv, index), _rows(grads["dv"], "dv", t, kv, index),
                                 at, have, _stream(index))
     if rc or sync:
         _done(rc, "lap_attention_grad", index, sync)
@@ -179,13 +181,13 @@ def attention_weights(q, k, lse, *, before=None, causal: bool = False, window: i
                       k_lens=None, weights=None, ws=None, sync: bool = True):
     """lap_attention_weights: returns dict(weights [batch, kv_heads, k_len]) = before (None: zeros) + what the keys receive."""
     lib = _lib()
-    s, index = _shape(q, k, causal, window, scale, q_lens, k_lens), q.get_device()
-    kv = (s.batch, s.kv_heads, s.k_len)
+    s, t, qs, ks, index = _shape(q, k, causal, window, scale, q_lens, k_lens)
+    kv = ks[:3]
     if weights is None:
         weights = torch.empty(kv, dtype=torch.float32, device=index)
     ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_WEIGHTS, s), index)
-    rc = lib.lap_attention_weights(s, _rows(q, "q", q, q.shape), _rows(k, "k", q, kv + (s.head_dim,)),
-                                   _plain(lse, "lse", torch.float32, q.shape[:3], index), _plain(before, "before", torch.float32, kv, index),
+    rc = lib.lap_attention_weights(s, _rows(q, "q", t, qs, index), _rows(k, "k", t, ks, index),
+                                   _plain(lse, "lse", torch.float32, qs[:3], index), _plain(before, "before", torch.float32, kv, index),
                                    _plain(weights, "weights", torch.float32, kv, index), at, have, _stream(index))
     if rc or sync:
         _done(rc, "lap_attention_weights", index, sync)
@@ -200,19 +202,19 @@ def attention_step(q, k_cache, v_cache, weights=None, *, lens=None, positions=No
     lib = _lib()
     if q.dim() != 3:
         _refuse("q", q, "[batch, heads, head_dim]")
-    b, h, d = q.shape
-    _four(k_cache, "k_cache")
-    index = q.get_device()
-    slots = (b, k_cache.shape[1], k_cache.shape[2])
-    s = _Shape(_type(q, "q"), b, h, slots[1], 1, slots[2], d, 0, 0, _scale(scale, d), None,
-               _plain(lens, "lens", torch.int32, (b,), index))
+    qs, ks = q.shape, _four(k_cache, "k_cache")
+    b, h, d = qs
+    _, kv, n, _ = ks
+    kind, t, index = _type(q, "q"), q.dtype, q.get_device()
+    slots, kv = (b, kv, n), (b, kv, n, d)
+    s = _Shape(kind, b, h, kv[1], 1, n, d, 0, 0, _scale(scale, d), None, _plain(lens, "lens", torch.int32, (b,), index))
     if out is None:
         out = dict(out=torch.empty_like(q), lse=torch.empty((b, h), dtype=torch.float32, device=index),
                    weights=None if weights is None else torch.empty(slots, dtype=torch.float32, device=index))
     ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_STEP, s), index)
-    rc = lib.lap_attention_step(s, _rows(q, "q", q, q.shape), _rows(k_cache, "k_cache", q, slots + (d,)), _rows(v_cache, "v_cache", q, slots + (d,)),
+    rc = lib.lap_attention_step(s, _rows(q, "q", t, qs, index), _rows(k_cache, "k_cache", t, kv, index), _rows(v_cache, "v_cache", t, kv, index),
                                 _plain(positions, "positions", torch.int32, slots, index), _plain(weights, "weights", torch.float32, slots, index),
-                                _rows(out["out"], "out", q, q.shape), _plain(out["lse"], "lse", torch.float32, (b, h), index),
+                                _rows(out["out"], "out", t, qs, index), _plain(out["lse"], "lse", torch.float32, (b, h), index),
                                 _plain(out.get("weights"), "out weights", torch.float32, slots, index), at, have, _stream(index))
     if rc or sync:
         _done(rc, "lap_attention_step", index, sync)
@@ -220,9 +222,9 @@ def attention_step(q, k_cache, v_cache, weights=None, *, lens=None, positions=No
 
 
 def _cache(k, v, weights, positions, name: str = ""):
-    b, h, n, d = _four(k, name + "k")
-    kind, index = _type(k, name + "k"), k.get_device()
-    return _Cache(kind, b, h, n, d, _rows(k, name + "k", k, k.shape), _rows(v, name + "v", k, k.shape),
+    b, h, n, d = shape = _four(k, name + "k")
+    kind, t, index = _type(k, name + "k"), k.dtype, k.get_device()
+    return _Cache(kind, b, h, n, d, _rows(k, name + "k", t, shape, index), _rows(v, name + "v", t, shape, index),
                   _plain(weights, name + "weights", torch.float32, (b, h, n), index),
                   _plain(positions, name + "positions", torch.int32, (b, h, n), index))
 
@@ -264,7 +266,7 @@ def cache_insert(k_new, v_new, k_cache, v_cache, weights, positions, position, r
     index = k_cache.get_device()
     if slots is None:
         slots = torch.empty((b, h), dtype=torch.int32, device=index)
-    rc = lib.lap_cache_insert(cache, _rows(k_new, "k_new", k_cache, (b, h, d)), _rows(v_new, "v_new", k_cache, (b, h, d)),
+    rc = lib.lap_cache_insert(cache, _rows(k_new, "k_new", k_cache.dtype, (b, h, d), index), _rows(v_new, "v_new", k_cache.dtype, (b, h, d), index),
                               _plain(position, "position", torch.int32, (b,), index), int(recent),
                               _plain(slots, "slots", torch.int32, (b, h), index), _stream(index))
     if rc or sync:
