@@ -10,6 +10,8 @@ ValueError here; the rest is LapError from the library.
 from __future__ import annotations
 
 import ctypes as C
+import struct
+from types import SimpleNamespace
 from typing import Optional
 
 from . import binding
@@ -34,30 +36,46 @@ class _Cache(C.Structure):
 
 torch = None      # set when the library is loaded, which loads torch first
 
+# The same structures as bytes, which a call's arguments are put together from: that and its checks are what the smallest
+# calls take longest for, and a ctypes object is twice as long in the making.
+_pack_rows = struct.Struct("@P3q").pack
+_pack_shape = struct.Struct("@9If2P").pack
+_pack_cache = struct.Struct("@5I4x").pack
+_pack_two = struct.Struct("@2P").pack
+_NOWHERE = _pack_rows(0, 0, 0, 0)
+assert len(_NOWHERE) == C.sizeof(_Rows) and len(_pack_shape(*[0] * 12)) == C.sizeof(_Shape)
+assert len(_pack_cache(*[0] * 5) + 2 * _NOWHERE + _pack_two(0, 0)) == C.sizeof(_Cache)
+
+_calls = SimpleNamespace()      # the library's calls, which take those bytes
+
 
 def declare(lib) -> None:
-    global torch, _stream
+    global torch, _stream, _kinds
     import torch
+    _kinds = {torch.bfloat16: 0, torch.float16: 1}
     # the handle alone, where torch has a call for it: a stream object takes 2 us to make
     _stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
-    p, rows, shape, cache = C.c_void_p, C.POINTER(_Rows), C.POINTER(_Shape), C.POINTER(_Cache)
-    ws = [p, C.c_size_t, p]
-    lib.lap_attention_workspace_bytes.restype = C.c_size_t
-    lib.lap_attention_workspace_bytes.argtypes = [C.c_int, shape]
-    lib.lap_cache_workspace_bytes.restype = C.c_size_t
-    lib.lap_cache_workspace_bytes.argtypes = [cache]
-    for name, args in (("lap_attention", [shape, rows, rows, rows, rows, p] + ws),
-                       ("lap_attention_grad", [shape] + [rows] * 5 + [p] + [rows] * 3 + ws),
-                       ("lap_attention_weights", [shape, rows, rows, p, p, p] + ws),
-                       ("lap_attention_step", [shape, rows, rows, rows, p, p, rows, p, p] + ws),
-                       ("lap_cache_evict", [cache, p, C.c_uint32, C.c_uint32, cache, p] + ws),
-                       ("lap_cache_insert", [cache, rows, rows, p, C.c_uint32, p, p])):
-        getattr(lib, name).restype = C.c_int
-        getattr(lib, name).argtypes = args
+    p, u32, size, rows, shape, cache = C.c_void_p, C.c_uint32, C.c_size_t, C.POINTER(_Rows), C.POINTER(_Shape), C.POINTER(_Cache)
+    ws = [p, size, p]
+    for name, result, args in (("lap_attention_workspace_bytes", size, [C.c_int, shape]),
+                               ("lap_cache_workspace_bytes", size, [cache]),
+                               ("lap_attention", C.c_int, [shape, rows, rows, rows, rows, p] + ws),
+                               ("lap_attention_grad", C.c_int, [shape] + [rows] * 5 + [p] + [rows] * 3 + ws),
+                               ("lap_attention_weights", C.c_int, [shape, rows, rows, p, p, p] + ws),
+                               ("lap_attention_step", C.c_int, [shape, rows, rows, rows, p, p, rows, p, p] + ws),
+                               ("lap_cache_evict", C.c_int, [cache, p, u32, u32, cache, p] + ws),
+                               ("lap_cache_insert", C.c_int, [cache, rows, rows, p, u32, p, p])):
+        call = getattr(lib, name)
+        call.restype, call.argtypes = result, args
+        call = lib[name]
+        call.restype, call.argtypes = result, [p if x in (rows, shape, cache) else x for x in args]
+        setattr(_calls, name, call)
 
 
 def _lib():
-    return binding._lib or binding.load_library()
+    if binding._lib is None:
+        binding.load_library()
+    return _calls
 
 
 def _done(rc: int, where: str, index: int, sync: bool) -> None:
@@ -81,7 +99,7 @@ def _rows(x, name: str, dtype, shape, index: int):
     st = x.stride()
     if st[-1] != 1 and x.numel():
         _refuse(name, x, "the elements of a row side by side")
-    return _Rows(x.data_ptr(), st[0], st[1], st[2] if len(st) == 4 else 0)
+    return _pack_rows(x.data_ptr(), st[0], st[1], st[2] if len(st) == 4 else 0)
 
 
 def _plain(x, name: str, dtype, shape, index: int):
@@ -93,26 +111,32 @@ def _plain(x, name: str, dtype, shape, index: int):
     return x.data_ptr()
 
 
-def _type(x, name: str) -> int:
-    if x.dtype is torch.bfloat16:
-        kind = 0
-    elif x.dtype is torch.float16:
-        kind = 1
-    else:
+def _type(x, name: str):
+    """lap's number for x's type, the type, the GPU."""
+    t, index = x.dtype, x.get_device()
+    kind = _kinds.get(t)
+    if kind is None:
         _refuse(name, x, "torch.bfloat16 or torch.float16")
-    if not x.is_cuda:
+    if index < 0:
         _refuse(name, x, "a tensor on the GPU")
-    return kind
+    return kind, t, index
 
 
 def _four(x, name: str):
-    if x.dim() != 4:
+    shape = x.shape
+    if len(shape) != 4:
         _refuse(name, x, "[batch, heads, length, head_dim]")
-    return x.shape
+    return shape
+
+
+def _count(x, name: str) -> int:
+    if not 0 <= x <= 0xFFFFFFFF:      # what the library takes; its own limits are lower
+        raise ValueError(f"{name} is a number of keys or slots, not {x}")
+    return int(x)
 
 
 def _scale(scale: Optional[float], d: int) -> float:
-    return float(scale) if scale is not None else d ** -0.5 if d else 0.0
+    return C.c_float(scale).value if scale is not None else d ** -0.5 if d else 0.0
 
 
 def _shape(q, k, causal, window, scale, q_lens, k_lens):
@@ -120,22 +144,19 @@ def _shape(q, k, causal, window, scale, q_lens, k_lens):
     qs, ks = _four(q, "q"), _four(k, "k")
     b, h, n, d = qs
     _, kv, m, _ = ks
-    kind, index = _type(q, "q"), q.get_device()
-    if window < 0:
-        raise ValueError("window is 0 (none) or a number of keys")
-    i32 = torch.int32
-    s = _Shape(kind, b, h, kv, n, m, d, 1 if causal else 0, window, _scale(scale, d),
-               None if q_lens is None else _plain(q_lens, "q_lens", i32, (b,), index),
-               None if k_lens is None else _plain(k_lens, "k_lens", i32, (b,), index))
-    return s, q.dtype, qs, (b, kv, m, d), index
+    kind, t, index = _type(q, "q")
+    s = _pack_shape(kind, b, h, kv, n, m, d, 1 if causal else 0, _count(window, "window") if window else 0, _scale(scale, d),
+                    0 if q_lens is None else _plain(q_lens, "q_lens", torch.int32, (b,), index),
+                    0 if k_lens is None else _plain(k_lens, "k_lens", torch.int32, (b,), index))
+    return s, t, qs, (b, kv, m, d), index
 
 
-def _workspace(ws, need: int, index: int):
+def _workspace(ws, need: int, index: int, like):
     """The workspace, its size and its address."""
     if ws is None:
         if not need:
             return None, 0, None
-        ws = torch.empty(need, dtype=torch.uint8, device=index)
+        ws = like.new_empty(need, dtype=torch.uint8)
     elif ws.dtype is not torch.uint8 or ws.get_device() != index or not ws.is_contiguous():
         _refuse("ws", ws, f"a contiguous torch.uint8 on GPU {index}")
     return ws, ws.numel(), ws.data_ptr()
@@ -147,8 +168,8 @@ def attention(q, k, v, *, causal: bool = False, window: int = 0, scale: Optional
     lib = _lib()
     s, t, qs, kv, index = _shape(q, k, causal, window, scale, q_lens, k_lens)
     if out is None:
-        out = dict(out=torch.empty_like(q), lse=torch.empty(qs[:3], dtype=torch.float32, device=index))
-    ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_FORWARD, s), index)
+        out = dict(out=torch.empty_like(q), lse=q.new_empty(qs[:3], dtype=torch.float32))
+    ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_FORWARD, s), index, q)
     rc = lib.lap_attention(s, _rows(q, "q", t, qs, index), _rows(k, "k", t, kv, index), _rows(v, "v", t, kv, index),
                            _rows(out["out"], "out", t, qs, index), _plain(out["lse"], "lse", torch.float32, qs[:3], index),
                            at, have, _stream(index))
@@ -164,9 +185,8 @@ def attention_grad(dout, q, k, v, out, lse, *, causal: bool = False, window: int
     lib = _lib()
     s, t, qs, kv, index = _shape(q, k, causal, window, scale, q_lens, k_lens)
     if grads is None:
-        grads = dict(dq=torch.empty_like(q), dk=torch.empty(kv, dtype=t, device=index),
-                     dv=torch.empty(kv, dtype=t, device=index))
-    ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_GRAD, s), index)
+        grads = dict(dq=torch.empty_like(q), dk=q.new_empty(kv), dv=q.new_empty(kv))
+    ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_GRAD, s), index, q)
     rc = lib.lap_attention_grad(s, _rows(dout, "dout", t, qs, index), _rows(q, "q", t, qs, index), _rows(k, "k", t, kv, index),
                                 _rows(v, "v", t, kv, index), _rows(out, "out", t, qs, index),
                                 _plain(lse, "lse", torch.float32, qs[:3], index), _rows(grads["dq"], "dq", t, qs, index),
@@ -184,8 +204,8 @@ def attention_weights(q, k, lse, *, before=None, causal: bool = False, window: i
     s, t, qs, ks, index = _shape(q, k, causal, window, scale, q_lens, k_lens)
     kv = ks[:3]
     if weights is None:
-        weights = torch.empty(kv, dtype=torch.float32, device=index)
-    ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_WEIGHTS, s), index)
+        weights = q.new_empty(kv, dtype=torch.float32)
+    ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_WEIGHTS, s), index, q)
     rc = lib.lap_attention_weights(s, _rows(q, "q", t, qs, index), _rows(k, "k", t, ks, index),
                                    _plain(lse, "lse", torch.float32, qs[:3], index), _plain(before, "before", torch.float32, kv, index),
                                    _plain(weights, "weights", torch.float32, kv, index), at, have, _stream(index))
@@ -205,13 +225,13 @@ def attention_step(q, k_cache, v_cache, weights=None, *, lens=None, positions=No
     qs, ks = q.shape, _four(k_cache, "k_cache")
     b, h, d = qs
     _, kv, n, _ = ks
-    kind, t, index = _type(q, "q"), q.dtype, q.get_device()
+    kind, t, index = _type(q, "q")
+    s = _pack_shape(kind, b, h, kv, 1, n, d, 0, 0, _scale(scale, d), 0, _plain(lens, "lens", torch.int32, (b,), index) or 0)
     slots, kv = (b, kv, n), (b, kv, n, d)
-    s = _Shape(kind, b, h, kv[1], 1, n, d, 0, 0, _scale(scale, d), None, _plain(lens, "lens", torch.int32, (b,), index))
     if out is None:
-        out = dict(out=torch.empty_like(q), lse=torch.empty((b, h), dtype=torch.float32, device=index),
-                   weights=None if weights is None else torch.empty(slots, dtype=torch.float32, device=index))
-    ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_STEP, s), index)
+        out = dict(out=torch.empty_like(q), lse=q.new_empty((b, h), dtype=torch.float32),
+                   weights=None if weights is None else q.new_empty(slots, dtype=torch.float32))
+    ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_STEP, s), index, q)
     rc = lib.lap_attention_step(s, _rows(q, "q", t, qs, index), _rows(k_cache, "k_cache", t, kv, index), _rows(v_cache, "v_cache", t, kv, index),
                                 _plain(positions, "positions", torch.int32, slots, index), _plain(weights, "weights", torch.float32, slots, index),
                                 _rows(out["out"], "out", t, qs, index), _plain(out["lse"], "lse", torch.float32, (b, h), index),
@@ -223,10 +243,11 @@ def attention_step(q, k_cache, v_cache, weights=None, *, lens=None, positions=No
 
 def _cache(k, v, weights, positions, name: str = ""):
     b, h, n, d = shape = _four(k, name + "k")
-    kind, t, index = _type(k, name + "k"), k.dtype, k.get_device()
-    return _Cache(kind, b, h, n, d, _rows(k, name + "k", t, shape, index), _rows(v, name + "v", t, shape, index),
-                  _plain(weights, name + "weights", torch.float32, (b, h, n), index),
-                  _plain(positions, name + "positions", torch.int32, (b, h, n), index))
+    kind, t, index = _type(k, name + "k")
+    slots = (b, h, n)
+    return (_pack_cache(kind, b, h, n, d) + _rows(k, name + "k", t, shape, index) + _rows(v, name + "v", t, shape, index)
+            + _pack_two(_plain(weights, name + "weights", torch.float32, slots, index) or 0,
+                        _plain(positions, name + "positions", torch.int32, slots, index) or 0))
 
 
 def cache_evict(k, v, weights, keep: int, recent: int, *, lens=None, positions=None, slots: Optional[int] = None,
@@ -235,20 +256,18 @@ def cache_evict(k, v, weights, keep: int, recent: int, *, lens=None, positions=N
     (None: keep).  Returns dict(k, v, weights, positions [batch, kv_heads, slots], lens [batch])."""
     lib = _lib()
     src = _cache(k, v, weights, positions)
-    if keep < 0 or recent < 0:
-        raise ValueError("keep and recent are numbers of slots")
+    keep, recent = _count(keep, "keep"), _count(recent, "recent")
     b, h, n, d = k.shape
     index = k.get_device()
     if out is None:
-        m = int(keep if slots is None else slots)
-        out = dict(k=torch.empty((b, h, m, d), dtype=k.dtype, device=index), v=torch.empty((b, h, m, d), dtype=k.dtype, device=index),
-                   weights=torch.empty((b, h, m), dtype=torch.float32, device=index),
-                   positions=torch.empty((b, h, m), dtype=torch.int32, device=index), lens=torch.empty(b, dtype=torch.int32, device=index))
+        m = keep if slots is None else int(slots)
+        out = dict(k=k.new_empty((b, h, m, d)), v=k.new_empty((b, h, m, d)), weights=k.new_empty((b, h, m), dtype=torch.float32),
+                   positions=k.new_empty((b, h, m), dtype=torch.int32), lens=k.new_empty(b, dtype=torch.int32))
     if out["k"].dtype is not k.dtype or out["k"].get_device() != index:
         _refuse("out k", out["k"], f"{k.dtype} on GPU {index}")
     dst = _cache(out["k"], out["v"], out["weights"], out["positions"], "out ")
-    ws, have, at = _workspace(ws, lib.lap_cache_workspace_bytes(dst), index)
-    rc = lib.lap_cache_evict(src, _plain(lens, "lens", torch.int32, (b,), index), int(keep), int(recent), dst,
+    ws, have, at = _workspace(ws, lib.lap_cache_workspace_bytes(dst), index, k)
+    rc = lib.lap_cache_evict(src, _plain(lens, "lens", torch.int32, (b,), index), keep, recent, dst,
                              _plain(out["lens"], "out lens", torch.int32, (b,), index), at, have, _stream(index))
     if rc or sync:
         _done(rc, "lap_cache_evict", index, sync)
@@ -260,14 +279,12 @@ def cache_insert(k_new, v_new, k_cache, v_cache, weights, positions, position, r
     Returns dict(slots [batch, kv_heads]): where it went."""
     lib = _lib()
     cache = _cache(k_cache, v_cache, weights, positions)
-    if recent < 0:
-        raise ValueError("recent is a number of slots")
     b, h, _, d = k_cache.shape
     index = k_cache.get_device()
     if slots is None:
-        slots = torch.empty((b, h), dtype=torch.int32, device=index)
+        slots = k_cache.new_empty((b, h), dtype=torch.int32)
     rc = lib.lap_cache_insert(cache, _rows(k_new, "k_new", k_cache.dtype, (b, h, d), index), _rows(v_new, "v_new", k_cache.dtype, (b, h, d), index),
-                              _plain(position, "position", torch.int32, (b,), index), int(recent),
+                              _plain(position, "position", torch.int32, (b,), index), _count(recent, "recent"),
                               _plain(slots, "slots", torch.int32, (b, h), index), _stream(index))
     if rc or sync:
         _done(rc, "lap_cache_insert", index, sync)
