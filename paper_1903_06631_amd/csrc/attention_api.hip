@@ -68,7 +68,7 @@ lap::Rows rows_of(const lap_rows *x) { return {x->data, x->batch, x->head, x->ro
 
 lap::StepShape step_of(const lap_attention_shape *s)
 {
-    lap::StepShape p = {s->batch, s->q_heads, s->kv_heads, s->k_len, s->head_dim, s->scale, s->k_lens, s->type == LAP_T_F16, 0, 0, 0};
+    lap::StepShape p = {s->batch, s->q_heads, s->kv_heads, s->k_len, s->head_dim, s->scale, s->k_lens, s->type == LAP_T_F16, 0, 0, 0, false};
     lap::step_split(p);
     return p;
 }
@@ -85,7 +85,7 @@ size_t ws_step(const lap_attention_shape *s)
 {
     const lap::StepShape p = step_of(s);
     const size_t heads = (size_t)s->batch * s->q_heads;
-    return up(heads * p.splits * padded_dim(s) * 4) + up(heads * p.splits * sizeof(float2)) + up(heads * p.score_row * 4);
+    return p.whole ? up(heads * p.score_row * 4) : up(heads * p.splits * padded_dim(s) * 4) + up(heads * p.splits * sizeof(float2)) + up(heads * p.score_row * 4);
 }
 
 int check_cache(const lap_cache *c, bool output)
@@ -184,11 +184,13 @@ int lap_attention_step(const lap_attention_shape *s, const lap_rows *q, const la
     if (rc) return rc;
     const lap::StepShape p = step_of(s);
     const size_t heads = (size_t)s->batch * s->q_heads;
-    char *at = (char *)ws;
     lap::StepWork w = {rows_of(q), rows_of(k), rows_of(v), rows_of(out), positions, before, lse, weights, nullptr, nullptr, nullptr};
-    w.outs = (float *)at, at += up(heads * p.splits * padded_dim(s) * 4);
-    w.sums = (float2 *)at, at += up(heads * p.splits * sizeof(float2));
-    w.scores = weights ? (float *)at : nullptr;
+    char *at = (char *)ws;
+    if (!p.whole) {
+        w.outs = (float *)at, at += up(heads * p.splits * padded_dim(s) * 4);
+        w.sums = (float2 *)at, at += up(heads * p.splits * sizeof(float2));
+    }
+    w.scores = (float *)at;
     LAP_HIP(lap::launch_attention_step(p, w, (hipStream_t)hip_stream));
     return LAP_OK;
 }

@@ -1,26 +1,41 @@
 // Attention of one new token of every sequence over its cache, and the weight that every slot receives from it:
 //   o = sum_j p_j v_j, p_j = exp(scale q.k_j - lse), over the slots in use; w_j += sum of p_j over the heads that share slot j
 //
-// Every key and value is read once and takes part in a few products only: the pass is bound by memory, and there are few
-// sequences and heads to share it out to.  So the slots are cut into chunks of up to 512, a workgroup each.  Its four
-// waves go through 32 slots at a time of their own, without waiting for each other: keys from memory straight into
-// registers as a matrix operand, values through LDS, which is where they are transposed.  The heads of a group are the
-// kept rows (up to 32; with fewer, part of the matrix instructions runs empty, at a rate that is far from binding).  A
-// second kernel joins the chunks' sums and outputs; the weights need the joined sums, so the first one leaves the scores
-// (4 bytes for each slot and head beside the slot's 4 head_dim).  Measured: 2 caches of 8 heads x 131072 slots x 128, 4 query heads
-// each, 216 + 16 us, the first kernel at 5.1 TB/s (a copy of 2 GiB: 4.9); 64 ragged caches of up to 4096 slots 123 + 12 us; one
-// of 16 heads x 1000 slots 6.2 + 3.5 us.
+// Every key and value is read once and takes part in a few products only: the pass is bound by memory.  Waves go through 32
+// slots at a time of their own, without waiting for each other: keys from memory straight into registers as a matrix operand,
+// values through LDS, which is where they are transposed.  The heads of a group are the kept rows (up to 32; with fewer,
+// part of the matrix instructions runs empty, at a rate that is far from binding).  Few long caches are cut into chunks of up to
+// 512 slots, a workgroup of four waves each, and a second kernel joins their sums and outputs; the weights need the joined
+// sums, so the first one leaves the scores (4 bytes for each slot and head beside the slot's 4 head_dim).  Short ones, and many, have
+// a workgroup of eight waves each, which adds the weights too: one launch, and nothing to join.
+//
+// Measured: 2 caches of 8 heads x 131072 slots x 128, 4 query heads each, 216 + 16 us, the first kernel at 5.1 TB/s (a copy of
+// 2 GiB: 4.9); 64 ragged caches of 8 heads x up to 4096 slots 128 us in a workgroup each (in chunks 123 + 12); one of 16
+// heads x 1000 slots 14 us, a launch and a chain of four tiles a wave.
 #include "attn_core.h"
 
 namespace lap {
 namespace {
 
-constexpr int NW = 4, TS = 32;      // waves, slots of a wave's tile
+constexpr int TS = 32;                      // slots of a wave's tile
+constexpr uint32_t CHUNK_WAVES = 4;         // waves of a chunk's workgroup
+constexpr uint32_t WHOLE_WAVES = 8;         // and of one that goes through a whole cache
+constexpr uint32_t WHOLE_SCORES = 6144;     // scores that the latter keeps in LDS
 
-template <class T, int DP>
+// floats from one head's scores to the next's there
+__host__ __device__ __forceinline__ uint32_t score_pitch(uint32_t slots) { return (slots + TS - 1) / TS * TS + 4; }
+
+// CHUNK: one of several workgroups of a cache, to be joined.  Or the only one, of up to 32 heads, with its scores in the
+// workspace (WHOLE) or in LDS.
+enum class Form { CHUNK, WHOLE, WHOLE_IN_LDS };
+
+template <class T, int DP, int NW, Form FORM>
 __global__ __launch_bounds__(NW * 64, 2) void k_step(StepShape s, StepWork w)
 {
+    constexpr bool WHOLE = FORM != Form::CHUNK, IN_LDS = FORM == Form::WHOLE_IN_LDS;
     constexpr int TILE = Tile<DP>::size(TS);
+    __shared__ __align__(16) float kept[IN_LDS ? WHOLE_SCORES : 4];
+    __shared__ float l2[32], totals[32];      // of a row: logarithm to base 2 of the whole sum, the sum on the maximum
     __shared__ __align__(16) char raw[NW * 2 * TILE * sizeof(T)];      // the waves' values; their outputs at the end
     __shared__ float2 sums[NW][32];
     T *const lv = (T *)raw;
@@ -44,7 +59,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_step(StepShape s, StepWork w)
     const T *gk = (const T *)w.k.data + (int64_t)b * w.k.batch + (int64_t)kvh * w.k.head;
     const T *gv = (const T *)w.v.data + (int64_t)b * w.v.batch + (int64_t)kvh * w.v.head;
     const int32_t *pos = w.positions ? w.positions + ((int64_t)b * s.kv_heads + kvh) * s.slots : nullptr;
-    float *scores = w.scores ? w.scores + ((int64_t)b * s.q_heads + head0 + r) * s.score_row : nullptr;
+    float *const scores = w.scores + ((int64_t)b * s.q_heads + head0 + r) * s.score_row;      // of the lane's head
+    const uint32_t pitch = score_pitch(s.slots);
     const float c = s.scale * LOG2E;
     const ColRead<DP, T> cols(lane);
     const TileLoad<DP, TS, 1> tv(w.v.row, (int)s.head_dim / 8 - 1, 0, lane);
@@ -79,9 +95,10 @@ __global__ __launch_bounds__(NW * 64, 2) void k_step(StepShape s, StepWork w)
                     if (!((live >> (n / (DP / 8))) & 1)) *(s16x8 *)(mine + buf * TILE + Tile<DP>::place(n / (DP / 8), n % (DP / 8))) = s16x8{};
             }
         }
-        if (scores && r < n_rows) {
+        if (w.weights && r < n_rows) {
+            float *const to = IN_LDS ? kept + r * pitch : scores;
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) *(f32x4 *)(scores + at + 2 * i + 4 * h) = f32x4{p[i], p[i + 1], p[i + 2], p[i + 3]};
+            for (int i = 0; i < 16; i += 4) *(f32x4 *)(to + at + 2 * i + 4 * h) = f32x4{p[i], p[i + 1], p[i + 2], p[i + 3]};
         }
         float top = p[0];
 #pragma unroll
@@ -127,17 +144,42 @@ __global__ __launch_bounds__(NW * 64, 2) void k_step(StepShape s, StepWork w)
                 for (int j = 0; j < 4; ++j) y[j] = acc[d][i + j] * by;
                 *(f32x4 *)(out + (r * NW + wave) * DP + 32 * d + 2 * i + 4 * h) = y;
             }
+    float total = 0.f;      // of row r
+    for (int i = 0; i < NW; ++i) total += sums[i][r].y * exp2_fast(sums[i][r].x - top);
+    const bool some = total != 0.f;
+    if (wave == 0 && lane < n_rows) {
+        if constexpr (WHOLE) {
+            w.lse[(int64_t)b * s.q_heads + head0 + r] = some ? top * LN2 + __logf(total) : -ATTN_INF;
+            l2[r] = some ? top + __log2f(total) : ATTN_INF;
+            totals[r] = total;
+        } else {
+            w.sums[((int64_t)b * s.q_heads + head0 + r) * s.splits + split] = make_float2(top, total);
+        }
+    }
     __syncthreads();
     for (int n = threadIdx.x; n < n_rows * (DP / 4); n += NW * 64) {
         const int row = n / (DP / 4), e = n % (DP / 4) * 4;
         f32x4 y = *(f32x4 *)(out + row * NW * DP + e);
         for (int i = 1; i < NW; ++i) y += *(f32x4 *)(out + (row * NW + i) * DP + e);
-        *(f32x4 *)(w.outs + (((int64_t)b * s.q_heads + head0 + row) * s.splits + split) * DP + e) = y;
+        if constexpr (WHOLE) {
+            typename Elem<T>::x4 z;
+            for (int j = 0; j < 4; ++j) z[j] = (T)(totals[row] != 0.f ? y[j] / totals[row] : 0.f);
+            if (e < (int)s.head_dim) *(typename Elem<T>::x4 *)((T *)w.out.data + (int64_t)b * w.out.batch + (int64_t)(head0 + row) * w.out.head + e) = z;
+        } else {
+            *(f32x4 *)(w.outs + (((int64_t)b * s.q_heads + head0 + row) * s.splits + split) * DP + e) = y;
+        }
     }
-    if (wave == 0 && lane < n_rows) {
-        float total = 0.f;
-        for (int i = 0; i < NW; ++i) total += sums[i][lane].y * exp2_fast(sums[i][lane].x - top);
-        w.sums[((int64_t)b * s.q_heads + head0 + lane) * s.splits + split] = make_float2(top, total);
+    if constexpr (WHOLE) {
+        if (!w.weights) return;
+        const float *const all = w.scores + ((int64_t)b * s.q_heads + head0) * s.score_row;
+        for (uint32_t slot = threadIdx.x; slot < s.slots; slot += NW * 64) {
+            float sum = 0.f;
+            if ((int)slot < len)
+                for (int g = 0; g < n_rows; ++g)
+                    sum += exp2_fast((IN_LDS ? kept[g * pitch + slot] : all[(int64_t)g * s.score_row + slot]) - l2[g]);
+            const int64_t to = ((int64_t)b * s.kv_heads + kvh) * s.slots + slot;
+            w.weights[to] = w.before[to] + sum;
+        }
     }
 }
 
@@ -226,7 +268,13 @@ template <class T, int DP> __global__ __launch_bounds__(JOIN) void k_step_join(S
 template <class T, int DP> hipError_t launch(const StepShape &s, const StepWork &w, hipStream_t st)
 {
     const uint32_t parts = (s.q_heads / s.kv_heads + 31) / 32;
-    k_step<T, DP><<<s.splits * parts * s.batch * s.kv_heads, NW * 64, 0, st>>>(s, w);
+    if (s.whole) {
+        const uint32_t grid = s.batch * s.kv_heads;
+        if (s.score_row) k_step<T, DP, WHOLE_WAVES, Form::WHOLE><<<grid, WHOLE_WAVES * 64, 0, st>>>(s, w);
+        else k_step<T, DP, WHOLE_WAVES, Form::WHOLE_IN_LDS><<<grid, WHOLE_WAVES * 64, 0, st>>>(s, w);
+        return hipGetLastError();
+    }
+    k_step<T, DP, CHUNK_WAVES, Form::CHUNK><<<s.splits * parts * s.batch * s.kv_heads, CHUNK_WAVES * 64, 0, st>>>(s, w);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const uint32_t pieces = w.weights ? (s.slots + JOIN_SLOTS - 1) / JOIN_SLOTS : 0;
@@ -236,19 +284,36 @@ template <class T, int DP> hipError_t launch(const StepShape &s, const StepWork 
 
 }  // namespace
 
+// One workgroup for a cache, in us, chunks beside it (keys of 128 elements, b caches of 8 heads, lengths all equal or ragged):
+//   1 x 16 heads   500 slots 12.9 17.2, 1000 14.1 17.3, 1500 18.6 17.5      b = 16   1500 22 26, 2900 36 41, 4000 60 53
+//   b = 24         2000 33 42, 4000 81 94, 16000 363 293                    b = 36   2000 74 71 (ragged 31 43), 4000 153 123 (70 70)
+//   b = 48         2000 87 100, 4000 162 160 (87 101)                       b = 64   1000 46 56, 4000 188 210, 16000 961 931
+//   b = 96         2000 145 161, 4000 278 305, 8000 622 603                 (b = 64, ragged, 4 query heads each: 4096 128 135)
+// So up to 1024 slots always, up to 2048 where there are workgroups for half the units, up to 4096 where the last round of
+// workgroups fills three quarters of them (eight waves take up a unit's LDS).
+static bool whole_caches(uint64_t rows, uint32_t slots)
+{
+    const uint64_t rounds = (rows + 255) / 256;
+    return slots <= 1024 || (slots <= 2048 && rows >= 128) || (slots <= 4096 && rows >= 192 * rounds);
+}
+
 // Chunks: workgroups enough to keep the chip evenly loaded to the end, of a tile for each wave at least and 512 slots at
-// most (64 caches of 8 heads, up to 4096 slots: 143 us, with 1024 slots 157, with 256 and caches next to each other 142
-// in place of 135).
+// most (64 caches of 8 heads, up to 4096 slots: 135 us, with 1024 slots 157, with 256 142; with eight waves and 1024 slots 144).
 void step_split(StepShape &s)
 {
     const uint64_t rows = (uint64_t)s.batch * s.kv_heads * ((s.q_heads / s.kv_heads + 31) / 32);
-    const uint64_t least = NW * TS, most = 512;
+    const uint64_t least = CHUNK_WAVES * TS, most = 512;
     const uint64_t want = (uint64_t)s.slots * rows / 4096;
     const uint64_t chunk = (want < least ? least : want > most ? most : want) / least * least;
     s.chunk = (uint32_t)chunk;
     s.splits = (uint32_t)((s.slots + chunk - 1) / chunk);
     if (!s.splits) s.splits = 1;
     s.score_row = ((uint64_t)s.slots + TS - 1) / TS * TS;
+    const uint32_t group = s.q_heads / s.kv_heads;
+    s.whole = group <= 32 && whole_caches(rows, s.slots);
+    if (!s.whole) return;
+    s.chunk = s.slots, s.splits = 1;
+    if ((uint64_t)group * score_pitch(s.slots) <= WHOLE_SCORES) s.score_row = 0;
 }
 
 hipError_t launch_attention_step(const StepShape &s, const StepWork &w, hipStream_t st)

@@ -46,7 +46,8 @@ struct StepShape {
     const int32_t *lens;
     bool half;
     uint32_t chunk, splits;      // slots of a workgroup, workgroups of a cache (step_split)
-    uint64_t score_row;          // floats between two heads' scores
+    uint64_t score_row;          // floats between two heads' scores (0: they stay in LDS)
+    bool whole;                  // one workgroup for all of a cache, and nothing to join
 };
 struct StepWork {
     Rows q, k, v, out;      // q, out: row unused
@@ -55,7 +56,7 @@ struct StepWork {
     float *lse, *weights;
     float *outs;            // [batch, q_heads, splits, 64 or 128]
     float2 *sums;           // [batch, q_heads, splits]: maximum in base 2, sum
-    float *scores;          // [batch, q_heads, score_row] in base 2; null: no weights asked for
+    float *scores;          // [batch, q_heads, score_row] in base 2, where weights are asked for
 };
 void step_split(StepShape &s);
 hipError_t launch_attention_step(const StepShape &s, const StepWork &w, hipStream_t st);

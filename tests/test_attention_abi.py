@@ -91,7 +91,9 @@ def test_step(lib):
     assert call(shape(q_heads=514, kv_heads=2, **one)) == -2
     assert call(before=None) == -1 and call(weights=None) == -1 and call(lse=None) == -1 and call(k=rows(data=None)) == -1
     assert call(out=rows(head=0)) == -10
-    assert call(have=lib.lap_attention_workspace_bytes(3, shape(**one)) - 1) == -3
+    many = shape(k_len=3000, **one)      # few caches of many slots: in chunks, joined in a workspace
+    assert lib.lap_attention_workspace_bytes(3, shape(**one)) == 0 and lib.lap_attention_workspace_bytes(3, many) > 0
+    assert call(many, have=lib.lap_attention_workspace_bytes(3, many) - 1) == -3
 
 
 def cache(**kw):

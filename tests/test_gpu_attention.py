@@ -211,6 +211,11 @@ STEPS = [
     (BF, 64, 40, 1, 300, [300, 0, 129], True),          # more heads than a matrix operand has columns
     (HF, 128, 16, 8, 5000, [5000, 4097, 2], False),
     (BF, 128, 256, 1, 200, None, False),
+    (HF, 128, 32, 1, 1000, [1000, 31, 0, 545], True),
+    (BF, 64, 4, 2, 1024, [1024, 1023], False),
+    (HF, 64, 2, 2, 1025, [1025, 1024], True),
+    (BF, 64, 8, 8, 1500, [1500 - 90 * i for i in range(16)], False),
+    (HF, 72, 24, 24, 2100, [2100, 2047, 1, 0, 2100, 33, 999, 5], False),
 ]
 
 
