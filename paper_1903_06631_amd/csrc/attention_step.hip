@@ -172,13 +172,24 @@ __global__ __launch_bounds__(NW * 64, 2) void k_step(StepShape s, StepWork w)
     if constexpr (WHOLE) {
         if (!w.weights) return;
         const float *const all = w.scores + ((int64_t)b * s.q_heads + head0) * s.score_row;
-        for (uint32_t slot = threadIdx.x; slot < s.slots; slot += NW * 64) {
-            float sum = 0.f;
-            if ((int)slot < len)
-                for (int g = 0; g < n_rows; ++g)
-                    sum += exp2_fast((IN_LDS ? kept[g * pitch + slot] : all[(int64_t)g * s.score_row + slot]) - l2[g]);
-            const int64_t to = ((int64_t)b * s.kv_heads + kvh) * s.slots + slot;
-            w.weights[to] = w.before[to] + sum;
+        const int64_t to = ((int64_t)b * s.kv_heads + kvh) * s.slots;
+        const bool aligned = s.slots % 4 == 0 && ((uintptr_t)w.weights | (uintptr_t)w.before) % 16 == 0;
+        for (uint32_t slot = threadIdx.x * 4; slot < s.slots; slot += NW * 64 * 4) {
+            f32x4 sum = {};
+            if ((int)slot < len) {
+#pragma unroll 4
+                for (int g = 0; g < n_rows; ++g) {
+                    const f32x4 x = *(const f32x4 *)(IN_LDS ? kept + g * pitch + slot : all + (int64_t)g * s.score_row + slot);
+                    for (int j = 0; j < 4; ++j) sum[j] += exp2_fast(x[j] - l2[g]);
+                }
+                for (int j = 1; j < 4; ++j) sum[j] = (int)slot + j < len ? sum[j] : 0.f;
+            }
+            if (aligned) {
+                *(f32x4 *)(w.weights + to + slot) = *(const f32x4 *)(w.before + to + slot) + sum;
+            } else {
+                for (int j = 0; j < 4; ++j)
+                    if (slot + j < s.slots) w.weights[to + slot + j] = w.before[to + slot + j] + sum[j];
+            }
         }
     }
 }
