@@ -50,22 +50,27 @@ __device__ __forceinline__ void count(uint32_t *bins, bool counts, uint32_t bin,
     if (counts && (bin != of || lane == first)) atomicAdd(&bins[bin], bin == of ? (uint32_t)__popcll(same) : 1u);
 }
 
-// The slots that stay, ascending, into kept[]; -1 after the last.  One workgroup for each row, a stretch of it for each
-// wave, with the weights of EACH x 64 slots in registers (EACH 0: read again from the L2 cache each time).  The key of the
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+constexpr int COPY_ROWS = 4;      // rows of keys and of values that a thread has on their way
+
+// The slots that stay, ascending, and their rows of keys and values.  `pieces` workgroups for each row find the same order each,
+// write a share of the new cache's slots, and copy these; a stretch of the row for each wave, with the weights of EACH x 64 slots in registers (EACH 0: read again from the L2 cache each time).  The key of the
 // last one that stays is found digit by digit (13, 13 and 6 bits: the first one has four bits of a weight's fraction, so
 // that weights of one size do not all meet in one counter) from counts in LDS.
 template <int EACH>
-__global__ __launch_bounds__(EV) void k_evict_choose(EvictShape s, const float *weights, const int32_t *positions, int32_t *kept,
-                                                   float *weights_out, int32_t *positions_out, int32_t *lens_out)
+__global__ __launch_bounds__(EV) void k_evict(EvictShape s, Rows k, Rows v, const float *weights, const int32_t *positions, Rows k_out, Rows v_out,
+                                            int32_t *kept, float *weights_out, int32_t *positions_out, int32_t *lens_out, uint32_t pieces)
 {
     __shared__ uint32_t bins[BINS];
     __shared__ uint32_t part[EW][2];
     __shared__ uint32_t found[3];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    const uint32_t b = blockIdx.x / s.kv_heads;
+    const uint32_t rows = s.batch * s.kv_heads, at_row = blockIdx.x % rows, piece = blockIdx.x / rows;      // (the pieces of a row on one die, mostly)
+    const uint32_t b = at_row / s.kv_heads, h = at_row % s.kv_heads;
+    const uint32_t first = (uint32_t)((uint64_t)s.slots_out * piece / pieces), last = (uint32_t)((uint64_t)s.slots_out * (piece + 1) / pieces);
     EvictRow row;
-    row.weights = weights + (int64_t)blockIdx.x * s.slots;
-    row.positions = positions ? positions + (int64_t)blockIdx.x * s.slots : nullptr;
+    row.weights = weights + (int64_t)at_row * s.slots;
+    row.positions = positions ? positions + (int64_t)at_row * s.slots : nullptr;
     row.len = clamp_len(s.lens, b, s.slots);
 
     int newest = row.len - 1, used = row.len;
@@ -174,7 +179,7 @@ __global__ __launch_bounds__(EV) void k_evict_choose(EvictShape s, const float *
 #pragma unroll
     for (int i = 0; i < EW; ++i)
         if (i < wave) place += part[i][0] + min(equal - min(equal, seen), part[i][1]), seen += part[i][1];
-    const int64_t out = (int64_t)blockIdx.x * s.slots_out;
+    const int64_t out = (int64_t)at_row * s.slots_out;
     kept += out, weights_out += out, positions_out += out;
     for_all([&](int base, uint32_t k, float w) {
         const uint64_t eq = ballot(k == bound && k != EMPTY);
@@ -186,44 +191,43 @@ __global__ __launch_bounds__(EV) void k_evict_choose(EvictShape s, const float *
         const uint64_t all = ballot(stays);
         if (stays) {
             const uint32_t to = place + before_lane(all);
-            kept[to] = base + lane;
-            weights_out[to] = w;
-            positions_out[to] = positions ? row.positions[base + lane] : base + lane;
+            if (to >= first && to < last) {
+                kept[to] = base + lane;
+                weights_out[to] = w;
+                positions_out[to] = positions ? row.positions[base + lane] : base + lane;
+            }
         }
         place += __popcll(all);
     });
-    for (int i = keep + t; i < (int)s.slots_out; i += EV) {
+    for (uint32_t i = max((uint32_t)keep, first) + t; i < last; i += EV) {
         kept[i] = -1;
         weights_out[i] = 0.f;
         positions_out[i] = -1;
     }
-    if (blockIdx.x % s.kv_heads == 0 && t == 0) lens_out[b] = min((int)s.keep, row.len);
-}
+    if (h == 0 && piece == 0 && t == 0) lens_out[b] = min((int)s.keep, row.len);
+    __syncthreads();
 
-// keys and values of the slots that stay: 16 bytes for each thread, rows side by side
-constexpr int CP = 256, CP_ROWS = 4;
-__global__ __launch_bounds__(CP) void k_evict_copy(EvictShape s, Rows k, Rows v, Rows k_out, Rows v_out, const int32_t *kept)
-{
-    const uint32_t across = s.head_dim / 8, rows = CP / across;
-    const uint32_t r = threadIdx.x / across, e = threadIdx.x % across * 8;
-    if (r >= rows) return;
-    const uint32_t b = blockIdx.y / s.kv_heads, h = blockIdx.y % s.kv_heads;
+    // keys and values: 16 bytes for each thread, rows side by side
+    const uint32_t across = s.head_dim / 8, side = EV / across, r = t / across, e = t % across * 8;
+    if (r >= side) return;
     const uint16_t *gk = (const uint16_t *)k.data + (int64_t)b * k.batch + (int64_t)h * k.head + e;
     const uint16_t *gv = (const uint16_t *)v.data + (int64_t)b * v.batch + (int64_t)h * v.head + e;
     uint16_t *ok = (uint16_t *)k_out.data + (int64_t)b * k_out.batch + (int64_t)h * k_out.head + e;
     uint16_t *ov = (uint16_t *)v_out.data + (int64_t)b * v_out.batch + (int64_t)h * v_out.head + e;
+    for (uint32_t to = first + r; to < last; to += side * COPY_ROWS) {
+        u32x4 x[COPY_ROWS] = {}, y[COPY_ROWS] = {};
+        int from[COPY_ROWS];
 #pragma unroll
-    for (int i = 0; i < CP_ROWS; ++i) {
-        const uint32_t to = blockIdx.x * rows * CP_ROWS + i * rows + r;
-        if (to >= s.slots_out) continue;
-        const int from = kept[(int64_t)blockIdx.y * s.slots_out + to];
-        uint4 x = {}, y = {};
-        if (from >= 0) {
-            x = *(const uint4 *)(gk + (int64_t)from * k.row);
-            y = *(const uint4 *)(gv + (int64_t)from * v.row);
-        }
-        *(uint4 *)(ok + (int64_t)to * k_out.row) = x;
-        *(uint4 *)(ov + (int64_t)to * v_out.row) = y;
+        for (int i = 0; i < COPY_ROWS; ++i) from[i] = to + i * side < last ? kept[to + i * side] : -1;
+#pragma unroll
+        for (int i = 0; i < COPY_ROWS; ++i)
+            if (from[i] >= 0) x[i] = *(const u32x4 *)(gk + (int64_t)from[i] * k.row), y[i] = *(const u32x4 *)(gv + (int64_t)from[i] * v.row);
+#pragma unroll
+        for (int i = 0; i < COPY_ROWS; ++i)
+            if (to + i * side < last) {
+                *(u32x4 *)(ok + (int64_t)(to + i * side) * k_out.row) = x[i];
+                *(u32x4 *)(ov + (int64_t)(to + i * side) * v_out.row) = y[i];
+            }
     }
 }
 
@@ -283,18 +287,18 @@ __global__ __launch_bounds__(IN) void k_insert(InsertShape s, Rows k_new, Rows v
 
 }  // namespace
 
+
+constexpr uint32_t EVICT_UNITS = 256;
+
 hipError_t launch_cache_evict(const EvictShape &s, const Rows &k, const Rows &v, const float *weights, const int32_t *positions,
                               const Rows &k_out, const Rows &v_out, float *weights_out, int32_t *positions_out, int32_t *lens_out,
                               int32_t *kept, hipStream_t st)
 {
     const uint32_t rows = s.batch * s.kv_heads;
-    if (s.slots <= 4 * EV) k_evict_choose<4><<<rows, EV, 0, st>>>(s, weights, positions, kept, weights_out, positions_out, lens_out);
-    else if (s.slots <= 16 * EV) k_evict_choose<16><<<rows, EV, 0, st>>>(s, weights, positions, kept, weights_out, positions_out, lens_out);
-    else k_evict_choose<0><<<rows, EV, 0, st>>>(s, weights, positions, kept, weights_out, positions_out, lens_out);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    const uint32_t per = CP / (s.head_dim / 8) * CP_ROWS;
-    k_evict_copy<<<dim3((s.slots_out + per - 1) / per, s.batch * s.kv_heads), CP, 0, st>>>(s, k, v, k_out, v_out, kept);
+    const uint32_t spread = rows < EVICT_UNITS ? EVICT_UNITS / rows : 1, passes = (s.slots_out + 255) / 256;
+    const uint32_t pieces = spread < passes ? spread : passes, grid = rows * pieces;
+    const auto kernel = s.slots <= 4 * EV ? k_evict<4> : s.slots <= 16 * EV ? k_evict<16> : k_evict<0>;
+    kernel<<<grid, EV, 0, st>>>(s, k, v, weights, positions, k_out, v_out, kept, weights_out, positions_out, lens_out, pieces);
     return hipGetLastError();
 }
 
