@@ -4,10 +4,10 @@
 // least), equal ones with the higher index first, then the newest `recent` positions.  An eviction keeps the last `keep`
 // of that order and copies them, in the order of their slots, into another cache; an insertion overwrites the first.
 //
-// Measured: 8 ragged prompts of up to 16384 tokens, 8 heads, into 2048 slots of 128 elements, 18 us to choose (a workgroup for
-// each of 64 rows: 2.6 to read 16384 weights, 6 for the first digit of the search, 4 for the others, 5 to place) + 20 us to copy
-// (134 MB read and written, 6.8 TB/s).  An insertion into 64 x 8 caches of 2048 slots 4.5 us, most of it a launch and three
-// dependent accesses.
+// Measured: 8 ragged prompts of up to 16384 tokens, 8 heads, into 2048 slots of 128 elements, 32 us: the choice is a chain of some
+// 18 in the longest rows (2.6 to read 16384 weights, 6 for the first digit of the search, 4 for the others, 5 to place), while
+// shorter ones are copied (134 MB read and written in all, 20 us alone).  An insertion into 64 x 8 caches of 2048 slots 4.7 us,
+// most of it a launch and three dependent accesses.
 #include "attn_core.h"
 #include "lap_dev.h"
 
@@ -54,8 +54,10 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int COPY_ROWS = 4;      // rows of keys and of values that a thread has on their way
 
 // The slots that stay, ascending, and their rows of keys and values.  `pieces` workgroups for each row find the same order each,
-// write a share of the new cache's slots, and copy these; a stretch of the row for each wave, with the weights of EACH x 64 slots in registers (EACH 0: read again from the L2 cache each time).  The key of the
-// last one that stays is found digit by digit (13, 13 and 6 bits: the first one has four bits of a weight's fraction, so
+// write a share of the new cache's slots, and copy these: a copy that starts with a row's choice and spreads over the chip, in
+// one launch (a choice by one workgroup a row, then a copy of all rows: 38 us in place of 32 above).  A stretch of the row
+// for each wave, with the weights of EACH x 64 slots in registers (EACH 0: read again from the L2 cache each time).  The key of
+// the last one that stays is found digit by digit (13, 13 and 6 bits: the first one has four bits of a weight's fraction, so
 // that weights of one size do not all meet in one counter) from counts in LDS.
 template <int EACH>
 __global__ __launch_bounds__(EV) void k_evict(EvictShape s, Rows k, Rows v, const float *weights, const int32_t *positions, Rows k_out, Rows v_out,
@@ -93,27 +95,30 @@ __global__ __launch_bounds__(EV) void k_evict(EvictShape s, Rows k, Rows v, cons
 
     // this wave's slots, in whole 64s
     const int each = ((row.len + EW - 1) / EW + 63) / 64 * 64, i0 = wave * each, i1 = min(i0 + each, row.len);
-    float mine[EACH ? EACH : 1];      // all asked for before the first is looked at
-    uint32_t keys[EACH ? EACH : 1];
-    if (EACH > 0 && i0 < i1) {
+    constexpr int AHEAD = EACH ? EACH : 16;      // times 64 weights, asked for before the first is looked at
+    float mine[AHEAD];
+    uint32_t keys[AHEAD];
+    const auto read = [&](int from) {
 #pragma unroll
-        for (int j = 0; j < EACH; ++j) mine[j] = row.weights[min(i0 + 64 * j + lane, i1 - 1)];
+        for (int j = 0; j < AHEAD; ++j) mine[j] = row.weights[min(from + 64 * j + lane, i1 - 1)];
 #pragma unroll
-        for (int j = 0; j < EACH; ++j) {
-            const int i = i0 + 64 * j + lane, p = positions ? row.positions[min(i, i1 - 1)] : i;
+        for (int j = 0; j < AHEAD; ++j) {
+            const int i = from + 64 * j + lane, p = positions ? row.positions[min(i, i1 - 1)] : i;
             keys[j] = i < i1 ? row.key(mine[j], p) : EMPTY;
         }
-    }
+    };
+    if (EACH > 0 && i0 < i1) read(i0);
     const auto for_all = [&](auto &&f) {      // f(first slot, this lane's key and weight), for 64 slots at a time
         if constexpr (EACH > 0) {
 #pragma unroll
             for (int j = 0; j < EACH; ++j)
                 if (i0 + 64 * j < i1) f(i0 + 64 * j, keys[j], mine[j]);
         } else
-            for (int i = i0; i < i1; i += 64) {
-                const int at = min(i + lane, i1 - 1);
-                const float w = row.weights[at];
-                f(i, i + lane < i1 ? row.key(w, positions ? row.positions[at] : i + lane) : EMPTY, w);
+            for (int from = i0; from < i1; from += 64 * AHEAD) {
+                read(from);
+#pragma unroll
+                for (int j = 0; j < AHEAD; ++j)
+                    if (from + 64 * j < i1) f(from + 64 * j, keys[j], mine[j]);
             }
     };
 
@@ -287,16 +292,17 @@ __global__ __launch_bounds__(IN) void k_insert(InsertShape s, Rows k_new, Rows v
 
 }  // namespace
 
-
-constexpr uint32_t EVICT_UNITS = 256;
+// Workgroups for a row: as many as rows leave units for (with twice as many, which take turns, 44 us in place of 32 above), of
+// 256 slots of the new cache at least.
+constexpr uint32_t EVICT_UNITS = 256, EVICT_LEAST = 256;
 
 hipError_t launch_cache_evict(const EvictShape &s, const Rows &k, const Rows &v, const float *weights, const int32_t *positions,
                               const Rows &k_out, const Rows &v_out, float *weights_out, int32_t *positions_out, int32_t *lens_out,
                               int32_t *kept, hipStream_t st)
 {
     const uint32_t rows = s.batch * s.kv_heads;
-    const uint32_t spread = rows < EVICT_UNITS ? EVICT_UNITS / rows : 1, passes = (s.slots_out + 255) / 256;
-    const uint32_t pieces = spread < passes ? spread : passes, grid = rows * pieces;
+    const uint32_t spread = rows < EVICT_UNITS ? EVICT_UNITS / rows : 1, most = (s.slots_out + EVICT_LEAST - 1) / EVICT_LEAST;
+    const uint32_t pieces = spread < most ? spread : most, grid = rows * pieces;
     const auto kernel = s.slots <= 4 * EV ? k_evict<4> : s.slots <= 16 * EV ? k_evict<16> : k_evict<0>;
     kernel<<<grid, EV, 0, st>>>(s, k, v, weights, positions, k_out, v_out, kept, weights_out, positions_out, lens_out, pieces);
     return hipGetLastError();
