@@ -9,7 +9,7 @@
 // A wave keeps 32 rows and their outputs in registers; four waves share tiles of keys and values in LDS, fetched while the
 // tile before is worked on.  For 32 rows and 64 keys of 128 elements a wave has 32 products of 32 cycles and 230 vector
 // instructions of 4 (exponentials 8); two or three waves on a SIMD overlap the two in part.  Measured: 32 heads x 12345 rows on
-// 13370 keys, causal, 1.35 ms = 1075 TFLOP/s, 88 % of what a large matrix product reaches on the same card, with the matrix
+// 13370 keys, causal, 1.36 ms = 1070 TFLOP/s, 88 % of what a large matrix product reaches on the same card, with the matrix
 // unit busy in 60 % of the cycles and the clock down to 1.7 GHz: bound by power, and other orders of the instructions (scores
 // of the next tile worked out beside the exponentials, products and vector instructions dealt out by hand) came out within
 // 3 % or worse.  8 x 16 heads x 2048 tokens, causal: 160 us = 860 TFLOP/s; 6 % of it is the diagonal's hidden half tiles and

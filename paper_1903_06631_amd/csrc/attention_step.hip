@@ -10,7 +10,7 @@
 // a workgroup of eight waves each, which adds the weights too: one launch, and nothing to join.
 //
 // Measured: 2 caches of 8 heads x 131072 slots x 128, 4 query heads each, 216 + 16 us, the first kernel at 5.1 TB/s (a copy of
-// 2 GiB: 4.9); 64 ragged caches of 8 heads x up to 4096 slots 128 us in a workgroup each (in chunks 123 + 12); one of 16
+// 2 GiB: 4.9); 64 ragged caches of 8 heads x up to 4096 slots 124 us in a workgroup each (in chunks 123 + 12); one of 16
 // heads x 1000 slots 14 us, a launch and a chain of four tiles a wave.
 #include "attn_core.h"
 
@@ -299,7 +299,7 @@ template <class T, int DP> hipError_t launch(const StepShape &s, const StepWork 
 //   1 x 16 heads   500 slots 12.9 17.2, 1000 14.1 17.3, 1500 18.6 17.5      b = 16   1500 22 26, 2900 36 41, 4000 60 53
 //   b = 24         2000 33 42, 4000 81 94, 16000 363 293                    b = 36   2000 74 71 (ragged 31 43), 4000 153 123 (70 70)
 //   b = 48         2000 87 100, 4000 162 160 (87 101)                       b = 64   1000 46 56, 4000 188 210, 16000 961 931
-//   b = 96         2000 145 161, 4000 278 305, 8000 622 603                 (b = 64, ragged, 4 query heads each: 4096 128 135)
+//   b = 96         2000 145 161, 4000 278 305, 8000 622 603                 (b = 64, ragged, 4 query heads each: 4096 123 135)
 // So up to 1024 slots always, up to 2048 where there are workgroups for half the units, up to 4096 where the last round of
 // workgroups fills three quarters of them (eight waves take up a unit's LDS).
 static bool whole_caches(uint64_t rows, uint32_t slots)
