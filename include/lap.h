@@ -389,7 +389,9 @@ int lap_plan_pool_orders(uint32_t n_vars, uint32_t n_steps, uint32_t B, const vo
  *   - A row that sees no key, and a row beyond its sequence's length, has o = 0, lse = minus infinity and gradients of 0.
  *     A score below -1e30 / scale counts as hidden.  A value that is not finite reaches the rows that see it and no others.
  * Sums, scores and probabilities are held in 32 bits; probabilities and their gradients are rounded to the element type
- * where they enter the next product, results once when they are written.  Every sum has a fixed order: equal calls give
+ * where they enter the next product, results once when they are written.  In the backward pass on binary16 both enter it as
+ * multiples of a power of two, of the row's own for the latter: gradients that the type holds come out whatever the size of
+ * what they are sums of.  Every sum has a fixed order: equal calls give
  * equal bits.  Rows are [batch, heads, length, head_dim] by strides, which also serve [batch, length, heads, head_dim];
  * inputs may be broadcast (stride 0).  Nothing is allocated, and all calls can be captured in a graph. */
 enum { LAP_T_BF16 = 0, LAP_T_F16 = 1 };      /* bfloat16, IEEE binary16 */

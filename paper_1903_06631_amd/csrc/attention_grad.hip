@@ -66,8 +66,8 @@ __global__ __launch_bounds__(QW * KG * 64, 2) void k_attention_dq(AttnShape s, R
         // a row without keys gets probabilities of zero
         const float sum = lse[at + used], l2 = sum == -ATTN_INF ? ATTN_INF : sum * LOG2E;
         if (row < sp.ql && lane < 32 && kg == 0) {
-            stats[at + row] = l2;
-            stats[(int64_t)s.batch * s.q_heads * s.q_len + at + row] = delta;
+            stats[at + row] = IS_F16<T> ? l2 - P16 : l2;      // probabilities times 2^P16 in the second kernel
+            stats[(int64_t)s.batch * s.q_heads * s.q_len + at + row] = IS_F16<T> ? -delta : delta;      // there the second kernel's sums start with it
         }
 
         if (k0 < k1) {
@@ -82,9 +82,11 @@ __global__ __launch_bounds__(QW * KG * 64, 2) void k_attention_dq(AttnShape s, R
             const RowRead<DP, T> rows(lane);
             const ColRead<DP, T> cols(lane);
             const TileLoad<DP, KT, NW> tk(k.row, last_chunk, wave, lane), tv(v.row, last_chunk, wave, lane);
+            float f;      // what z and ds are multiplied by, in binary16
             const auto pass = [&](auto careful) {
                 constexpr bool care = decltype(careful)::value;
                 bool odd = false;      // blocks have been left out
+                f = IS_F16<T> ? FIRST_F : 1.f;
                 tk.issue(lk[0], gk, k0, sp.kl - 1, wave);
                 tv.issue(lv[0], gv, k0, sp.kl - 1, wave);
                 int buf = 0;
@@ -103,11 +105,23 @@ __global__ __launch_bounds__(QW * KG * 64, 2) void k_attention_dq(AttnShape s, R
                         for (int d = 0; d < DP / 16; ++d) x = Elem<T>::mfma(rows.get(lk[buf], kb, d), qf[d], x);
 #pragma unroll
                         for (int d = 0; d < DP / 16; ++d) y = Elem<T>::mfma(rows.get(lv[buf], kb, d), gf[d], y);
-                        float ds[16];
+                        const bool part = at + 32 > all_hi || at < all_lo;
+                        const int key0 = at + 4 * (lane >> 5);
+                        float z[16], ds[16];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) ds[i] = exp2_fast(__builtin_fmaf(x[i], c, -l2)) * (y[i] - delta);
-                        if (at + 32 > all_hi || at < all_lo) {
-                            const int key0 = at + 4 * (lane >> 5);
+                        for (int i = 0; i < 16; ++i) z[i] = IS_F16<T> ? __builtin_fmaf(y[i], f, -delta * f) : y[i] - delta;
+                        if constexpr (IS_F16<T>) {
+                            if (part)
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) {
+                                    const int key = key0 + 8 * (i / 4) + i % 4;
+                                    z[i] = key < hi && key >= lo ? z[i] : 0.f;
+                                }
+                            hold_in_range<15>(z, f, acc);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) ds[i] = exp2_fast(__builtin_fmaf(x[i], c, -l2)) * z[i];
+                        if (part) {
 #pragma unroll
                             for (int i = 0; i < 16; ++i) {
                                 const int key = key0 + 8 * (i / 4) + i % 4;
@@ -141,7 +155,7 @@ __global__ __launch_bounds__(QW * KG * 64, 2) void k_attention_dq(AttnShape s, R
                             for (int key = max(at, lo); key < min(at + 32, hi); ++key) {
                                 const T *const krow = gk + (int64_t)key * k.row;
                                 const float p = exp2_fast(__builtin_fmaf(dot(qrow, krow, s.head_dim), c, -l2));
-                                add_row<DP>(acc, krow, p * (dot(grow, gv + (int64_t)key * v.row, s.head_dim) - delta), s.head_dim, lane);
+                                add_row<DP>(acc, krow, p * ((dot(grow, gv + (int64_t)key * v.row, s.head_dim) - delta) * f), s.head_dim, lane);
                             }
                         }
                 }
@@ -154,6 +168,7 @@ __global__ __launch_bounds__(QW * KG * 64, 2) void k_attention_dq(AttnShape s, R
                 for (int d = 0; d < DP / 32; ++d) acc[d] = f32x16{};
                 pass(std::true_type());
             }
+            if constexpr (IS_F16<T>) times(acc, 1.f / f);
         }
     }
     if constexpr (KG > 1) {
@@ -227,9 +242,11 @@ __global__ __launch_bounds__(KW * RG * 64, 2) void k_attention_dkv(AttnShape s, 
         const ColRead<DP, T> cols(lane);
         const TileLoad<DP, QT, NW> tq(q.row, last_chunk, wave, lane), tg(g.row, last_chunk, wave, lane);
         const int64_t to_delta = (int64_t)s.batch * s.q_heads * s.q_len;
+        float f;      // what z and ds are multiplied by, in binary16 (ds beside the 2^P16 of its probability)
         const auto pass = [&](auto careful) {
             constexpr bool care = decltype(careful)::value;
             bool odd = false;      // blocks have been left out
+            f = IS_F16<T> ? FIRST_F : 1.f;
             const T *gq = (const T *)q.data + (int64_t)b * q.batch + head0 * q.head;
             const T *gg = (const T *)g.data + (int64_t)b * g.batch + head0 * g.head;
             const float *gs = stats + ((int64_t)b * s.q_heads + head0) * s.q_len;
@@ -250,20 +267,35 @@ __global__ __launch_bounds__(KW * RG * 64, 2) void k_attention_dkv(AttnShape s, 
                 qt = qt + QT >= r1 ? r0 : qt + QT;
                 const int at = tile + 32 * rg;
                 if (at >= any_hi || at + 32 <= any_lo) continue;
+                const float *const l2 = lst[buf][0] + 32 * rg + 4 * (lane >> 5), *const delta = lst[buf][1] + 32 * rg + 4 * (lane >> 5);
                 f32x16 x = {}, y = {};
+                if constexpr (IS_F16<T>)      // (minus delta there: the difference comes out of the product)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) y[i] = delta[8 * (i / 4) + i % 4];
 #pragma unroll
                 for (int d = 0; d < DP / 16; ++d) x = Elem<T>::mfma(rows.get(lq[buf], rg, d), kf[d], x);
 #pragma unroll
                 for (int d = 0; d < DP / 16; ++d) y = Elem<T>::mfma(rows.get(lg[buf], rg, d), rows.get(lkept, kw, d), y);
-                const float *const l2 = lst[buf][0] + 32 * rg + 4 * (lane >> 5), *const delta = lst[buf][1] + 32 * rg + 4 * (lane >> 5);
-                float p[16], ds[16];
+                const bool part = at + 32 > all_hi || at < all_lo;
+                const int row0 = at + 4 * (lane >> 5);
+                float z[16], p[16], ds[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[i] = IS_F16<T> ? y[i] * f : y[i] - delta[8 * (i / 4) + i % 4];
+                if constexpr (IS_F16<T>) {
+                    if (part)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int row = row0 + 8 * (i / 4) + i % 4;
+                            z[i] = row < hi && row >= lo ? z[i] : 0.f;
+                        }
+                    hold_in_range<15 - P16>(z, f, ak);
+                }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     p[i] = exp2_fast(__builtin_fmaf(x[i], c, -l2[8 * (i / 4) + i % 4]));
-                    ds[i] = p[i] * (y[i] - delta[8 * (i / 4) + i % 4]);
+                    ds[i] = p[i] * z[i];
                 }
-                if (at + 32 > all_hi || at < all_lo) {
-                    const int row0 = at + 4 * (lane >> 5);
+                if (part) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int row = row0 + 8 * (i / 4) + i % 4;
@@ -304,7 +336,7 @@ __global__ __launch_bounds__(KW * RG * 64, 2) void k_attention_dkv(AttnShape s, 
                         const T *const qrow = q0 + (int64_t)row * q.row, *const grow = g0 + (int64_t)row * g.row;
                         const float p = exp2_fast(__builtin_fmaf(dot(qrow, krow, s.head_dim), c, -st[row]));
                         add_row<DP>(av, grow, p, s.head_dim, lane);
-                        add_row<DP>(ak, qrow, p * (dot(grow, vrow, s.head_dim) - st[to_delta + row]), s.head_dim, lane);
+                        add_row<DP>(ak, qrow, p * ((dot(grow, vrow, s.head_dim) - (IS_F16<T> ? -st[to_delta + row] : st[to_delta + row])) * f), s.head_dim, lane);
                     }
                 }
             }
@@ -317,6 +349,7 @@ __global__ __launch_bounds__(KW * RG * 64, 2) void k_attention_dkv(AttnShape s, 
             for (int d = 0; d < DP / 32; ++d) ak[d] = av[d] = f32x16{};
             pass(std::true_type());
         }
+        if constexpr (IS_F16<T>) times(av, 1.f / (1 << P16)), times(ak, 1.f / (1 << P16) / f);
     }
     if constexpr (RG > 1) {
         static_assert((RG - 1) * KW * DP / 2 * 64 * sizeof(float) <= sizeof(tiles_qg), "the sums fit where the tiles were");
