@@ -21,6 +21,10 @@
 namespace lap {
 namespace {
 
+// What probabilities are multiplied by, in base 2: they are taken from a maximum that may be passed by 2^8 (below), and in
+// binary16 all that are below 2^-25 of it would be nothing (400 000 keys at 2^-25.5 beside one at 1: 0.8 % of the row).
+template <class T> constexpr float SHIFT = __is_same(T, _Float16) ? 7.f : 0.f;
+
 // QW blocks of 32 rows; their keys are dealt to KG waves each, NB blocks of 32 keys at a time.  Where rows are few, waves that
 // share them fill the units that would have none; they join their sums at the end.
 template <class T, int DP, int QW, int KG, int NB>
@@ -129,7 +133,7 @@ __global__ __launch_bounds__(QW * KG * 64, NB == 1 && KG == 1 ? 3 : 2) void k_at
 #pragma unroll
                         for (int i = 0; i < 16; ++i) acc[d][i] *= by;
                 }
-                const float mc = m * c;
+                const float mc = m * c - SHIFT<T>;
                 float part = 0.f;
                 if (!finite) {
                     odd = true;
@@ -166,7 +170,7 @@ __global__ __launch_bounds__(QW * KG * 64, NB == 1 && KG == 1 ? 3 : 2) void k_at
 #pragma unroll 1
                     for (int key = max(mine, lo); key < min(mine + 32 * NB, hi); ++key) {
                         const float x = dot(qrow, gk + (int64_t)key * k.row, s.head_dim);
-                        add_row<DP>(acc, gv + (int64_t)key * v.row, exp2_fast((x - m) * c), s.head_dim, lane);
+                        add_row<DP>(acc, gv + (int64_t)key * v.row, exp2_fast((x - m) * c + SHIFT<T>), s.head_dim, lane);
                     }
                 }
             }
@@ -222,7 +226,7 @@ __global__ __launch_bounds__(QW * KG * 64, NB == 1 && KG == 1 ? 3 : 2) void k_at
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d) acc[d] = f32x16{};
         store_kept<DP>(orow, acc, some ? 1.f / l : 0.f, s.head_dim, lane);
-        if (lane < 32) *lrow = some ? m * s.scale + __logf(l) : -ATTN_INF;
+        if (lane < 32) *lrow = some ? m * s.scale + __logf(l) - SHIFT<T> * LN2 : -ATTN_INF;
     }
 }
 
@@ -255,7 +259,7 @@ __global__ __launch_bounds__(256) void k_attention_join(AttnShape s, Rows o, flo
 #pragma unroll
     for (int j = 0; j < N; ++j) z[j] = (T)(some ? y[j] / l : 0.f);
     if (lane * N < (int)s.head_dim) *(TN *)to = z;
-    if (lane == 0) lse[at] = some ? m * s.scale + __logf(l) : -ATTN_INF;
+    if (lane == 0) lse[at] = some ? m * s.scale + __logf(l) - SHIFT<T> * LN2 : -ATTN_INF;
 }
 
 template <class T, int DP, int QW, int KG, int NB>
