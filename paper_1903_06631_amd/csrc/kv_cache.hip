@@ -28,8 +28,8 @@ constexpr int EV = 1024, EW = EV / 64, BIN_BITS = 13, BINS = 1 << BIN_BITS;
 struct EvictRow {
     const float *weights;
     const int32_t *positions;
-    int len, from;      // slots in use; the first position that is among the newest
-    __device__ __forceinline__ uint32_t key(float w, int p) const { return p < 0 ? EMPTY : p >= from ? NEWEST : weight_key(w); }
+    int len, newest, recent;      // slots in use; the largest position; how many up to it are among the newest
+    __device__ __forceinline__ uint32_t key(float w, int p) const { return p < 0 ? EMPTY : newest - p < recent ? NEWEST : weight_key(w); }
 };
 
 // how many of the lanes before this one are among `set`
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(EV) void k_evict(EvictShape s, Rows k, Rows v, cons
         for (int i = 0; i < EW; ++i) newest = max(newest, (int)part[i][0]), used += (int)part[i][1];
         __syncthreads();
     }
-    row.from = newest - (int)s.recent + 1;
+    row.newest = newest, row.recent = (int)s.recent;
     const int keep = min((int)s.keep, used);
 
     // this wave's slots, in whole 64s
