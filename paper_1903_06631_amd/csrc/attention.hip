@@ -67,6 +67,7 @@ __global__ __launch_bounds__(QW * KG * 64, NB == 1 && KG == 1 ? 3 : 2) void k_at
         k0 = uniform(k0 + (int)(n * part / parts) * KT);
     }
     if (k0 < k1) {
+        zero_tiles<DP, NW * 64>(tiles_kv[0], sizeof(tiles_kv) / sizeof(T), s.head_dim);
         const int used = min(row, sp.ql - 1);       // padding takes the last row's part and is thrown away
         const int last_chunk = (int)s.head_dim / 8 - 1, last = sp.kl - 1;
         const T *gk = (const T *)k.data + (int64_t)b * k.batch + (int64_t)wk.kvh * k.head;

@@ -83,6 +83,7 @@ __global__ __launch_bounds__(QW * KG * 64, 2) void k_attention_dq(AttnShape s, R
             const ColRead<DP, T> cols(lane);
             const TileLoad<DP, KT, NW> tk(k.row, last_chunk, wave, lane), tv(v.row, last_chunk, wave, lane);
             float f;      // what z and ds are multiplied by, in binary16
+            zero_tiles<DP, NW * 64>(tiles_kv[0], sizeof(tiles_kv) / sizeof(T), s.head_dim);
             const auto pass = [&](auto careful) {
                 constexpr bool care = decltype(careful)::value;
                 bool odd = false;      // blocks have been left out
@@ -242,6 +243,7 @@ __global__ __launch_bounds__(KW * RG * 64, 2) void k_attention_dkv(AttnShape s, 
         const ColRead<DP, T> cols(lane);
         const TileLoad<DP, QT, NW> tq(q.row, last_chunk, wave, lane), tg(g.row, last_chunk, wave, lane);
         const int64_t to_delta = (int64_t)s.batch * s.q_heads * s.q_len;
+        zero_tiles<DP, NW * 64>(tiles_qg[0], sizeof(tiles_qg) / sizeof(T), s.head_dim);
         float f;      // what z and ds are multiplied by, in binary16 (ds beside the 2^P16 of its probability)
         const auto pass = [&](auto careful) {
             constexpr bool care = decltype(careful)::value;

@@ -64,6 +64,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_weights(AttnShape s, R
             if (next >= r1) next = r0, gq += q.head, gs += s.q_len;
         };
         int buf = 0, qt = next;
+        zero_tiles<DP, NW * 64>(lq[0], sizeof(lq) / sizeof(T), s.head_dim);
         issue(0);
         for (int n = n0; n < n1; ++n, buf ^= 1) {
             tiles_arrive();

@@ -71,8 +71,10 @@ template <int DP> struct Tile {
     static __device__ __forceinline__ int place(int row, int chunk) { return row / G * GROUP + row % G * DP + (chunk ^ swz(row)) * 8; }
 };
 
-// ROWS rows from global memory into LDS, asynchronously, by NW waves.  Rows past `last` are copies of it and chunks past
-// the last one of a row copies of that one: padding is never read, and what stands in its place is part of the same row.
+// ROWS rows from global memory into LDS, asynchronously, by NW waves.  Rows past `last` are copies of it: padding is never
+// read.  Chunks past the last one of a row are left alone by lanes that sit out; zero_tiles() has put zeros there, or what comes of them
+// is thrown away.  (Copies of the last chunk, times the zeros on the other side of a product, are not a number where that
+// chunk holds an infinity.)
 // The compiler does not see these loads: it would wait for the ones just sent off before any read of LDS, as it cannot
 // tell the tiles apart.  tiles_arrive() waits for them.
 template <int DP, int ROWS, int NW> struct TileLoad {
@@ -80,13 +82,17 @@ template <int DP, int ROWS, int NW> struct TileLoad {
     static constexpr int PER = ROWS / L::G / NW;      // instructions of a wave
     static_assert(PER * NW * L::G == ROWS, "whole instructions");
     uint32_t off;           // this lane's bytes of the first instruction; the others are a number of rows further on
-    uint32_t stride;        // bytes of a row (at most 2^25: 64 rows stay within 32 bits)
+    uint32_t stride;        // bytes of a row (at most 2^25 - 16: the start of a tile's 128th row, and that row, are within 32 bits)
     int row0;
+    bool takes_part;
+    static_assert(ROWS <= 128, "offsets within 32 bits");
     __device__ __forceinline__ TileLoad(int64_t row_stride, int last_chunk, int wave, int lane)
     {
         stride = (uint32_t)row_stride * 2u;
         row0 = wave * PER * L::G + lane / L::CH;
-        off = (uint32_t)row0 * stride + (uint32_t)min((lane % L::CH) ^ L::swz(lane / L::CH), last_chunk) * 16u;
+        const int chunk = (lane % L::CH) ^ L::swz(lane / L::CH);
+        off = (uint32_t)row0 * stride + (uint32_t)chunk * 16u;
+        takes_part = chunk <= last_chunk;
     }
     // rows first .. first + ROWS - 1 of g; first <= last
     template <class T> __device__ __forceinline__ void issue(T *lds, const T *g, int first, int last, int wave) const
@@ -94,6 +100,7 @@ template <int DP, int ROWS, int NW> struct TileLoad {
         const char *base = (const char *)g + (int64_t)first * stride;
         const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(ATTN_LDS void *)lds + (uint32_t)(wave * PER * L::GROUP * 2));
         const int left = last - first;
+        if (!takes_part) return;
         if (left >= ROWS - 1) {
 #pragma unroll
             for (int j = 0; j < PER; ++j) send(to + j * (L::GROUP * 2u), off, base + (uint64_t)(j * L::G) * stride);
@@ -118,6 +125,14 @@ __device__ __forceinline__ void load_floats(float *lds, const float *g, int firs
     const char *base = (const char *)(g + first);
     const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(ATTN_LDS void *)(lds + 64 * part));
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(4u * (uint32_t)min(64 * part + lane, last - first)), "s"(base) : "memory");
+}
+
+// Zeros into tiles of rows with fewer than DP elements, before the first of them is asked for.
+template <int DP, int NT, class T> __device__ __forceinline__ void zero_tiles(T *tiles, int n, uint32_t head_dim)
+{
+    if (head_dim == DP) return;
+    for (int i = threadIdx.x * 8; i < n; i += NT * 8) *(s16x8 *)(tiles + i) = s16x8{};
+    __syncthreads();
 }
 
 // what has been asked for has arrived in LDS, for every wave, and every wave is done with what it has read there

@@ -1,0 +1,48 @@
+"""Values that are not finite, or lie at the ends of their type, where the definition still says what a result is."""
+import math
+
+import pytest
+import torch
+
+import attention_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+BF, HF = torch.bfloat16, torch.float16
+
+
+@pytest.fixture(scope="module")
+def lap():
+    import paper_1903_06631_amd as lap
+    lap.load_library()
+    return lap
+
+
+def normal(gen, h, n, d, kind):
+    return torch.randn(1, h, n, d, generator=gen).to(kind).cuda()
+
+
+# head size; query heads and key heads; the rest of the shapes as few as reach the sharings of the waves
+@pytest.mark.parametrize("kind", [BF, HF])
+@pytest.mark.parametrize("d,heads,kv", [(72, 2, 1), (8, 2, 2), (40, 150, 75), (120, 300, 300), (64, 2, 1), (128, 2, 1)])
+def test_a_key_hidden_by_minus_infinity(lap, kind, d, heads, kv):
+    """The last element of the head as a mask: 1 in every query, minus infinity in the keys that are not to be seen.  Their
+    scores are minus infinity, their probabilities 0, and so are their weights and the gradients of their values; all else is
+    what it is without those keys."""
+    gen = torch.Generator().manual_seed(d)
+    n = 130
+    q, k, v, g = normal(gen, heads, n, d, kind), normal(gen, kv, n, d, kind), normal(gen, kv, n, d, kind), normal(gen, heads, n, d, kind)
+    hide = torch.zeros(n, dtype=torch.bool)
+    hide[[3, 64, 100, n - 1]] = True
+    q[..., d - 1], k[..., d - 1] = 1, 0
+    want = ref.Case(q, k[:, :, ~hide], v[:, :, ~hide])
+    k[:, :, hide.cuda(), d - 1] = -math.inf
+    got = lap.attention(q, k, v)
+    assert float(((got["lse"].cpu().double() - want.lse).abs() - want.lse_bound).max()) <= 0
+    assert float(((got["out"].cpu().double() - want.out).abs() - want.out_bound).max()) <= 0
+    grads = lap.attention_grad(g, q, k, v, got["out"], got["lse"])
+    dv, bound = want.grads(g, got["out"])["dv"]
+    assert float(((grads["dv"][:, :, ~hide.cuda()].cpu().double() - dv).abs() - bound).max()) <= 0 and not grads["dv"][:, :, hide.cuda()].any()
+    w, bound = want.weights()
+    got_w = lap.attention_weights(q, k, got["lse"])["weights"].cpu().double()
+    assert float(((got_w[:, :, ~hide] - w).abs() - bound).max()) <= 0 and not got_w[:, :, hide].any()
