@@ -90,10 +90,10 @@ __global__ __launch_bounds__(NW * 64, 2) void k_step(StepShape s, StepWork w)
         if (live != ~0u) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) p[i] = (live >> (8 * (i / 4) + 4 * h + i % 4)) & 1 ? p[i] : -ATTN_INF;
-            if (pos) {      // what an empty slot holds may be anything, and zero times it is not always zero
-                for (int n = lane; n < TS * DP / 8; n += 64)
-                    if (!((live >> (n / (DP / 8))) & 1)) *(s16x8 *)(mine + buf * TILE + Tile<DP>::place(n / (DP / 8), n % (DP / 8))) = s16x8{};
-            }
+            // what an empty slot holds may be anything, and past the length stand copies of the last slot, which may be
+            // infinite: zero times it is not always zero
+            for (int n = lane; n < TS * DP / 8; n += 64)
+                if (!((live >> (n / (DP / 8))) & 1)) *(s16x8 *)(mine + buf * TILE + Tile<DP>::place(n / (DP / 8), n % (DP / 8))) = s16x8{};
         }
         if (w.weights && r < n_rows) {
             float *const to = IN_LDS ? kept + r * pitch : scores;

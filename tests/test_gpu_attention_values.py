@@ -46,3 +46,20 @@ def test_a_key_hidden_by_minus_infinity(lap, kind, d, heads, kv):
     w, bound = want.weights()
     got_w = lap.attention_weights(q, k, got["lse"])["weights"].cpu().double()
     assert float(((got_w[:, :, ~hide] - w).abs() - bound).max()) <= 0 and not got_w[:, :, hide].any()
+
+
+@pytest.mark.parametrize("kind", [BF, HF])
+@pytest.mark.parametrize("kv,slots,lens", [(1, 40, [33]), (8, 1000, [1000 - 7]), (2, 5000, [4097]), (96, 1500, [1025, 3, 64])])
+def test_an_infinite_value_in_the_last_slot_of_a_step(lap, kind, kv, slots, lens):
+    """Its sign is the output's: the rest of its tile, past the length, has no part in it."""
+    gen = torch.Generator().manual_seed(slots)
+    b, d = len(lens), 64
+    q = torch.randn(b, 2 * kv, d, generator=gen).to(kind).cuda()
+    k, v = (torch.randn(b, kv, slots, d, generator=gen).to(kind).cuda() for _ in range(2))
+    clean = lap.attention_step(q, k, v, lens=torch.tensor(lens, dtype=torch.int32, device="cuda"))["out"]
+    for i, n in enumerate(lens):
+        v[i, :, n - 1, 5], v[i, :, n - 1, 6] = math.inf, -math.inf
+    out = lap.attention_step(q, k, v, lens=torch.tensor(lens, dtype=torch.int32, device="cuda"))["out"]
+    assert (out[..., 5] == math.inf).all() and (out[..., 6] == -math.inf).all()
+    rest = [e for e in range(d) if e not in (5, 6)]
+    assert torch.equal(out[..., rest], clean[..., rest])
