@@ -87,8 +87,10 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention_weights(AttnShape s, R
                 float l2[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    // minus infinity: a row without keys, or whose scores are all below what counts, far below this
-                    l2[i] = -LOG2E * fmaxf(lst[buf][32 * qb + 8 * (i / 4) + 4 * (lane >> 5) + i % 4], -1e20f);
+                    // minus infinity: a row without keys, or whose scores are all below what counts; others as they are, so
+                    // that what is not a number stays so
+                    const float sum = lst[buf][32 * qb + 8 * (i / 4) + 4 * (lane >> 5) + i % 4];
+                    l2[i] = sum == -ATTN_INF ? sum : -LOG2E * sum;
                 }
                 const bool whole = at + 32 <= all_hi && at >= all_lo;
 #pragma unroll

@@ -63,3 +63,20 @@ def test_an_infinite_value_in_the_last_slot_of_a_step(lap, kind, kv, slots, lens
     assert (out[..., 5] == math.inf).all() and (out[..., 6] == -math.inf).all()
     rest = [e for e in range(d) if e not in (5, 6)]
     assert torch.equal(out[..., rest], clean[..., rest])
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("n,heads", [(200, 2), (600, 40)])
+def test_weights_of_a_row_that_is_not_a_number(lap, n, heads, causal):
+    """Every key that such a row sees has a weight that is not a number, and no key that only others see."""
+    gen = torch.Generator().manual_seed(n)
+    q, k, v = normal(gen, heads, n, 64, BF), normal(gen, heads // 2, n, 64, BF), normal(gen, heads // 2, n, 64, BF)
+    k[:, :, 150] = math.nan
+    got = lap.attention(q, k, v, causal=causal)
+    w = lap.attention_weights(q, k, got["lse"], causal=causal)["weights"]
+    assert torch.isnan(w).all()      # the last rows see key 150 and all before them; without a mask all do
+    k[:, :, 150] = 1
+    q[:, ::2, 100] = math.nan        # one row: keys up to 100 under a causal mask
+    got = lap.attention(q, k, v, causal=causal)
+    w = lap.attention_weights(q, k, got["lse"], causal=causal)["weights"]
+    assert torch.isnan(w[..., :101]).all() and (not causal or torch.isfinite(w[..., 101:]).all())
