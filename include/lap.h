@@ -387,7 +387,7 @@ int lap_plan_pool_orders(uint32_t n_vars, uint32_t n_steps, uint32_t B, const vo
  *     i + k_lens[b] - q_lens[b].
  *   - causal: a row sees the keys up to where it stands; with window > 0 only the last `window` of those.
  *   - A row that sees no key, and a row beyond its sequence's length, has o = 0, lse = minus infinity and gradients of 0.
- *     A score below -1e30 / scale counts as hidden.  A value that is not finite reaches the rows that see it and no others.
+ *     A key with q.k below -1e30 counts as hidden, whatever the scale.  A value that is not finite reaches the rows that see it and no others.
  * Sums, scores and probabilities are held in 32 bits; probabilities and their gradients are rounded to the element type
  * where they enter the next product, results once when they are written.  In the backward pass on binary16 both enter it as
  * multiples of a power of two, of the row's own for the latter: gradients that the type holds come out whatever the size of

@@ -67,7 +67,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_step(StepShape s, StepWork w)
     T *const mine = lv + wave * 2 * TILE;
 
     f32x16 acc[DP / 32] = {};
-    float m = LOWEST, l = 0.f;
+    float m = LOWEST * c, l = 0.f;
     const auto fetch = [&](int at, int to) {      // slots at .. at + 31
         tv.issue(mine + to * TILE, gv, at, len - 1, 0);
         load_kept<DP>(kf, gk + (int64_t)min(at + r, len - 1) * w.k.row, s.head_dim, lane);
@@ -199,7 +199,7 @@ constexpr int JOIN = 256, JOIN_SLOTS = 1024;
 // maximum and sum of a head over its chunks, by a wave
 __device__ __forceinline__ float2 join_sums(const float2 *sums, uint32_t n, int lane)
 {
-    float m = LOWEST;
+    float m = sums[0].x;
     for (uint32_t i = lane; i < n; i += 64) m = fmaxf(m, sums[i].x);
     for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
     float l = 0.f;

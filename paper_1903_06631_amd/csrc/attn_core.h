@@ -38,7 +38,7 @@ template <> struct Elem<_Float16> {
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
-constexpr float LOWEST = -1e30f;      // running maximum of a row that has seen no key
+constexpr float LOWEST = -1e30f;      // running maximum of a row's products before its first key; times 1.5e6 still a number
 #define ATTN_INF __builtin_inff()
 
 // a number that all lanes hold alike, told to the compiler (divisions leave theirs in vector registers)

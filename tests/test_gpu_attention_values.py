@@ -80,3 +80,24 @@ def test_weights_of_a_row_that_is_not_a_number(lap, n, heads, causal):
     got = lap.attention(q, k, v, causal=causal)
     w = lap.attention_weights(q, k, got["lse"], causal=causal)["weights"]
     assert torch.isnan(w[..., :101]).all() and (not causal or torch.isfinite(w[..., 101:]).all())
+
+
+@pytest.mark.parametrize("product,scale,hidden", [(-2.0 ** 93, 2.0 ** 10, False), (-2.0 ** 93, 2.0 ** -10, False), (-2.0 ** 101, 2.0 ** 10, True),
+                                                  (-2.0 ** 101, 2.0 ** -10, True)])
+def test_one_rule_for_what_counts_as_hidden(lap, product, scale, hidden):
+    """A product q.k below -1e30 (2^99.7), whatever the scale, in a prompt, in its weights and in a step."""
+    for n in (1, 700, 3000):
+        q, k, v = torch.zeros(1, 1, 1, 64, dtype=BF, device="cuda"), torch.zeros(1, 1, n, 64, dtype=BF, device="cuda"), torch.ones(1, 1, n, 64, dtype=BF, device="cuda")
+        q[..., 0], k[..., 0] = 2.0 ** 40, product / 2.0 ** 40
+        # n equal scores: the logarithm of n is far below what 32 bits hold beside them
+        want = -math.inf if hidden else product * scale
+        weight = 0.0 if hidden else 1.0
+        a, b = lap.attention(q, k, v, scale=scale), lap.attention_step(q[:, :, 0], k, v, torch.zeros(1, 1, n, device="cuda"), scale=scale)
+        assert float(a["lse"][0, 0, 0]) == want
+        assert float(b["lse"][0, 0]) == (want if hidden else pytest.approx(want, rel=1e-6))      # (held to base 2 there)
+        assert (a["out"] == weight).all() and (b["out"] == weight).all()
+        w = lap.attention_weights(q, k, a["lse"], scale=scale)["weights"]
+        if n == 1:
+            assert float(w[0, 0, 0]) == weight and float(b["weights"][0, 0, 0]) == weight
+        elif hidden:
+            assert not w.any() and not b["weights"].any()
