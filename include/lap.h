@@ -399,7 +399,7 @@ enum { LAP_T_BF16 = 0, LAP_T_F16 = 1 };      /* bfloat16, IEEE binary16 */
 
 typedef struct {
     void *data;                 /* device, 16-byte aligned */
-    int64_t batch, head, row;   /* strides in elements, multiples of 8, row < 2^24; head_dim elements lie side by side */
+    int64_t batch, head, row;   /* strides in elements, multiples of 8, row < 2^24 (of one place: unused); head_dim elements lie side by side */
 } lap_rows;
 
 typedef struct {

@@ -2,6 +2,8 @@
 #include <math.h>
 #include <stdio.h>
 
+#include <algorithm>
+
 #include "../../include/lap.h"
 #include "attn_kernels.h"
 
@@ -28,20 +30,57 @@ int check_ws(void *ws, size_t have, size_t need)
 constexpr uint32_t MAX_LEN = 1u << 30, MAX_ITEMS = 1u << 30, MAX_GRID = 65535;
 constexpr int64_t MAX_ROW_STRIDE = 1 << 24;
 
+// The dimensions of rows that have more than one place; the others' strides are nobody's business.
+struct Dim {
+    int64_t stride, extent;
+};
+int dims_of(const lap_rows *x, uint64_t batch, uint64_t heads, uint64_t len, Dim (&d)[3])
+{
+    int n = 0;
+    if (batch > 1) d[n++] = {x->batch, (int64_t)batch};
+    if (heads > 1) d[n++] = {x->head, (int64_t)heads};
+    if (len > 1) d[n++] = {x->row, (int64_t)len};
+    return n;
+}
+
+// Whether two rows of head_dim elements, places apart by these strides, share an element.
+bool rows_overlap(Dim (&d)[3], int n, int64_t head_dim)
+{
+    std::sort(d, d + n, [](const Dim &a, const Dim &b) { return a.stride < b.stride; });
+    __int128 span = head_dim;      // the elements from the first to the last of all dimensions so far
+    int i = 0;
+    for (; i < n && d[i].stride >= span; ++i) span += (__int128)d[i].stride * (d[i].extent - 1);
+    if (i == n) return false;      // one within the other, as views of a tensor are
+    if (d[0].stride < head_dim) return true;
+    // Two or three dimensions that reach into each other: two rows are nearer than head_dim if for some number of steps along
+    // all dimensions but the one with most places, a number of steps along that one comes near to minus as much.
+    std::sort(d, d + n, [](const Dim &a, const Dim &b) { return a.extent < b.extent; });
+    const Dim last = d[n - 1], first = n == 3 ? d[0] : Dim{0, 1}, second = d[n - 2];
+    for (int64_t a = 0; a < first.extent; ++a)      // (the other half are these with all signs turned round)
+        for (int64_t b = a ? 1 - second.extent : 0; b < second.extent; ++b) {
+            const __int128 away = (__int128)a * first.stride + (__int128)b * second.stride;
+            const __int128 c = away >= 0 ? away / last.stride : -((-away + last.stride - 1) / last.stride);
+            for (__int128 k = c; k <= c + 1; ++k) {
+                const __int128 gap = away - k * last.stride;
+                if (k > -last.extent && k < last.extent && (a || b || k) && gap > -head_dim && gap < head_dim) return true;
+            }
+        }
+    return false;
+}
+
 // rows x of [batch, heads, len]; an output's rows have to be apart from each other
 int check_rows(const lap_rows *x, uint64_t batch, uint64_t heads, uint64_t len, uint32_t head_dim, bool output)
 {
     if (!x) return LAP_E_NULL;
     if (batch * heads * len == 0) return LAP_OK;
     if (!x->data) return LAP_E_NULL;
-    const int64_t all[3] = {x->batch, x->head, x->row};
     if ((uintptr_t)x->data % 16) return LAP_E_LAYOUT;
-    for (const int64_t st : all)
-        if (st < 0 || st % 8) return LAP_E_LAYOUT;
-    if (x->row >= MAX_ROW_STRIDE) return LAP_E_LAYOUT;
-    if (output && ((len > 1 && x->row < (int64_t)head_dim) || (heads > 1 && x->head < (int64_t)head_dim) || (batch > 1 && x->batch < (int64_t)head_dim)))
-        return LAP_E_LAYOUT;
-    return LAP_OK;
+    Dim d[3];
+    const int n = dims_of(x, batch, heads, len, d);
+    for (int i = 0; i < n; ++i)
+        if (d[i].stride < 0 || d[i].stride % 8) return LAP_E_LAYOUT;
+    if (len > 1 && x->row >= MAX_ROW_STRIDE) return LAP_E_LAYOUT;
+    return output && rows_overlap(d, n, head_dim) ? LAP_E_LAYOUT : LAP_OK;
 }
 
 int check_shape(const lap_attention_shape *s)
@@ -64,7 +103,13 @@ lap::AttnShape shape_of(const lap_attention_shape *s)
     return {s->batch, s->q_heads, s->kv_heads, s->q_len, s->k_len, s->head_dim, (int32_t)s->causal, (int32_t)s->window, s->scale,
             s->q_lens, s->k_lens, s->type == LAP_T_F16};
 }
-lap::Rows rows_of(const lap_rows *x) { return {x->data, x->batch, x->head, x->row}; }
+// strides of one place are not used: 0
+lap::Rows rows_of(const lap_rows *x, uint64_t batch, uint64_t heads, uint64_t len)
+{
+    return {x->data, batch > 1 ? x->batch : 0, heads > 1 ? x->head : 0, len > 1 ? x->row : 0};
+}
+lap::Rows queries_of(const lap_attention_shape *s, const lap_rows *x) { return rows_of(x, s->batch, s->q_heads, s->q_len); }
+lap::Rows keys_of(const lap_attention_shape *s, const lap_rows *x) { return rows_of(x, s->batch, s->kv_heads, s->k_len); }
 
 lap::StepShape step_of(const lap_attention_shape *s)
 {
@@ -87,6 +132,8 @@ size_t ws_step(const lap_attention_shape *s)
     const size_t heads = (size_t)s->batch * s->q_heads;
     return p.whole ? up(heads * p.score_row * 4) : up(heads * p.splits * padded_dim(s) * 4) + up(heads * p.splits * sizeof(float2)) + up(heads * p.score_row * 4);
 }
+
+lap::Rows slots_of(const lap_cache *c, const lap_rows *x) { return rows_of(x, c->batch, c->kv_heads, c->slots); }
 
 int check_cache(const lap_cache *c, bool output)
 {
@@ -132,7 +179,7 @@ int lap_attention(const lap_attention_shape *s, const lap_rows *q, const lap_row
     if (!rc && s->q_len && !lse) rc = LAP_E_NULL;
     if (!rc) rc = check_ws(ws, ws_bytes, up(lap::forward_workspace(shape_of(s))));
     if (rc || !s->q_len) return rc;
-    LAP_HIP(lap::launch_attention(shape_of(s), rows_of(q), rows_of(k), rows_of(v), rows_of(out), lse, ws, (hipStream_t)hip_stream));
+    LAP_HIP(lap::launch_attention(shape_of(s), queries_of(s, q), keys_of(s, k), keys_of(s, v), queries_of(s, out), lse, ws, (hipStream_t)hip_stream));
     return LAP_OK;
 }
 
@@ -151,8 +198,8 @@ int lap_attention_grad(const lap_attention_shape *s, const lap_rows *dout, const
     if (!rc && s->q_len && !lse) rc = LAP_E_NULL;
     if (!rc) rc = check_ws(ws, ws_bytes, ws_grad(s));
     if (rc || (!s->q_len && !s->k_len)) return rc;
-    LAP_HIP(lap::launch_attention_grad(shape_of(s), {rows_of(dout), rows_of(q), rows_of(k), rows_of(v), rows_of(out), rows_of(dq),
-                                                     rows_of(dk), rows_of(dv), lse, (float *)ws, (float *)((char *)ws + ws_stats(s))}, (hipStream_t)hip_stream));
+    LAP_HIP(lap::launch_attention_grad(shape_of(s), {queries_of(s, dout), queries_of(s, q), keys_of(s, k), keys_of(s, v), queries_of(s, out), queries_of(s, dq),
+                                                     keys_of(s, dk), keys_of(s, dv), lse, (float *)ws, (float *)((char *)ws + ws_stats(s))}, (hipStream_t)hip_stream));
     return LAP_OK;
 }
 
@@ -165,7 +212,7 @@ int lap_attention_weights(const lap_attention_shape *s, const lap_rows *q, const
     if (!rc && ((s->q_len && !lse) || (s->k_len && !weights))) rc = LAP_E_NULL;
     if (!rc) rc = check_ws(ws, ws_bytes, ws_weights(s));
     if (rc || !s->k_len) return rc;
-    LAP_HIP(lap::launch_attention_weights(shape_of(s), rows_of(q), rows_of(k), lse, before, weights, (float *)ws, (hipStream_t)hip_stream));
+    LAP_HIP(lap::launch_attention_weights(shape_of(s), queries_of(s, q), keys_of(s, k), lse, before, weights, (float *)ws, (hipStream_t)hip_stream));
     return LAP_OK;
 }
 
@@ -184,7 +231,7 @@ int lap_attention_step(const lap_attention_shape *s, const lap_rows *q, const la
     if (rc) return rc;
     const lap::StepShape p = step_of(s);
     const size_t heads = (size_t)s->batch * s->q_heads;
-    lap::StepWork w = {rows_of(q), rows_of(k), rows_of(v), rows_of(out), positions, before, lse, weights, nullptr, nullptr, nullptr};
+    lap::StepWork w = {queries_of(s, q), keys_of(s, k), keys_of(s, v), queries_of(s, out), positions, before, lse, weights, nullptr, nullptr, nullptr};
     char *at = (char *)ws;
     if (!p.whole) {
         w.outs = (float *)at, at += up(heads * p.splits * padded_dim(s) * 4);
@@ -208,8 +255,8 @@ int lap_cache_evict(const lap_cache *from, const int32_t *lens, uint32_t keep, u
     rc = check_ws(ws, ws_bytes, lap_cache_workspace_bytes(to));
     if (rc) return rc;
     const lap::EvictShape s = {from->batch, from->kv_heads, from->slots, to->slots, from->head_dim, keep, recent, lens};
-    LAP_HIP(lap::launch_cache_evict(s, rows_of(&from->k), rows_of(&from->v), from->weights, from->positions, rows_of(&to->k),
-                                    rows_of(&to->v), to->weights, to->positions, lens_out, (int32_t *)ws, (hipStream_t)hip_stream));
+    LAP_HIP(lap::launch_cache_evict(s, slots_of(from, &from->k), slots_of(from, &from->v), from->weights, from->positions, slots_of(to, &to->k),
+                                    slots_of(to, &to->v), to->weights, to->positions, lens_out, (int32_t *)ws, (hipStream_t)hip_stream));
     return LAP_OK;
 }
 
@@ -224,7 +271,8 @@ int lap_cache_insert(const lap_cache *c, const lap_rows *k_new, const lap_rows *
     if (rc) return rc;
     if (!c->weights || !c->positions || !position || !slots) return LAP_E_NULL;
     const lap::InsertShape s = {c->batch, c->kv_heads, c->slots, c->head_dim, recent};
-    LAP_HIP(lap::launch_cache_insert(s, rows_of(k_new), rows_of(v_new), rows_of(&c->k), rows_of(&c->v), c->weights, c->positions, position,
+    LAP_HIP(lap::launch_cache_insert(s, rows_of(k_new, c->batch, c->kv_heads, 1), rows_of(v_new, c->batch, c->kv_heads, 1),
+                                     slots_of(c, &c->k), slots_of(c, &c->v), c->weights, c->positions, position,
                                      slots, (hipStream_t)hip_stream));
     return LAP_OK;
 }
