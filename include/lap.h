@@ -82,7 +82,8 @@ enum {
     LAP_E_ATTENTION = -9,  /* unknown element type, query heads no multiple of the key heads, scale not positive or
                               above 1e6, window without causal, a call's own rule on its shape broken, caches that differ */
     LAP_E_LAYOUT = -10     /* rows not 16-byte aligned, head_dim no multiple of 8, a stride negative or no multiple of 8,
-                              a row stride of 2^24 or more, or an output whose rows overlap */
+                              a row stride of 2^24 or more, an output whose rows overlap or that starts where an operand
+                              does that other rows need */
 };
 
 /* One training iteration's variable trace (Section III-A), structure of arrays. */
@@ -393,7 +394,8 @@ int lap_plan_pool_orders(uint32_t n_vars, uint32_t n_steps, uint32_t B, const vo
  * multiples of a power of two, of the row's own for the latter: gradients that the type holds come out whatever the size of
  * what they are sums of.  Every sum has a fixed order: equal calls give
  * equal bits.  Rows are [batch, heads, length, head_dim] by strides, which also serve [batch, length, heads, head_dim];
- * inputs may be broadcast (stride 0).  Nothing is allocated, and all calls can be captured in a graph. */
+ * inputs may be broadcast (stride 0).  The outputs and the workspace of a call share no memory with its inputs or with each
+ * other (but weights may be before); most calls in which two of them start at one address are refused.  Nothing is allocated, and all calls can be captured in a graph. */
 enum { LAP_T_BF16 = 0, LAP_T_F16 = 1 };      /* bfloat16, IEEE binary16 */
 #define LAP_MAX_HEAD_DIM 128u
 
@@ -454,7 +456,7 @@ size_t lap_cache_workspace_bytes(const lap_cache *to);
  * `to`, whose further slots are marked empty (rows and weights 0, position -1).  Of the slots below lens[b] (NULL: all) that
  * are not empty those stay that hold the newest `recent` positions (position > newest - recent), then those of the highest
  * weight, equal ones by lower slot; a weight that is not a number is below all others.  1 <= keep <= to->slots, recent <=
- * keep.  lens_out [batch]: min(lens, keep).  The two caches have the same type and sizes but for slots, and do not overlap. */
+ * keep.  lens_out [batch]: min(lens, keep).  The two caches have the same type and sizes but for slots. */
 int lap_cache_evict(const lap_cache *from, const int32_t *lens, uint32_t keep, uint32_t recent, const lap_cache *to,
                     int32_t *lens_out, void *ws, size_t ws_bytes, void *hip_stream);
 

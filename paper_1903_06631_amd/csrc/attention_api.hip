@@ -3,6 +3,7 @@
 #include <stdio.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "../../include/lap.h"
 #include "attn_kernels.h"
@@ -81,6 +82,15 @@ int check_rows(const lap_rows *x, uint64_t batch, uint64_t heads, uint64_t len, 
         if (d[i].stride < 0 || d[i].stride % 8) return LAP_E_LAYOUT;
     if (len > 1 && x->row >= MAX_ROW_STRIDE) return LAP_E_LAYOUT;
     return output && rows_overlap(d, n, head_dim) ? LAP_E_LAYOUT : LAP_OK;
+}
+
+// An output that starts where something does that is read, or written, for other rows than those that are written.  (That
+// memory is shared in other ways is not looked for: rows of one tensor may stand between those of another.)
+int check_apart(const void *output, std::initializer_list<const void *> others)
+{
+    for (const void *x : others)
+        if (x && x == output) return LAP_E_LAYOUT;
+    return LAP_OK;
 }
 
 int check_shape(const lap_attention_shape *s)
@@ -179,6 +189,8 @@ int lap_attention(const lap_attention_shape *s, const lap_rows *q, const lap_row
     if (!rc && s->q_len && !lse) rc = LAP_E_NULL;
     if (!rc) rc = check_ws(ws, ws_bytes, up(lap::forward_workspace(shape_of(s))));
     if (rc || !s->q_len) return rc;
+    if (s->k_len) rc = check_apart(out->data, {k->data, v->data});
+    if (rc) return rc;
     LAP_HIP(lap::launch_attention(shape_of(s), queries_of(s, q), keys_of(s, k), keys_of(s, v), queries_of(s, out), lse, ws, (hipStream_t)hip_stream));
     return LAP_OK;
 }
@@ -198,6 +210,12 @@ int lap_attention_grad(const lap_attention_shape *s, const lap_rows *dout, const
     if (!rc && s->q_len && !lse) rc = LAP_E_NULL;
     if (!rc) rc = check_ws(ws, ws_bytes, ws_grad(s));
     if (rc || (!s->q_len && !s->k_len)) return rc;
+    if (s->q_len && s->k_len) {      // the first kernel writes dq while it streams k and v, the second dk and dv while it streams q and dout
+        rc = check_apart(dq->data, {q->data, dout->data, k->data, v->data, dk->data, dv->data});
+        if (!rc) rc = check_apart(dk->data, {q->data, dout->data, dv->data});
+        if (!rc) rc = check_apart(dv->data, {q->data, dout->data});
+        if (rc) return rc;
+    }
     LAP_HIP(lap::launch_attention_grad(shape_of(s), {queries_of(s, dout), queries_of(s, q), keys_of(s, k), keys_of(s, v), queries_of(s, out), queries_of(s, dq),
                                                      keys_of(s, dk), keys_of(s, dv), lse, (float *)ws, (float *)((char *)ws + ws_stats(s))}, (hipStream_t)hip_stream));
     return LAP_OK;
@@ -212,6 +230,8 @@ int lap_attention_weights(const lap_attention_shape *s, const lap_rows *q, const
     if (!rc && ((s->q_len && !lse) || (s->k_len && !weights))) rc = LAP_E_NULL;
     if (!rc) rc = check_ws(ws, ws_bytes, ws_weights(s));
     if (rc || !s->k_len) return rc;
+    if (s->q_len) rc = check_apart(weights, {lse, q->data, k->data});
+    if (rc) return rc;
     LAP_HIP(lap::launch_attention_weights(shape_of(s), queries_of(s, q), keys_of(s, k), lse, before, weights, (float *)ws, (hipStream_t)hip_stream));
     return LAP_OK;
 }
@@ -228,6 +248,7 @@ int lap_attention_step(const lap_attention_shape *s, const lap_rows *q, const la
     if (!rc) rc = check_rows(out, s->batch, s->q_heads, 1, s->head_dim, true);
     if (!rc && (!lse || (before != nullptr) != (weights != nullptr))) rc = LAP_E_NULL;
     if (!rc) rc = check_ws(ws, ws_bytes, ws_step(s));
+    if (!rc && s->k_len) rc = check_apart(out->data, {k->data, v->data});
     if (rc) return rc;
     const lap::StepShape p = step_of(s);
     const size_t heads = (size_t)s->batch * s->q_heads;
@@ -253,6 +274,13 @@ int lap_cache_evict(const lap_cache *from, const int32_t *lens, uint32_t keep, u
     if (keep == 0 || keep > to->slots || recent > keep) return LAP_E_SIZE;
     if ((from->slots && !from->weights) || !to->weights || !to->positions || !lens_out) return LAP_E_NULL;
     rc = check_ws(ws, ws_bytes, lap_cache_workspace_bytes(to));
+    if (!rc) rc = check_apart(to->k.data, {to->v.data});
+    if (!rc && from->slots) {
+        rc = check_apart(to->k.data, {from->k.data, from->v.data});
+        if (!rc) rc = check_apart(to->v.data, {from->k.data, from->v.data});
+        if (!rc) rc = check_apart(to->weights, {from->weights});
+        if (!rc) rc = check_apart(to->positions, {from->positions});
+    }
     if (rc) return rc;
     const lap::EvictShape s = {from->batch, from->kv_heads, from->slots, to->slots, from->head_dim, keep, recent, lens};
     LAP_HIP(lap::launch_cache_evict(s, slots_of(from, &from->k), slots_of(from, &from->v), from->weights, from->positions, slots_of(to, &to->k),
