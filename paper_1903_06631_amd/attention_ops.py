@@ -50,11 +50,12 @@ _calls = SimpleNamespace()      # the library's calls, which take those bytes
 
 
 def declare(lib) -> None:
-    global torch, _stream, _kinds
+    global torch, _stream, _device, _kinds
     import torch
     _kinds = {torch.bfloat16: 0, torch.float16: 1}
     # the handle alone, where torch has a call for it: a stream object takes 2 us to make
     _stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+    _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
     p, u32, size, rows, shape, cache = C.c_void_p, C.c_uint32, C.c_size_t, C.POINTER(_Rows), C.POINTER(_Shape), C.POINTER(_Cache)
     ws = [p, size, p]
     for name, result, args in (("lap_attention_workspace_bytes", size, [C.c_int, shape]),
@@ -76,6 +77,15 @@ def _lib():
     if binding._lib is None:
         binding.load_library()
     return _calls
+
+
+def _on(index: int, call, *args) -> int:
+    """The call with its tensors' GPU as the current one, which is where the library launches (every GPU's default stream has
+    the same handle)."""
+    if _device() == index:
+        return call(*args)
+    with torch.cuda.device(index):
+        return call(*args)
 
 
 def _done(rc: int, where: str, index: int, sync: bool) -> None:
@@ -170,9 +180,9 @@ def attention(q, k, v, *, causal: bool = False, window: int = 0, scale: Optional
     if out is None:
         out = dict(out=torch.empty_like(q), lse=q.new_empty(qs[:3], dtype=torch.float32))
     ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_FORWARD, s), index, q)
-    rc = lib.lap_attention(s, _rows(q, "q", t, qs, index), _rows(k, "k", t, kv, index), _rows(v, "v", t, kv, index),
-                           _rows(out["out"], "out", t, qs, index), _plain(out["lse"], "lse", torch.float32, qs[:3], index),
-                           at, have, _stream(index))
+    rc = _on(index, lib.lap_attention, s, _rows(q, "q", t, qs, index), _rows(k, "k", t, kv, index), _rows(v, "v", t, kv, index),
+             _rows(out["out"], "out", t, qs, index), _plain(out["lse"], "lse", torch.float32, qs[:3], index),
+             at, have, _stream(index))
     if rc or sync:
         _done(rc, "lap_attention", index, sync)
     return out
@@ -187,11 +197,11 @@ def attention_grad(dout, q, k, v, out, lse, *, causal: bool = False, window: int
     if grads is None:
         grads = dict(dq=torch.empty_like(q), dk=q.new_empty(kv), dv=q.new_empty(kv))
     ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_GRAD, s), index, q)
-    rc = lib.lap_attention_grad(s, _rows(dout, "dout", t, qs, index), _rows(q, "q", t, qs, index), _rows(k, "k", t, kv, index),
-                                _rows(v, "v", t, kv, index), _rows(out, "out", t, qs, index),
-                                _plain(lse, "lse", torch.float32, qs[:3], index), _rows(grads["dq"], "dq", t, qs, index),
-                                _rows(grads["dk"], "dk", t, kv, index), _rows(grads["dv"], "dv", t, kv, index),
-                                at, have, _stream(index))
+    rc = _on(index, lib.lap_attention_grad, s, _rows(dout, "dout", t, qs, index), _rows(q, "q", t, qs, index), _rows(k, "k", t, kv, index),
+             _rows(v, "v", t, kv, index), _rows(out, "out", t, qs, index),
+             _plain(lse, "lse", torch.float32, qs[:3], index), _rows(grads["dq"], "dq", t, qs, index),
+             _rows(grads["dk"], "dk", t, kv, index), _rows(grads["dv"], "dv", t, kv, index),
+             at, have, _stream(index))
     if rc or sync:
         _done(rc, "lap_attention_grad", index, sync)
     return grads
@@ -206,9 +216,9 @@ def attention_weights(q, k, lse, *, before=None, causal: bool = False, window: i
     if weights is None:
         weights = q.new_empty(kv, dtype=torch.float32)
     ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_WEIGHTS, s), index, q)
-    rc = lib.lap_attention_weights(s, _rows(q, "q", t, qs, index), _rows(k, "k", t, ks, index),
-                                   _plain(lse, "lse", torch.float32, qs[:3], index), _plain(before, "before", torch.float32, kv, index),
-                                   _plain(weights, "weights", torch.float32, kv, index), at, have, _stream(index))
+    rc = _on(index, lib.lap_attention_weights, s, _rows(q, "q", t, qs, index), _rows(k, "k", t, ks, index),
+             _plain(lse, "lse", torch.float32, qs[:3], index), _plain(before, "before", torch.float32, kv, index),
+             _plain(weights, "weights", torch.float32, kv, index), at, have, _stream(index))
     if rc or sync:
         _done(rc, "lap_attention_weights", index, sync)
     return dict(weights=weights)
@@ -232,10 +242,10 @@ def attention_step(q, k_cache, v_cache, weights=None, *, lens=None, positions=No
         out = dict(out=torch.empty_like(q), lse=q.new_empty((b, h), dtype=torch.float32),
                    weights=None if weights is None else q.new_empty(slots, dtype=torch.float32))
     ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_STEP, s), index, q)
-    rc = lib.lap_attention_step(s, _rows(q, "q", t, qs, index), _rows(k_cache, "k_cache", t, kv, index), _rows(v_cache, "v_cache", t, kv, index),
-                                _plain(positions, "positions", torch.int32, slots, index), _plain(weights, "weights", torch.float32, slots, index),
-                                _rows(out["out"], "out", t, qs, index), _plain(out["lse"], "lse", torch.float32, (b, h), index),
-                                _plain(out.get("weights"), "out weights", torch.float32, slots, index), at, have, _stream(index))
+    rc = _on(index, lib.lap_attention_step, s, _rows(q, "q", t, qs, index), _rows(k_cache, "k_cache", t, kv, index), _rows(v_cache, "v_cache", t, kv, index),
+             _plain(positions, "positions", torch.int32, slots, index), _plain(weights, "weights", torch.float32, slots, index),
+             _rows(out["out"], "out", t, qs, index), _plain(out["lse"], "lse", torch.float32, (b, h), index),
+             _plain(out.get("weights"), "out weights", torch.float32, slots, index), at, have, _stream(index))
     if rc or sync:
         _done(rc, "lap_attention_step", index, sync)
     return out
@@ -267,8 +277,8 @@ def cache_evict(k, v, weights, keep: int, recent: int, *, lens=None, positions=N
         _refuse("out k", out["k"], f"{k.dtype} on GPU {index}")
     dst = _cache(out["k"], out["v"], out["weights"], out["positions"], "out ")
     ws, have, at = _workspace(ws, lib.lap_cache_workspace_bytes(dst), index, k)
-    rc = lib.lap_cache_evict(src, _plain(lens, "lens", torch.int32, (b,), index), keep, recent, dst,
-                             _plain(out["lens"], "out lens", torch.int32, (b,), index), at, have, _stream(index))
+    rc = _on(index, lib.lap_cache_evict, src, _plain(lens, "lens", torch.int32, (b,), index), keep, recent, dst,
+             _plain(out["lens"], "out lens", torch.int32, (b,), index), at, have, _stream(index))
     if rc or sync:
         _done(rc, "lap_cache_evict", index, sync)
     return out
@@ -283,9 +293,9 @@ def cache_insert(k_new, v_new, k_cache, v_cache, weights, positions, position, r
     index = k_cache.get_device()
     if slots is None:
         slots = k_cache.new_empty((b, h), dtype=torch.int32)
-    rc = lib.lap_cache_insert(cache, _rows(k_new, "k_new", k_cache.dtype, (b, h, d), index), _rows(v_new, "v_new", k_cache.dtype, (b, h, d), index),
-                              _plain(position, "position", torch.int32, (b,), index), _count(recent, "recent"),
-                              _plain(slots, "slots", torch.int32, (b, h), index), _stream(index))
+    rc = _on(index, lib.lap_cache_insert, cache, _rows(k_new, "k_new", k_cache.dtype, (b, h, d), index), _rows(v_new, "v_new", k_cache.dtype, (b, h, d), index),
+             _plain(position, "position", torch.int32, (b,), index), _count(recent, "recent"),
+             _plain(slots, "slots", torch.int32, (b, h), index), _stream(index))
     if rc or sync:
         _done(rc, "lap_cache_insert", index, sync)
     return dict(slots=slots)
