@@ -45,7 +45,9 @@ class Recorder:
 def record(layers, batch, heads, tokens, size, keep_probabilities):
     """Attention alone: layer l runs forward at step l and backward at step 2 layers - 1 - l."""
     r, steps = Recorder(), 2 * layers
-    rows, numbers = batch * heads * tokens * size * 2, batch * heads * tokens * 4
+    shape, numbers = (batch, heads, tokens, size), batch * heads * tokens * 4
+    rows = math.prod(shape) * 2
+    ws = [lap.attention_workspace_bytes(call, shape, shape, torch.bfloat16, causal=True) for call in (lap.AT_FORWARD, lap.AT_GRAD)]
     for l in range(layers):
         back = steps - 1 - l
         for name in ("q", "k", "v", "out"):
@@ -56,7 +58,8 @@ def record(layers, batch, heads, tokens, size, keep_probabilities):
             r.add(f"dp{l}", rows // size * tokens, back, back + 1)
         else:
             r.add(f"lse{l}", numbers, l, back + 1)
-            r.add(f"ws{l}", 2 * numbers + 256, back, back + 1)
+            r.add(f"forward ws{l}", ws[0], l, l + 1)
+            r.add(f"ws{l}", ws[1], back, back + 1)
         for name in ("dout", "dq", "dk", "dv"):
             r.add(f"{name}{l}", rows, back, min(back + 2, steps))
     return r, r.trace(steps)
@@ -93,7 +96,7 @@ def train(layers=4, batch=2, heads=8, tokens=1024, size=64):
     for l in range(layers):
         for name, x in zip("qkv", given[l]):
             at(f"{name}{l}").copy_(x)
-        lap.attention(at(f"q{l}"), at(f"k{l}"), at(f"v{l}"), causal=True, sync=False,
+        lap.attention(at(f"q{l}"), at(f"k{l}"), at(f"v{l}"), causal=True, sync=False, ws=at(f"forward ws{l}", torch.uint8),
                       out=dict(out=at(f"out{l}"), lse=at(f"lse{l}", torch.float32, shape[:3])))
     grads = []
     for l in reversed(range(layers)):

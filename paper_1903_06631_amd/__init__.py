@@ -33,10 +33,15 @@ from .binding import (  # noqa: F401
     workspace_bytes,
 )
 from .attention_ops import (  # noqa: F401
+    AT_FORWARD,
+    AT_GRAD,
+    AT_STEP,
+    AT_WEIGHTS,
     attention,
     attention_grad,
     attention_step,
     attention_weights,
+    attention_workspace_bytes,
     cache_evict,
     cache_insert,
 )

@@ -4,7 +4,8 @@ Tensors are [batch, heads, length, head_dim] in torch.bfloat16 or torch.float16 
 strides are free (a [batch, length, heads, head_dim] tensor goes in as its transpose(1, 2)).  Lengths, positions and slots
 are torch.int32, weights and logarithms of softmax sums torch.float32, all contiguous.  Work is enqueued on the current
 stream of q's device; `sync=False` returns without waiting for it.  `out` takes result tensors that the caller owns, `ws` a
-workspace (uint8, at least as large as the call asks for).  What a library call cannot see (types, shapes, devices) raises
+workspace (uint8, 256-byte aligned, at least attention_workspace_bytes; cache_evict: 4 bytes for every slot of the new cache,
+rounded up to a multiple of 256).  What a library call cannot see (types, shapes, devices) raises
 ValueError here; the rest is LapError from the library.
 """
 from __future__ import annotations
@@ -170,6 +171,15 @@ def _workspace(ws, need: int, index: int, like):
     elif ws.dtype is not torch.uint8 or ws.get_device() != index or not ws.is_contiguous():
         _refuse("ws", ws, f"a contiguous torch.uint8 on GPU {index}")
     return ws, ws.numel(), ws.data_ptr()
+
+
+def attention_workspace_bytes(which: int, q_shape, kv_shape, dtype, *, causal: bool = False) -> int:
+    """lap_attention_workspace_bytes: of a call (AT_FORWARD, AT_GRAD, AT_WEIGHTS, AT_STEP) on queries and keys of these shapes,
+    [batch, heads, length, head_dim], for a step's queries without a length.  0: none, also where the call is refused."""
+    lib = _lib()
+    b, h, *n, d = q_shape
+    s = _pack_shape(_kinds[dtype], b, h, kv_shape[1], n[0] if n else 1, kv_shape[2], d, 1 if causal else 0, 0, 1.0, 0, 0)
+    return int(lib.lap_attention_workspace_bytes(which, s))
 
 
 def attention(q, k, v, *, causal: bool = False, window: int = 0, scale: Optional[float] = None, q_lens=None, k_lens=None,

@@ -88,3 +88,12 @@ def test_results_with_strides_that_are_not_used():
         assert torch.equal(a["out"], b["out"]) and torch.equal(a["lse"], b["lse"])
         a, b = lap.attention_grad(g, q, k, v, a["out"], a["lse"]), lap.attention_grad(odd[3], *odd[:3], a["out"], a["lse"])
         assert all(torch.equal(a[x], b[x]) for x in a)
+
+
+def test_workspaces_by_shape(lib):
+    import paper_1903_06631_amd as lap
+    q, kv = (2, 4, 5, 64), (2, 2, 7, 64)
+    for which in range(4):
+        assert lap.attention_workspace_bytes(which, q, kv, torch.bfloat16, causal=True) == lib.lap_attention_workspace_bytes(which, shape())
+    long = shape(type=1, q_len=1, k_len=3000, causal=0)
+    assert lap.attention_workspace_bytes(lap.AT_STEP, (2, 4, 64), (2, 2, 3000, 64), torch.float16) == lib.lap_attention_workspace_bytes(3, long) > 0
