@@ -141,7 +141,7 @@ def _four(x, name: str):
 
 
 def _count(x, name: str) -> int:
-    if not 0 <= x <= 0xFFFFFFFF:      # what the library takes; its own limits are lower
+    if not 0 <= x <= 0xFFFFFFFF or int(x) != x:      # what the library takes; its own limits are lower
         raise ValueError(f"{name} is a number of keys or slots, not {x}")
     return int(x)
 
@@ -280,7 +280,7 @@ def cache_evict(k, v, weights, keep: int, recent: int, *, lens=None, positions=N
     b, h, n, d = k.shape
     index = k.get_device()
     if out is None:
-        m = keep if slots is None else int(slots)
+        m = keep if slots is None else _count(slots, "slots")
         out = dict(k=k.new_empty((b, h, m, d)), v=k.new_empty((b, h, m, d)), weights=k.new_empty((b, h, m), dtype=torch.float32),
                    positions=k.new_empty((b, h, m), dtype=torch.int32), lens=k.new_empty(b, dtype=torch.int32))
     if out["k"].dtype is not k.dtype or out["k"].get_device() != index:
