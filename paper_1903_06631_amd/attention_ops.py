@@ -5,13 +5,16 @@ strides are free (a [batch, length, heads, head_dim] tensor goes in as its trans
 are torch.int32, weights and logarithms of softmax sums torch.float32, all contiguous.  Work is enqueued on the current
 stream of q's device; `sync=False` returns without waiting for it.  `out` takes result tensors that the caller owns, `ws` a
 workspace (uint8, 256-byte aligned, at least attention_workspace_bytes; cache_evict: 4 bytes for every slot of the new cache,
-rounded up to a multiple of 256).  What a library call cannot see (types, shapes, devices) raises
+rounded up to a multiple of 256).  Autograd does not see these calls: their results have no gradient, attention_grad computes
+it, and a torch.autograd.Function around the two is the caller's (a result that would be expected to have one is warned of).
+What a library call cannot see (types, shapes, devices) raises
 ValueError here; the rest is LapError from the library.
 """
 from __future__ import annotations
 
 import ctypes as C
 import struct
+import warnings
 from types import SimpleNamespace
 from typing import Optional
 
@@ -87,6 +90,11 @@ def _on(index: int, call, *args) -> int:
         return call(*args)
     with torch.cuda.device(index):
         return call(*args)
+
+
+def _warn_of_autograd(name: str, where: str) -> None:
+    if torch.is_grad_enabled():
+        warnings.warn(f"{name}: the result has no gradient for autograd; {where}", stacklevel=3)
 
 
 def _done(rc: int, where: str, index: int, sync: bool) -> None:
@@ -184,8 +192,11 @@ def attention_workspace_bytes(which: int, q_shape, kv_shape, dtype, *, causal: b
 
 def attention(q, k, v, *, causal: bool = False, window: int = 0, scale: Optional[float] = None, q_lens=None, k_lens=None,
               out: Optional[dict] = None, ws=None, sync: bool = True):
-    """lap_attention: returns dict(out like q, lse [batch, q_heads, q_len]).  scale None: 1 / sqrt(head_dim)."""
+    """lap_attention: returns dict(out like q, lse [batch, q_heads, q_len]), without gradients for autograd.  scale None:
+    1 / sqrt(head_dim)."""
     lib = _lib()
+    if q.requires_grad or k.requires_grad or v.requires_grad:
+        _warn_of_autograd("attention", "attention_grad computes that of q, k and v")
     s, t, qs, kv, index = _shape(q, k, causal, window, scale, q_lens, k_lens)
     if out is None:
         out = dict(out=torch.empty_like(q), lse=q.new_empty(qs[:3], dtype=torch.float32))
@@ -240,6 +251,8 @@ def attention_step(q, k_cache, v_cache, weights=None, *, lens=None, positions=No
     dict(out like q, lse [batch, q_heads], weights = the given ones + this token's, a new tensor unless out holds one; None
     where none are given)."""
     lib = _lib()
+    if q.requires_grad or k_cache.requires_grad or v_cache.requires_grad:
+        _warn_of_autograd("attention_step", "there is none of a step")
     if q.dim() != 3:
         _refuse("q", q, "[batch, heads, head_dim]")
     qs, ks = q.shape, _four(k_cache, "k_cache")
