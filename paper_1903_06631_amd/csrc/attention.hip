@@ -2,7 +2,9 @@
 // of the sum of exp(scale q_i.k_j) over the keys that row i sees.
 //
 // One pass over the keys with a running maximum m and sum l for every row: a tile of keys gives s = K Q^T, p = 2^(c s - c m)
-// with c = scale log2(e), l += sum p, O^T += V^T P^T.  Nothing of the size queries x keys is ever stored.  Where there are few
+// with c = scale log2(e), l += sum p, O^T += V^T P^T.  The matrix instruction takes p in the values' type: each is off by half a
+// unit of that at most, as each value is already, and a product of 32-bit operands runs at a sixteenth of the rate; l is the sum
+// of the unrounded ones, so that lse has 32 bits.  Nothing of the size queries x keys is ever stored.  Where there are few
 // rows and many keys, the keys are cut into parts, a workgroup each, which leave m, l and O in the workspace for a second
 // kernel to join.
 //

@@ -1,6 +1,8 @@
 // Attention's backward pass.  With p_ij = exp(scale q_i.k_j - lse_i) computed again from the rows and the forward pass's
 // sums, g_i the gradient of o_i and delta_i = g_i.o_i:
 //   dv_j = sum_i p_ij g_i      ds_ij = p_ij (g_i.v_j - delta_i)      dq_i = scale sum_j ds_ij k_j      dk_j = scale sum_i ds_ij q_i
+// p and ds are rounded to the rows' type where they enter a product, which is what the matrix instruction takes (in binary16 as
+// multiples of a power of two: hold_in_range); scores, g.v, p and ds themselves and all sums are 32 bits.
 //
 // Two kernels, each with its sums in registers from the first product to the last, added in a fixed order: one keeps
 // query rows and streams keys (dq; it also leaves delta and the sums in base 2 in the workspace), the other keeps keys and

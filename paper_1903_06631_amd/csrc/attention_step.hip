@@ -1,6 +1,9 @@
 // Attention of one new token of every sequence over its cache, and the weight that every slot receives from it:
 //   o = sum_j p_j v_j, p_j = exp(scale q.k_j - lse), over the slots in use; w_j += sum of p_j over the heads that share slot j
 //
+// p is rounded to the values' type for its product with them (a matrix operand); in binary16, those below 2^-25 of the largest
+// of their wave, which has up to 512 slots, vanish: less than 2^-16 of the row.  Sums, scores and weights are 32 bits.
+//
 // Every key and value is read once and takes part in a few products only: the pass is bound by memory.  Waves go through 32
 // slots at a time of their own, without waiting for each other: keys from memory straight into registers as a matrix operand,
 // values through LDS, which is where they are transposed.  The heads of a group are the kept rows (up to 32; with fewer,

@@ -126,8 +126,7 @@ __global__ __launch_bounds__(EV) void k_evict(EvictShape s, Rows k, Rows v, cons
     uint32_t bound = LEAST, equal = 0xFFFFFFFFu;      // all slots in use
     if (keep < used) {
         uint32_t prefix = 0, mask = 0, want = (uint32_t)keep;      // of the slots whose key begins with prefix, the want-th
-        if (want == 0) bound = NEWEST, equal = 0;
-        for (int digit = 0; want && digit < 3; ++digit) {
+        for (int digit = 0; digit < 3; ++digit) {
             const int shift = digit == 0 ? 19 : digit == 1 ? 6 : 0;
             const uint32_t ones = digit == 2 ? 63 : BINS - 1;
             for (int i = t; i < BINS; i += EV) bins[i] = 0;
@@ -168,7 +167,7 @@ __global__ __launch_bounds__(EV) void k_evict(EvictShape s, Rows k, Rows v, cons
                 break;
             }
         }
-        if (mask) bound = prefix, equal = want;
+        bound = prefix, equal = want;
     }
 
     // how many of every wave's are above the bound and at it, then the places
