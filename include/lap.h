@@ -388,7 +388,8 @@ int lap_plan_pool_orders(uint32_t n_vars, uint32_t n_steps, uint32_t B, const vo
  *     i + k_lens[b] - q_lens[b].
  *   - causal: a row sees the keys up to where it stands; with window > 0 only the last `window` of those.
  *   - A row that sees no key, and a row beyond its sequence's length, has o = 0, lse = minus infinity and gradients of 0.
- *     A key with q.k below -1e30 counts as hidden, whatever the scale.  A value that is not finite reaches the rows that see it and no others.
+ *     A key with q.k below -1e30 counts as hidden, whatever the scale.  A value that is not finite reaches the rows that see
+ *     it and no others.
  * Sums, scores and probabilities are held in 32 bits; probabilities and their gradients are rounded to the element type
  * where they enter the next product, results once when they are written.  In the backward pass on binary16 both enter it as
  * multiples of a power of two, of the row's own for the latter: gradients that the type holds come out whatever the size of
@@ -456,7 +457,8 @@ size_t lap_cache_workspace_bytes(const lap_cache *to);
  * `to`, whose further slots are marked empty (rows and weights 0, position -1).  Of the slots below lens[b] (NULL: all) that
  * are not empty those stay that hold the newest `recent` positions (position > newest - recent), then those of the highest
  * weight, equal ones by lower slot; a weight that is not a number is below all others.  1 <= keep <= to->slots, recent <=
- * keep.  lens_out [batch]: min(lens, keep).  The two caches have the same type and sizes but for slots. */
+ * keep.  lens_out [batch]: min(lens, keep), for all heads alike: a head with
+ * fewer slots in use has empty ones below that, which `positions` tells a step and lens does not.  The two caches have the same type and sizes but for slots. */
 int lap_cache_evict(const lap_cache *from, const int32_t *lens, uint32_t keep, uint32_t recent, const lap_cache *to,
                     int32_t *lens_out, void *ws, size_t ws_bytes, void *hip_stream);
 

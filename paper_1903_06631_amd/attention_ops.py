@@ -286,7 +286,8 @@ def _cache(k, v, weights, positions, name: str = ""):
 def cache_evict(k, v, weights, keep: int, recent: int, *, lens=None, positions=None, slots: Optional[int] = None,
                 out: Optional[dict] = None, ws=None, sync: bool = True):
     """lap_cache_evict: the `keep` rows of highest weight of k and v, the newest `recent` among them, into a cache of `slots`
-    (None: keep).  Returns dict(k, v, weights, positions [batch, kv_heads, slots], lens [batch])."""
+    (None: keep).  Returns dict(k, v, weights, positions [batch, kv_heads, slots], lens [batch]: the lengths given, up to keep).
+    Where a head has fewer slots in use than that, only `positions` tells attention_step which are empty."""
     lib = _lib()
     src = _cache(k, v, weights, positions)
     keep, recent = _count(keep, "keep"), _count(recent, "recent")

@@ -14,8 +14,12 @@
 // 13370 keys, causal, 1.36 ms = 1070 TFLOP/s, 88 % of what a large matrix product reaches on the same card, with the matrix
 // unit busy in 60 % of the cycles and the clock down to 1.7 GHz: bound by power, and other orders of the instructions (scores
 // of the next tile worked out beside the exponentials, products and vector instructions dealt out by hand) came out within
-// 3 % or worse.  8 x 16 heads x 2048 tokens, causal: 160 us = 860 TFLOP/s; 6 % of it is the diagonal's hidden half tiles and
-// as much the starts and ends of workgroups with 2 to 32 tiles.
+// 3 % or worse.  Shorter rows are slower, causal ones most (16 heads of 128 elements, TFLOP/s of the visible pairs):
+//   tokens       8 x 1024   8 x 2048   8 x 4096   4 x 8192   1 x 16384
+//   causal            608        866        941       1042        1064
+//   all keys          826        989       1007       1076        1069
+// Starts and ends of workgroups are what shorter rows without a mask lose.  Causal ones lose 12 % more at 2048 tokens: 6 % are the
+// diagonal's hidden pairs and the waves that wait for the last of four there, the rest is not accounted for.
 #include <type_traits>
 
 #include "attn_core.h"

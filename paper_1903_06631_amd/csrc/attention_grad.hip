@@ -10,9 +10,10 @@
 // in place of five: the price for results that do not depend on the order in which workgroups finish.  Where there are few
 // keys and many rows, the second kernel's rows are cut into parts, whose sums a third adds in order.
 //
-// Measured, 8 x 16 heads x 2048 tokens x 128, causal: 230 + 300 us = 650 TFLOP/s of the five products that a backward pass cannot
-// do without (910 of the seven), the matrix units busy in 45 % of the cycles at 2.0 GHz: bound by power as the forward pass is.
-// 6 ragged sequences of up to 1001 tokens, 12 heads on 4: 35 + 55 us, bound by the longest workgroup's chain of tiles.
+// Measured, 8 x 16 heads x 2048 tokens x 128, causal, bfloat16: 228 + 313 us = 635 TFLOP/s of the five products that a backward
+// pass cannot do without (890 of the seven), the matrix units busy in 44 % of the cycles at 2.0 GHz.  6 ragged sequences of up to
+// 1001 tokens x 80, 12 heads on 4, binary16: 36 + 59 us, with the compute units busy in 48 % of the cycles: bound by the longest
+// workgroup's chain of tiles, a third of whose products are of the padding to 128 elements.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>

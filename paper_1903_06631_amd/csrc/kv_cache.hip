@@ -5,8 +5,10 @@
 // of that order and copies them, in the order of their slots, into another cache; an insertion overwrites the first.
 //
 // Measured: 8 ragged prompts of up to 16384 tokens, 8 heads, into 2048 slots of 128 elements, 32 us: the choice is a chain of some
-// 18 in the longest rows (2.6 to read 16384 weights, 6 for the first digit of the search, 4 for the others, 5 to place), while
-// shorter ones are copied (134 MB read and written in all, 20 us alone).  An insertion into 64 x 8 caches of 2048 slots 4.7 us,
+// 18 in the longest rows (by leaving its steps out one by one: 2.6 to read 16384 weights, 6 for the first digit of the search, 4
+// for the others, 5 to place), while shorter ones are copied (134 MB read and written in all, 20 us alone); waves wait in 62 % of
+// their cycles.  Rows that do not fit into registers: 8 heads of 60000 slots into 8000 76 us, where every workgroup of a row
+// reads its weights up to five times.  An insertion into 64 x 8 caches of 2048 slots 4.7 us,
 // most of it a launch and three dependent accesses.
 #include "attn_core.h"
 #include "lap_dev.h"
