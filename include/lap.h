@@ -397,7 +397,8 @@ int lap_plan_pool_orders(uint32_t n_vars, uint32_t n_steps, uint32_t B, const vo
  * equal bits.  Rows are [batch, heads, length, head_dim] by strides, which also serve [batch, length, heads, head_dim];
  * inputs may be broadcast (stride 0).  The outputs and the workspace of a call share no memory with its inputs or with each
  * other (but weights may be before); most calls in which two of them start at one address are refused.  Nothing is allocated, and all calls can be captured in a graph. */
-enum { LAP_T_BF16 = 0, LAP_T_F16 = 1 };      /* bfloat16, IEEE binary16 */
+enum { LAP_T_BF16 = 0, LAP_T_F16 = 1,      /* bfloat16, IEEE binary16 */
+       LAP_T_BYTES = 2 };                  /* of a lap_cache alone: packed rows, below */
 #define LAP_MAX_HEAD_DIM 128u
 
 typedef struct {
@@ -416,7 +417,7 @@ typedef struct {
 } lap_attention_shape;
 
 /* Bytes of workspace of a call with this shape, 256-byte aligned (0: ws may be NULL; also for a shape that is refused). */
-enum { LAP_AT_FORWARD = 0, LAP_AT_GRAD = 1, LAP_AT_WEIGHTS = 2, LAP_AT_STEP = 3 };
+enum { LAP_AT_FORWARD = 0, LAP_AT_GRAD = 1, LAP_AT_WEIGHTS = 2, LAP_AT_STEP = 3, LAP_AT_STEP_PACKED = 4 };
 size_t lap_attention_workspace_bytes(int which_call, const lap_attention_shape *shape);
 
 /* out, and lse [batch, q_heads, q_len], which the backward pass and lap_attention_weights take. */
@@ -442,7 +443,8 @@ int lap_attention_step(const lap_attention_shape *shape, const lap_rows *q, cons
                        const int32_t *positions, const float *before, const lap_rows *out, float *lse, float *weights,
                        void *ws, size_t ws_bytes, void *hip_stream);
 
-/* A cache of one layer: `slots` places for every sequence and key head. */
+/* A cache of one layer: `slots` places for every sequence and key head.  Packed rows are moved as they are: type LAP_T_BYTES,
+ * with head_dim (and the strides of k and v, and of the rows put into the cache) in bytes, multiples of 16. */
 typedef struct {
     uint32_t type, batch, kv_heads, slots, head_dim;      /* batch * kv_heads up to 65535 */
     lap_rows k, v;
@@ -468,6 +470,42 @@ int lap_cache_evict(const lap_cache *from, const int32_t *lens, uint32_t keep, u
  * ones.  A sequence with position[b] < 0 is left alone.  recent <= slots.  slots_out [batch, kv_heads]: the slot, or -1. */
 int lap_cache_insert(const lap_cache *cache, const lap_rows *k_new, const lap_rows *v_new, const int32_t *position,
                      uint32_t recent, int32_t *slots_out, void *hip_stream);
+
+/* ---- A cache in 4 or 8 bits an element -------------------------------------------------------------------------------
+ *
+ * The limit on a cache may also be held by the bits of an element: of 128 elements a row is 80 bytes in 4 bits and 144 in 8, in
+ * place of 256.  Elements of a row come in groups of 32, the last one perhaps shorter.  Of L = 2^bits - 1 levels, lo the least
+ * element of a group and step the least number of the elements' type from (largest - least) / L on (the one below where
+ * lo + L step would pass the type's largest), element x is held as u, the whole number nearest to (x - lo) / step, ties to even,
+ * and stands for lo + u step, rounded once to the type; quotients and differences are 32-bit ones.  A group with an element that
+ * is not finite, or a range over 2^100, is not a number, all of it.  A row's bytes: the words of 32 bits of each group, `bits` of
+ * them, whose low half holds the even elements from its lowest bits up and whose high half the odd ones; then lo and step of each
+ * group, 16 bits each; then zeros up to a multiple of 16. */
+typedef struct {
+    uint32_t type, bits;                                   /* of the elements, LAP_T_BF16 or LAP_T_F16; 4 or 8 */
+    uint32_t batch, kv_heads, slots, head_dim;             /* batch * kv_heads up to 65535, head_dim a multiple of 8 up to 128 */
+    lap_rows k, v;                                         /* rows of lap_packed_row_bytes; strides in BYTES, multiples of 16 */
+} lap_packed_cache;
+
+/* Bytes of a packed row (0: refused). */
+size_t lap_packed_row_bytes(uint32_t bits, uint32_t head_dim);
+
+/* Rows k and v [batch, kv_heads, n] into the cache: row i of sequence b into slot first[b] + i, for i below lens[b] (device, NULL:
+ * n; 0).  Rows whose slot the cache does not have go nowhere; slots that no row goes to are left as they are. */
+int lap_cache_pack(const lap_packed_cache *to, const lap_rows *k, const lap_rows *v, uint32_t n, const int32_t *lens,
+                   const int32_t *first, void *hip_stream);
+
+/* What the slots first[b] + i, i below lens[b], stand for, as rows k and v [batch, kv_heads, n]; zeros in the other rows. */
+int lap_cache_unpack(const lap_packed_cache *from, uint32_t n, const int32_t *lens, const int32_t *first, const lap_rows *k,
+                     const lap_rows *v, void *hip_stream);
+
+/* lap_attention_step on a packed cache, for q_len new tokens of every sequence, whose keys and values are its last q_len slots
+ * in use: shape with the cache's sizes, k_len its slots, window 0 and up to 256 rows (query heads times q_len) to a key
+ * head.  With q_len > 1, causal is 1 (row i of a sequence sees the slots below k_lens[b] - q_lens[b] + i + 1) and positions NULL; with
+ * q_len 1 causal may be either.  lse [batch, q_heads, q_len]; weights are the sums over all heads and rows of the call. */
+int lap_attention_step_packed(const lap_attention_shape *shape, const lap_rows *q, const lap_packed_cache *cache,
+                              const int32_t *positions, const float *before, const lap_rows *out, float *lse, float *weights,
+                              void *ws, size_t ws_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

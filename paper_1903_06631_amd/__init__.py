@@ -36,14 +36,19 @@ from .attention_ops import (  # noqa: F401
     AT_FORWARD,
     AT_GRAD,
     AT_STEP,
+    AT_STEP_PACKED,
     AT_WEIGHTS,
     attention,
     attention_grad,
     attention_step,
+    attention_step_packed,
     attention_weights,
     attention_workspace_bytes,
     cache_evict,
     cache_insert,
+    cache_pack,
+    cache_unpack,
+    packed_row_bytes,
 )
 
 ORD_SIZE_DESC, ORD_LIFE_DESC, ORD_AREA_DESC, ORD_ALLOC_ASC, ORD_SEEDED, ORD_EXPLICIT, ORD_CLASS_SEEDED = range(7)

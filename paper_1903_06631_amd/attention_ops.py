@@ -9,6 +9,9 @@ rounded up to a multiple of 256).  Autograd does not see these calls: their resu
 it, and a torch.autograd.Function around the two is the caller's (a result that would be expected to have one is warned of).
 What a library call cannot see (types, shapes, devices) raises
 ValueError here; the rest is LapError from the library.
+
+A cache in 4 or 8 bits an element is a pair of torch.uint8 tensors [batch, kv_heads, slots, packed_row_bytes], strides that are
+multiples of 16; a call knows the bits by that size.  cache_evict and cache_insert take such rows as well.
 """
 from __future__ import annotations
 
@@ -20,7 +23,7 @@ from typing import Optional
 
 from . import binding
 
-AT_FORWARD, AT_GRAD, AT_WEIGHTS, AT_STEP = range(4)
+AT_FORWARD, AT_GRAD, AT_WEIGHTS, AT_STEP, AT_STEP_PACKED = range(5)
 
 
 class _Rows(C.Structure):
@@ -38,6 +41,11 @@ class _Cache(C.Structure):
                 ("head_dim", C.c_uint32), ("k", _Rows), ("v", _Rows), ("weights", C.c_void_p), ("positions", C.c_void_p)]
 
 
+class _Packed(C.Structure):
+    _fields_ = [("type", C.c_uint32), ("bits", C.c_uint32), ("batch", C.c_uint32), ("kv_heads", C.c_uint32), ("slots", C.c_uint32),
+                ("head_dim", C.c_uint32), ("k", _Rows), ("v", _Rows)]
+
+
 torch = None      # set when the library is loaded, which loads torch first
 
 # The same structures as bytes, which a call's arguments are put together from: that and its checks are what the smallest
@@ -46,21 +54,26 @@ _pack_rows = struct.Struct("@P3q").pack
 _pack_shape = struct.Struct("@9If2P").pack
 _pack_cache = struct.Struct("@5I4x").pack
 _pack_two = struct.Struct("@2P").pack
+_pack_packed = struct.Struct("@6I").pack
 _NOWHERE = _pack_rows(0, 0, 0, 0)
 assert len(_NOWHERE) == C.sizeof(_Rows) and len(_pack_shape(*[0] * 12)) == C.sizeof(_Shape)
 assert len(_pack_cache(*[0] * 5) + 2 * _NOWHERE + _pack_two(0, 0)) == C.sizeof(_Cache)
+assert len(_pack_packed(*[0] * 6) + 2 * _NOWHERE) == C.sizeof(_Packed)
 
 _calls = SimpleNamespace()      # the library's calls, which take those bytes
 
 
 def declare(lib) -> None:
-    global torch, _stream, _device, _kinds
+    global torch, _stream, _device, _kinds, _moved
     import torch
     _kinds = {torch.bfloat16: 0, torch.float16: 1}
+    _moved = dict(_kinds)
+    _moved[torch.uint8] = 2
     # the handle alone, where torch has a call for it: a stream object takes 2 us to make
     _stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
     _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
     p, u32, size, rows, shape, cache = C.c_void_p, C.c_uint32, C.c_size_t, C.POINTER(_Rows), C.POINTER(_Shape), C.POINTER(_Cache)
+    packed = C.POINTER(_Packed)
     ws = [p, size, p]
     for name, result, args in (("lap_attention_workspace_bytes", size, [C.c_int, shape]),
                                ("lap_cache_workspace_bytes", size, [cache]),
@@ -69,11 +82,15 @@ def declare(lib) -> None:
                                ("lap_attention_weights", C.c_int, [shape, rows, rows, p, p, p] + ws),
                                ("lap_attention_step", C.c_int, [shape, rows, rows, rows, p, p, rows, p, p] + ws),
                                ("lap_cache_evict", C.c_int, [cache, p, u32, u32, cache, p] + ws),
-                               ("lap_cache_insert", C.c_int, [cache, rows, rows, p, u32, p, p])):
+                               ("lap_cache_insert", C.c_int, [cache, rows, rows, p, u32, p, p]),
+                               ("lap_packed_row_bytes", size, [u32, u32]),
+                               ("lap_cache_pack", C.c_int, [packed, rows, rows, u32, p, p, p]),
+                               ("lap_cache_unpack", C.c_int, [packed, u32, p, p, rows, rows, p]),
+                               ("lap_attention_step_packed", C.c_int, [shape, rows, packed, p, p, rows, p, p] + ws)):
         call = getattr(lib, name)
         call.restype, call.argtypes = result, args
         call = lib[name]
-        call.restype, call.argtypes = result, [p if x in (rows, shape, cache) else x for x in args]
+        call.restype, call.argtypes = result, [p if x in (rows, shape, cache, packed) else x for x in args]
         setattr(_calls, name, call)
 
 
@@ -130,12 +147,12 @@ def _plain(x, name: str, dtype, shape, index: int):
     return x.data_ptr()
 
 
-def _type(x, name: str):
+def _type(x, name: str, kinds=None):
     """lap's number for x's type, the type, the GPU."""
     t, index = x.dtype, x.get_device()
-    kind = _kinds.get(t)
+    kind = (kinds or _kinds).get(t)
     if kind is None:
-        _refuse(name, x, "torch.bfloat16 or torch.float16")
+        _refuse(name, x, "torch.bfloat16 or torch.float16" + (" (packed rows: torch.uint8)" if kinds else ""))
     if index < 0:
         _refuse(name, x, "a tensor on the GPU")
     return kind, t, index
@@ -182,11 +199,13 @@ def _workspace(ws, need: int, index: int, like):
 
 
 def attention_workspace_bytes(which: int, q_shape, kv_shape, dtype, *, causal: bool = False) -> int:
-    """lap_attention_workspace_bytes: of a call (AT_FORWARD, AT_GRAD, AT_WEIGHTS, AT_STEP) on queries and keys of these shapes,
-    [batch, heads, length, head_dim], for a step's queries without a length.  0: none, also where the call is refused."""
+    """lap_attention_workspace_bytes: of a call (AT_FORWARD, AT_GRAD, AT_WEIGHTS, AT_STEP, AT_STEP_PACKED) on queries and keys of
+    these shapes, [batch, heads, length, head_dim], for a step's queries without a length.  dtype and head_dim are the elements',
+    also of a packed cache.  0: none, also where the call is refused."""
     lib = _lib()
     b, h, *n, d = q_shape
-    s = _pack_shape(_kinds[dtype], b, h, kv_shape[1], n[0] if n else 1, kv_shape[2], d, 1 if causal else 0, 0, 1.0, 0, 0)
+    s = _pack_shape(_kinds[dtype], b, h, kv_shape[1], n[0] if n else 1, kv_shape[2], d, 1 if causal or which == AT_STEP_PACKED else 0, 0,
+                    1.0, 0, 0)
     return int(lib.lap_attention_workspace_bytes(which, s))
 
 
@@ -276,7 +295,7 @@ def attention_step(q, k_cache, v_cache, weights=None, *, lens=None, positions=No
 
 def _cache(k, v, weights, positions, name: str = ""):
     b, h, n, d = shape = _four(k, name + "k")
-    kind, t, index = _type(k, name + "k")
+    kind, t, index = _type(k, name + "k", _moved)
     slots = (b, h, n)
     return (_pack_cache(kind, b, h, n, d) + _rows(k, name + "k", t, shape, index) + _rows(v, name + "v", t, shape, index)
             + _pack_two(_plain(weights, name + "weights", torch.float32, slots, index) or 0,
@@ -323,3 +342,112 @@ def cache_insert(k_new, v_new, k_cache, v_cache, weights, positions, position, r
     if rc or sync:
         _done(rc, "lap_cache_insert", index, sync)
     return dict(slots=slots)
+
+
+_row_bits = {}      # (bytes of a row, head_dim): bits
+
+
+def packed_row_bytes(bits: int, head_dim: int) -> int:
+    """lap_packed_row_bytes: of a row of head_dim elements in 4 or 8 bits each."""
+    need = int(_lib().lap_packed_row_bytes(_count(bits, "bits"), _count(head_dim, "head_dim")))
+    if not need:
+        raise ValueError(f"there are no packed rows of {head_dim} elements in {bits} bits: 4 or 8 bits, a multiple of 8 up to 128 elements")
+    return need
+
+
+def _packed(kind: int, d: int, k, v, index: int, name: str = ""):
+    """lap_packed_cache of rows of bytes that stand for d elements each, the shape of the rows."""
+    b, h, n, row = shape = _four(k, name + "k_cache")
+    bits = _row_bits.get((row, d))
+    if bits is None:
+        for bits in (4, 8):
+            if _lib().lap_packed_row_bytes(bits, d) == row:
+                break
+        else:
+            _refuse(name + "k_cache", k, f"rows of packed_row_bytes of 4 or 8 bits and {d} elements")
+        _row_bits[row, d] = bits
+    t = torch.uint8
+    return (_pack_packed(kind, bits, b, h, n, d) + _rows(k, name + "k_cache", t, shape, index) + _rows(v, name + "v_cache", t, shape, index)), shape
+
+
+def cache_pack(k, v, bits: Optional[int] = None, *, lens=None, first=None, slots: Optional[int] = None, out: Optional[dict] = None,
+               sync: bool = True):
+    """lap_cache_pack: rows k and v [batch, kv_heads, length, head_dim] into a cache in `bits` (4 or 8) an element, row i of sequence b into
+    slot first[b] + i (None: i).  Returns dict(k, v), the cache: out's, whose other slots stay as they are, or a new one of
+    `slots` slots (None: length), zeros elsewhere."""
+    lib = _lib()
+    if k.requires_grad or v.requires_grad:
+        _warn_of_autograd("cache_pack", "there is none of a cache")
+    b, h, n, d = shape = _four(k, "k")
+    kind, t, index = _type(k, "k")
+    if out is None:
+        if bits is None:
+            raise ValueError("cache_pack: bits, or out, says how many an element takes")
+        m, row = n if slots is None else _count(slots, "slots"), packed_row_bytes(bits, d)
+        out = dict(k=k.new_zeros((b, h, m, row), dtype=torch.uint8), v=k.new_zeros((b, h, m, row), dtype=torch.uint8))
+    elif slots is not None:
+        raise ValueError("cache_pack: the slots are out's")
+    cache, rows = _packed(kind, d, out["k"], out["v"], index, "out ")
+    if rows[:2] != shape[:2] or (bits is not None and rows[3] != packed_row_bytes(bits, d)):
+        _refuse("out k_cache", out["k"], f"a cache of {b} sequences and {h} heads" + (f" in {bits} bits" if bits is not None else ""))
+    rc = _on(index, lib.lap_cache_pack, cache, _rows(k, "k", t, shape, index), _rows(v, "v", t, shape, index), n,
+             _plain(lens, "lens", torch.int32, (b,), index), _plain(first, "first", torch.int32, (b,), index), _stream(index))
+    if rc or sync:
+        _done(rc, "lap_cache_pack", index, sync)
+    return out
+
+
+def cache_unpack(k_cache, v_cache, dtype, head_dim: int, *, lens=None, first=None, length: Optional[int] = None, out: Optional[dict] = None,
+                 sync: bool = True):
+    """lap_cache_unpack: what the slots first[b] + i of a packed cache stand for, as rows [batch, kv_heads, length, head_dim] of dtype
+    (None: as many as there are slots); rows i from lens[b] on are zeros.  Returns dict(k, v)."""
+    lib = _lib()
+    kind = _kinds.get(dtype)
+    if kind is None:
+        raise ValueError(f"cache_unpack: {dtype}, expected torch.bfloat16 or torch.float16")
+    index = k_cache.get_device()
+    if index < 0:
+        _refuse("k_cache", k_cache, "a tensor on the GPU")
+    cache, (b, h, m, _) = _packed(kind, _count(head_dim, "head_dim"), k_cache, v_cache, index)
+    n = m if length is None else _count(length, "length")
+    shape = (b, h, n, head_dim)
+    if out is None:
+        out = dict(k=k_cache.new_empty(shape, dtype=dtype), v=k_cache.new_empty(shape, dtype=dtype))
+    rc = _on(index, lib.lap_cache_unpack, cache, n, _plain(lens, "lens", torch.int32, (b,), index), _plain(first, "first", torch.int32, (b,), index),
+             _rows(out["k"], "out k", dtype, shape, index), _rows(out["v"], "out v", dtype, shape, index), _stream(index))
+    if rc or sync:
+        _done(rc, "lap_cache_unpack", index, sync)
+    return out
+
+
+def attention_step_packed(q, k_cache, v_cache, weights=None, *, lens=None, positions=None, q_lens=None, scale: Optional[float] = None,
+                          out: Optional[dict] = None, ws=None, sync: bool = True):
+    """lap_attention_step_packed: attention_step on a packed cache, for q [batch, q_heads, head_dim] of one token of every sequence, or
+    [batch, q_heads, tokens, head_dim] of its last few, whose keys and values are in the cache already (q_lens: how many of them are in
+    use).  Returns dict(out like q, lse [batch, q_heads] or [batch, q_heads, tokens], weights as there)."""
+    lib = _lib()
+    if q.requires_grad:
+        _warn_of_autograd("attention_step_packed", "there is none of a step")
+    qs = q.shape
+    if len(qs) not in (3, 4):
+        _refuse("q", q, "[batch, heads, head_dim] or [batch, heads, tokens, head_dim]")
+    b, h, d = qs[0], qs[1], qs[-1]
+    tokens = qs[2] if len(qs) == 4 else 1
+    kind, t, index = _type(q, "q")
+    cache, (cb, kv, n, _) = _packed(kind, d, k_cache, v_cache, index)
+    if cb != b:
+        _refuse("k_cache", k_cache, f"a cache of {b} sequences")
+    s = _pack_shape(kind, b, h, kv, tokens, n, d, 1, 0, _scale(scale, d), 0 if q_lens is None else _plain(q_lens, "q_lens", torch.int32, (b,), index),
+                    0 if lens is None else _plain(lens, "lens", torch.int32, (b,), index))
+    slots, lse = (b, kv, n), qs[:-1]
+    if out is None:
+        out = dict(out=torch.empty_like(q), lse=q.new_empty(lse, dtype=torch.float32),
+                   weights=None if weights is None else q.new_empty(slots, dtype=torch.float32))
+    ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_STEP_PACKED, s), index, q)
+    rc = _on(index, lib.lap_attention_step_packed, s, _rows(q, "q", t, qs, index), cache, _plain(positions, "positions", torch.int32, slots, index),
+             _plain(weights, "weights", torch.float32, slots, index), _rows(out["out"], "out", t, qs, index),
+             _plain(out["lse"], "lse", torch.float32, lse, index), _plain(out.get("weights"), "out weights", torch.float32, slots, index),
+             at, have, _stream(index))
+    if rc or sync:
+        _done(rc, "lap_attention_step_packed", index, sync)
+    return out

@@ -121,10 +121,12 @@ lap::Rows rows_of(const lap_rows *x, uint64_t batch, uint64_t heads, uint64_t le
 lap::Rows queries_of(const lap_attention_shape *s, const lap_rows *x) { return rows_of(x, s->batch, s->q_heads, s->q_len); }
 lap::Rows keys_of(const lap_attention_shape *s, const lap_rows *x) { return rows_of(x, s->batch, s->kv_heads, s->k_len); }
 
-lap::StepShape step_of(const lap_attention_shape *s)
+lap::StepShape step_of(const lap_attention_shape *s, bool packed)
 {
-    lap::StepShape p = {s->batch, s->q_heads, s->kv_heads, s->k_len, s->head_dim, s->scale, s->k_lens, s->type == LAP_T_F16, 0, 0, 0, false};
-    lap::step_split(p);
+    lap::StepShape p = {s->batch, s->q_heads, s->kv_heads, s->k_len, s->head_dim, s->scale, s->k_lens, s->type == LAP_T_F16, packed ? s->q_len : 1,
+                        packed ? s->q_lens : nullptr, 0, 0, 0, false};
+    if (packed) lap::packed_step_split(p);
+    else lap::step_split(p);
     return p;
 }
 inline size_t padded_dim(const lap_attention_shape *s) { return s->head_dim <= 64 ? 64 : 128; }
@@ -136,24 +138,96 @@ size_t ws_weights(const lap_attention_shape *s)
     const uint32_t parts = lap::weights_parts(shape_of(s));
     return parts == 1 ? 0 : up((size_t)s->batch * s->kv_heads * parts * s->k_len * 4);
 }
-size_t ws_step(const lap_attention_shape *s)
+size_t ws_step(const lap_attention_shape *s, bool packed)
 {
-    const lap::StepShape p = step_of(s);
-    const size_t heads = (size_t)s->batch * s->q_heads;
-    return p.whole ? up(heads * p.score_row * 4) : up(heads * p.splits * padded_dim(s) * 4) + up(heads * p.splits * sizeof(float2)) + up(heads * p.score_row * 4);
+    const lap::StepShape p = step_of(s, packed);
+    const size_t rows = (size_t)s->batch * s->q_heads * p.tokens;
+    return p.whole ? up(rows * p.score_row * 4) : up(rows * p.splits * padded_dim(s) * 4) + up(rows * p.splits * sizeof(float2)) + up(rows * p.score_row * 4);
+}
+void carve_step(lap::StepWork &w, const lap_attention_shape *s, const lap::StepShape &p, void *ws)
+{
+    const size_t rows = (size_t)s->batch * s->q_heads * p.tokens;
+    char *at = (char *)ws;
+    if (!p.whole) {
+        w.outs = (float *)at, at += up(rows * p.splits * padded_dim(s) * 4);
+        w.sums = (float2 *)at, at += up(rows * p.splits * sizeof(float2));
+    }
+    w.scores = (float *)at;
 }
 
-lap::Rows slots_of(const lap_cache *c, const lap_rows *x) { return rows_of(x, c->batch, c->kv_heads, c->slots); }
+// rows of bytes as rows of half as many 16-bit elements
+lap_rows halved(const lap_rows *x) { return {x->data, x->batch / 2, x->head / 2, x->row / 2}; }
+int check_bytes(const lap_rows *x, uint64_t batch, uint64_t heads, uint64_t len, uint32_t row_bytes, bool output)
+{
+    if (!x) return LAP_E_NULL;
+    if ((batch > 1 && x->batch % 16) || (heads > 1 && x->head % 16) || (len > 1 && x->row % 16)) return LAP_E_LAYOUT;
+    const lap_rows y = halved(x);
+    return check_rows(&y, batch, heads, len, row_bytes / 2, output);
+}
+
+// what moves the rows of a cache of bytes takes them as 16-bit elements
+lap::Rows moved(const lap_cache *c, const lap_rows *x, uint64_t len)
+{
+    const lap_rows y = c->type == LAP_T_BYTES ? halved(x) : *x;
+    return rows_of(&y, c->batch, c->kv_heads, len);
+}
+lap::Rows slots_of(const lap_cache *c, const lap_rows *x) { return moved(c, x, c->slots); }
+uint32_t moved_dim(const lap_cache *c) { return c->type == LAP_T_BYTES ? c->head_dim / 2 : c->head_dim; }
+
+int check_moved(const lap_cache *c, const lap_rows *x, uint64_t len, bool output)
+{
+    if (c->type == LAP_T_BYTES) return check_bytes(x, c->batch, c->kv_heads, len, c->head_dim, output);
+    return check_rows(x, c->batch, c->kv_heads, len, c->head_dim, output);
+}
 
 int check_cache(const lap_cache *c, bool output)
 {
     if (!c) return LAP_E_NULL;
-    if (c->type != LAP_T_BF16 && c->type != LAP_T_F16) return LAP_E_ATTENTION;
+    if (c->type != LAP_T_BF16 && c->type != LAP_T_F16 && c->type != LAP_T_BYTES) return LAP_E_ATTENTION;
+    if (!c->batch || !c->kv_heads || !c->head_dim) return LAP_E_SIZE;
+    if (moved_dim(c) > LAP_MAX_HEAD_DIM || c->slots > MAX_LEN || (uint64_t)c->batch * c->kv_heads > MAX_GRID) return LAP_E_SIZE;
+    if (c->head_dim % (c->type == LAP_T_BYTES ? 16 : 8)) return LAP_E_LAYOUT;
+    const int rc = check_moved(c, &c->k, c->slots, output);
+    return rc ? rc : check_moved(c, &c->v, c->slots, output);
+}
+
+int check_packed(const lap_packed_cache *c, bool output)
+{
+    if (!c) return LAP_E_NULL;
+    if ((c->type != LAP_T_BF16 && c->type != LAP_T_F16) || (c->bits != 4 && c->bits != 8)) return LAP_E_ATTENTION;
     if (!c->batch || !c->kv_heads || !c->head_dim) return LAP_E_SIZE;
     if (c->head_dim > LAP_MAX_HEAD_DIM || c->slots > MAX_LEN || (uint64_t)c->batch * c->kv_heads > MAX_GRID) return LAP_E_SIZE;
     if (c->head_dim % 8) return LAP_E_LAYOUT;
-    const int rc = check_rows(&c->k, c->batch, c->kv_heads, c->slots, c->head_dim, output);
-    return rc ? rc : check_rows(&c->v, c->batch, c->kv_heads, c->slots, c->head_dim, output);
+    const uint32_t bytes = (uint32_t)lap_packed_row_bytes(c->bits, c->head_dim);
+    const int rc = check_bytes(&c->k, c->batch, c->kv_heads, c->slots, bytes, output);
+    return rc ? rc : check_bytes(&c->v, c->batch, c->kv_heads, c->slots, bytes, output);
+}
+lap::Rows packed_of(const lap_packed_cache *c, const lap_rows *x) { return rows_of(x, c->batch, c->kv_heads, c->slots); }
+
+// a step's shape on a packed cache, but for the cache
+int check_step_packed(const lap_attention_shape *s)
+{
+    const int rc = check_shape(s);
+    if (rc) return rc;
+    if (!s->q_len || s->window || (s->q_len > 1 && !s->causal)) return LAP_E_ATTENTION;
+    if ((uint64_t)(s->q_heads / s->kv_heads) * s->q_len > lap::MAX_GROUP || (uint64_t)s->batch * s->kv_heads > MAX_GRID) return LAP_E_SIZE;
+    return LAP_OK;
+}
+
+int check_pack(const lap_packed_cache *c, const lap_rows *k, const lap_rows *v, uint32_t n, bool write)
+{
+    int rc = check_packed(c, write);
+    if (!rc && n > MAX_LEN) rc = LAP_E_SIZE;
+    if (!rc && (uint64_t)c->batch * c->kv_heads * ((uint64_t)n / 32 + 1) > MAX_ITEMS) rc = LAP_E_SIZE;
+    for (const lap_rows *x : {k, v})
+        if (!rc) rc = check_rows(x, c->batch, c->kv_heads, n, c->head_dim, !write);
+    if (rc || !n || !c->slots) return rc;
+    if (write) {
+        rc = check_apart(c->k.data, {c->v.data, k->data, v->data});
+        return rc ? rc : check_apart(c->v.data, {k->data, v->data});
+    }
+    rc = check_apart(k->data, {v->data, c->k.data, c->v.data});
+    return rc ? rc : check_apart(v->data, {c->k.data, c->v.data});
 }
 
 }  // namespace
@@ -167,7 +241,8 @@ size_t lap_attention_workspace_bytes(int which_call, const lap_attention_shape *
     case LAP_AT_FORWARD: return up(lap::forward_workspace(shape_of(s)));
     case LAP_AT_GRAD: return ws_grad(s);
     case LAP_AT_WEIGHTS: return ws_weights(s);
-    case LAP_AT_STEP: return ws_step(s);
+    case LAP_AT_STEP: return ws_step(s, false);
+    case LAP_AT_STEP_PACKED: return check_step_packed(s) ? 0 : ws_step(s, true);
     default: return 0;
     }
 }
@@ -247,18 +322,12 @@ int lap_attention_step(const lap_attention_shape *s, const lap_rows *q, const la
     if (!rc) rc = check_rows(v, s->batch, s->kv_heads, s->k_len, s->head_dim, false);
     if (!rc) rc = check_rows(out, s->batch, s->q_heads, 1, s->head_dim, true);
     if (!rc && (!lse || (before != nullptr) != (weights != nullptr))) rc = LAP_E_NULL;
-    if (!rc) rc = check_ws(ws, ws_bytes, ws_step(s));
+    if (!rc) rc = check_ws(ws, ws_bytes, ws_step(s, false));
     if (!rc && s->k_len) rc = check_apart(out->data, {k->data, v->data});
     if (rc) return rc;
-    const lap::StepShape p = step_of(s);
-    const size_t heads = (size_t)s->batch * s->q_heads;
+    const lap::StepShape p = step_of(s, false);
     lap::StepWork w = {queries_of(s, q), keys_of(s, k), keys_of(s, v), queries_of(s, out), positions, before, lse, weights, nullptr, nullptr, nullptr};
-    char *at = (char *)ws;
-    if (!p.whole) {
-        w.outs = (float *)at, at += up(heads * p.splits * padded_dim(s) * 4);
-        w.sums = (float2 *)at, at += up(heads * p.splits * sizeof(float2));
-    }
-    w.scores = (float *)at;
+    carve_step(w, s, p, ws);
     LAP_HIP(lap::launch_attention_step(p, w, (hipStream_t)hip_stream));
     return LAP_OK;
 }
@@ -282,7 +351,7 @@ int lap_cache_evict(const lap_cache *from, const int32_t *lens, uint32_t keep, u
         if (!rc) rc = check_apart(to->positions, {from->positions});
     }
     if (rc) return rc;
-    const lap::EvictShape s = {from->batch, from->kv_heads, from->slots, to->slots, from->head_dim, keep, recent, lens};
+    const lap::EvictShape s = {from->batch, from->kv_heads, from->slots, to->slots, moved_dim(from), keep, recent, lens};
     LAP_HIP(lap::launch_cache_evict(s, slots_of(from, &from->k), slots_of(from, &from->v), from->weights, from->positions, slots_of(to, &to->k),
                                     slots_of(to, &to->v), to->weights, to->positions, lens_out, (int32_t *)ws, (hipStream_t)hip_stream));
     return LAP_OK;
@@ -294,14 +363,65 @@ int lap_cache_insert(const lap_cache *c, const lap_rows *k_new, const lap_rows *
     int rc = check_cache(c, true);
     if (rc) return rc;
     if (c->slots == 0 || recent > c->slots) return LAP_E_SIZE;
-    rc = check_rows(k_new, c->batch, c->kv_heads, 1, c->head_dim, false);
-    if (!rc) rc = check_rows(v_new, c->batch, c->kv_heads, 1, c->head_dim, false);
+    rc = check_moved(c, k_new, 1, false);
+    if (!rc) rc = check_moved(c, v_new, 1, false);
     if (rc) return rc;
     if (!c->weights || !c->positions || !position || !slots) return LAP_E_NULL;
-    const lap::InsertShape s = {c->batch, c->kv_heads, c->slots, c->head_dim, recent};
-    LAP_HIP(lap::launch_cache_insert(s, rows_of(k_new, c->batch, c->kv_heads, 1), rows_of(v_new, c->batch, c->kv_heads, 1),
+    const lap::InsertShape s = {c->batch, c->kv_heads, c->slots, moved_dim(c), recent};
+    LAP_HIP(lap::launch_cache_insert(s, moved(c, k_new, 1), moved(c, v_new, 1),
                                      slots_of(c, &c->k), slots_of(c, &c->v), c->weights, c->positions, position,
                                      slots, (hipStream_t)hip_stream));
+    return LAP_OK;
+}
+
+size_t lap_packed_row_bytes(uint32_t bits, uint32_t head_dim)
+{
+    if ((bits != 4 && bits != 8) || !head_dim || head_dim > LAP_MAX_HEAD_DIM || head_dim % 8) return 0;
+    return lap::pack_row_bytes(head_dim, bits);
+}
+
+int lap_cache_pack(const lap_packed_cache *to, const lap_rows *k, const lap_rows *v, uint32_t n, const int32_t *lens, const int32_t *first,
+                   void *hip_stream)
+{
+    const int rc = check_pack(to, k, v, n, true);
+    if (rc || !n || !to->slots) return rc;
+    const lap::PackShape s = {to->batch, to->kv_heads, to->slots, n, to->head_dim, to->bits, lens, first, to->type == LAP_T_F16};
+    LAP_HIP(lap::launch_cache_pack(s, rows_of(k, s.batch, s.kv_heads, n), rows_of(v, s.batch, s.kv_heads, n), packed_of(to, &to->k), packed_of(to, &to->v),
+                                   (hipStream_t)hip_stream));
+    return LAP_OK;
+}
+
+int lap_cache_unpack(const lap_packed_cache *from, uint32_t n, const int32_t *lens, const int32_t *first, const lap_rows *k, const lap_rows *v,
+                     void *hip_stream)
+{
+    const int rc = check_pack(from, k, v, n, false);
+    if (rc || !n) return rc;
+    const lap::PackShape s = {from->batch, from->kv_heads, from->slots, n, from->head_dim, from->bits, lens, first, from->type == LAP_T_F16};
+    LAP_HIP(lap::launch_cache_unpack(s, packed_of(from, &from->k), packed_of(from, &from->v), rows_of(k, s.batch, s.kv_heads, n),
+                                     rows_of(v, s.batch, s.kv_heads, n), (hipStream_t)hip_stream));
+    return LAP_OK;
+}
+
+int lap_attention_step_packed(const lap_attention_shape *s, const lap_rows *q, const lap_packed_cache *cache, const int32_t *positions,
+                              const float *before, const lap_rows *out, float *lse, float *weights, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    int rc = check_step_packed(s);
+    if (!rc) rc = check_packed(cache, false);
+    if (rc) return rc;
+    if (cache->type != s->type || cache->batch != s->batch || cache->kv_heads != s->kv_heads || cache->slots != s->k_len || cache->head_dim != s->head_dim ||
+        (positions && s->q_len > 1))
+        return LAP_E_ATTENTION;
+    rc = check_rows(q, s->batch, s->q_heads, s->q_len, s->head_dim, false);
+    if (!rc) rc = check_rows(out, s->batch, s->q_heads, s->q_len, s->head_dim, true);
+    if (!rc && (!lse || (before != nullptr) != (weights != nullptr))) rc = LAP_E_NULL;
+    if (!rc) rc = check_ws(ws, ws_bytes, ws_step(s, true));
+    if (!rc && s->k_len) rc = check_apart(out->data, {cache->k.data, cache->v.data});
+    if (rc) return rc;
+    const lap::StepShape p = step_of(s, true);
+    lap::StepWork w = {queries_of(s, q), packed_of(cache, &cache->k), packed_of(cache, &cache->v), queries_of(s, out), positions, before, lse, weights,
+                       nullptr, nullptr, nullptr};
+    carve_step(w, s, p, ws);
+    LAP_HIP(lap::launch_attention_step_packed(p, w, cache->bits, (hipStream_t)hip_stream));
     return LAP_OK;
 }
 

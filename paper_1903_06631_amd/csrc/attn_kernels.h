@@ -38,28 +38,53 @@ uint32_t weights_parts(const AttnShape &s);
 hipError_t launch_attention_weights(const AttnShape &s, const Rows &q, const Rows &k, const float *lse, const float *before, float *weights,
                                     float *sums, hipStream_t st);
 
-constexpr uint32_t MAX_GROUP = 256;      // query heads that share one key head, in attention_step.hip
+constexpr uint32_t MAX_GROUP = 256;      // rows of queries (heads times tokens) that share one key head in a step
 
 struct StepShape {
     uint32_t batch, q_heads, kv_heads, slots, head_dim;
     float scale;
     const int32_t *lens;
     bool half;
+    uint32_t tokens;             // of every sequence (of rows in 16 bits: 1)
+    const int32_t *q_lens;       // how many of them are in use, NULL: all
     uint32_t chunk, splits;      // slots of a workgroup, workgroups of a cache (step_split)
     uint64_t score_row;          // floats between two heads' scores (0: they stay in LDS)
     bool whole;                  // one workgroup for all of a cache, and nothing to join
 };
 struct StepWork {
-    Rows q, k, v, out;      // q, out: row unused
+    Rows q, k, v, out;      // q, out: row unused where there is one token; packed k, v: strides in bytes
     const int32_t *positions;
     const float *before;
     float *lse, *weights;
-    float *outs;            // [batch, q_heads, splits, 64 or 128]
-    float2 *sums;           // [batch, q_heads, splits]: maximum in base 2, sum
-    float *scores;          // [batch, q_heads, score_row] in base 2, where weights are asked for
+    float *outs;            // [batch, q_heads, tokens, splits, 64 or 128]
+    float2 *sums;           // [batch, q_heads, tokens, splits]: maximum in base 2, sum
+    float *scores;          // [batch, q_heads, tokens, score_row] in base 2, where weights are asked for
 };
 void step_split(StepShape &s);
 hipError_t launch_attention_step(const StepShape &s, const StepWork &w, hipStream_t st);
+hipError_t launch_step_join(const StepShape &s, const StepWork &w, hipStream_t st);
+
+// caches in 4 or 8 bits an element: packed_rows.h
+constexpr int PACK_GROUP = 32;
+__host__ __device__ __forceinline__ uint32_t pack_groups(uint32_t head_dim) { return (head_dim + PACK_GROUP - 1) / PACK_GROUP; }
+// byte of a row where lo and step of its groups begin
+__host__ __device__ __forceinline__ uint32_t pack_ends(uint32_t head_dim, uint32_t bits) { return pack_groups(head_dim) * bits * 4; }
+__host__ __device__ __forceinline__ uint32_t pack_row_bytes(uint32_t head_dim, uint32_t bits)
+{
+    return (pack_ends(head_dim, bits) + pack_groups(head_dim) * 4 + 15) / 16 * 16;
+}
+
+void packed_step_split(StepShape &s);
+hipError_t launch_attention_step_packed(const StepShape &s, const StepWork &w, uint32_t bits, hipStream_t st);
+
+struct PackShape {
+    uint32_t batch, kv_heads, slots, n, head_dim, bits;      // n: rows of the plain tensors
+    const int32_t *lens, *first;      // rows in use, slot of the first one; NULL: n, 0
+    bool half;
+};
+// k, v: plain rows; k_cache, v_cache: strides in bytes
+hipError_t launch_cache_pack(const PackShape &s, const Rows &k, const Rows &v, const Rows &k_cache, const Rows &v_cache, hipStream_t st);
+hipError_t launch_cache_unpack(const PackShape &s, const Rows &k_cache, const Rows &v_cache, const Rows &k, const Rows &v, hipStream_t st);
 
 struct EvictShape {
     uint32_t batch, kv_heads, slots, slots_out, head_dim, keep, recent;

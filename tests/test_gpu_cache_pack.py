@@ -1,0 +1,228 @@
+"""Packing and unpacking: the bytes that the definition gives, bit by bit, and what they stand for."""
+import math
+
+import pytest
+import torch
+
+import packed_ref as ref
+from test_gpu_attention import BF, HF, rows
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def lap():
+    import paper_1903_06631_amd as lap
+    lap.load_library()
+    return lap
+
+
+def i32(values):
+    return None if values is None else torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+def same(a, b):
+    """Equal numbers, not-a-number where the other is."""
+    a, b = a.detach().cpu(), b.detach().cpu()
+    return torch.equal(a.isnan(), b.isnan()) and torch.equal(a.nan_to_num(0.0), b.nan_to_num(0.0))
+
+
+def empty_cache(b, h, n, row, layout="bhnr"):
+    """Bytes that no row has: slots that are not written stay so."""
+    if layout == "gaps":
+        return torch.full((b, h + 1, n + 2, row + 32), 0xA5, dtype=torch.uint8, device="cuda")[:, 1:, 1:n + 1, 16:row + 16]
+    if layout == "bnhr":
+        return torch.full((b, n, h, row), 0xA5, dtype=torch.uint8, device="cuda").transpose(1, 2)
+    return torch.full((b, h, n, row), 0xA5, dtype=torch.uint8, device="cuda")
+
+
+def check_bytes(got, want, kind, d, bits):
+    """Rows of bytes: equal, but for which not-a-number a group is."""
+    got, want = got.cpu(), want.clone()
+    a, b = ref.unpack(got, kind, d, bits), ref.unpack(want, kind, d, bits)
+    assert same(a, b)
+    ok = (got == want).all(-1) | a.isnan().any(-1)
+    assert ok.all(), f"rows {(~ok).nonzero().tolist()[:4]}"
+
+
+# type, bits, head size, key heads, rows, slots, lengths, first slots, layout of the rows, of the cache
+CASES = [
+    (BF, 4, 128, 2, 1, 1, None, None, "bhnd", "bhnr"),
+    (HF, 4, 128, 2, 1, 50, None, [49, 0, 17], "bhnd", "bnhr"),
+    (BF, 8, 128, 1, 37, 40, [37, 0, 1], [3, 40, 39], "bnhd", "bhnr"),
+    (HF, 8, 64, 3, 33, 33, [40, -5, 32], None, "gaps", "gaps"),
+    (BF, 4, 64, 2, 70, 300, None, [230, 0, 299], "bnhd", "gaps"),          # rows past the cache's end
+    (HF, 4, 80, 2, 51, 64, [51, 50, 2], [-3, 5, 62], "gaps", "bnhr"),       # and before its start
+    (BF, 8, 96, 2, 20, 20, None, None, "bhnd", "bhnr"),
+    (HF, 4, 8, 2, 65, 65, None, None, "gaps", "bhnr"),
+    (BF, 4, 24, 2, 17, 17, None, None, "bhnd", "bhnr"),
+    (HF, 8, 40, 1, 18, 30, None, [5, 11, 12], "bhnd", "gaps"),
+    (BF, 4, 104, 1, 300, 301, [300, 299, 257], [1, 1, 0], "bhnd", "bhnr"),
+    (HF, 8, 120, 1, 9, 9, None, None, "bnhd", "bnhr"),
+    (BF, 8, 72, 1, 5, 9, None, [2 ** 31 - 1, -(2 ** 31), 4], "bhnd", "bhnr"),
+    (HF, 4, 128, 1, 700, 700, None, None, "bnhd", "bhnr"),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(str(x).replace("torch.", "") for x in c))
+def test_rows(lap, case):
+    kind, bits, d, h, n, slots, lens, first, layout, cache_layout = case
+    b = 3
+    gen = torch.Generator().manual_seed(n + d)
+    k, v = rows(gen, b, h, n, d, kind, layout=layout), rows(gen, b, h, n, d, kind, layout=layout, times=5.0)
+    row = ref.row_bytes(d, bits)
+    out = dict(k=empty_cache(b, h, slots, row, cache_layout), v=empty_cache(b, h, slots, row, cache_layout))
+    assert lap.cache_pack(k, v, lens=i32(lens), first=i32(first), out=out) is out
+    back = lap.cache_unpack(out["k"], out["v"], kind, d, lens=i32(lens), first=i32(first), length=n)
+    for x, cache, y in ((k, out["k"], back["k"]), (v, out["v"], back["v"])):
+        want = torch.full((b, h, slots, row), 0xA5, dtype=torch.uint8)
+        stands = torch.zeros(b, h, n, d, dtype=kind)
+        packed = ref.pack(x, bits)
+        for i in range(b):
+            m, at = n if lens is None else max(0, min(n, lens[i])), 0 if first is None else first[i]
+            for j in range(m):
+                if 0 <= at + j < slots:
+                    want[i, :, at + j] = packed[i, :, j]
+                    stands[i, :, j] = ref.unpack(packed[i, :, j], kind, d, bits)
+        check_bytes(cache, want, kind, d, bits)
+        assert same(y, stands)
+        # what lies around the cache in memory is not touched
+        if cache_layout == "gaps":
+            assert (cache._base[:, 0] == 0xA5).all() and (cache._base[:, :, 0] == 0xA5).all() and (cache._base[..., -16:] == 0xA5).all()
+
+
+def groups_of(kind, gen):
+    """Rows of one group each that go wrong easily."""
+    top, least = torch.finfo(kind).max, torch.finfo(kind).smallest_normal
+    r = torch.randn(24, 32, generator=gen).to(kind)
+    x = [r[0] * 0, r[0] * 0 + 3.0, -r[1].abs(), r[2] * least, r[3].abs() * (least / 8), r[4] * (2 * least / 64)]
+    one = r[5].clone(); one[7] = math.nan; x.append(one)
+    one = r[6].clone(); one[31] = math.inf; x.append(one)
+    one = r[7].clone(); one[0] = -math.inf; x.append(one)
+    one = r[8].clone(); one[3], one[9] = math.inf, -math.inf; x.append(one)
+    one = r[9] * 0; one[::2] = -0.0; x.append(one)
+    one = torch.full((32,), top, dtype=kind); one[5] = -top; x.append(one)          # bfloat16: a range over 2^100
+    one = torch.full((32,), top, dtype=kind); one[5] = top * 0.37; x.append(one)
+    one = torch.full((32,), 2.0 ** 15, dtype=kind) * (1 + torch.rand(32, generator=gen).to(kind) * 0.99); one[1] = 65504.0; x.append(one)
+    one = r[10].clone(); one[2] = 2.0 ** -14; one[4] = 512.0; x.append(one)
+    x += [torch.arange(32).to(kind), torch.arange(32).to(kind) / 2, -torch.arange(32).to(kind) * 7.5, torch.arange(32).to(kind) * 8 + 0.5]      # ties
+    if kind is BF:
+        one = r[11].clone(); one[2] = 2.0 ** 99; one[5] = -(2.0 ** 98); x.append(one)
+        one = r[12] * 0; one[3] = 2.0 ** 100; x.append(one)                          # the widest that is held
+        one = r[12] * 0; one[3] = 2.0 ** 100 * (1 + 2.0 ** -7); x.append(one)
+        x += [r[13] * 2.0 ** -100, r[14] * 2.0 ** -126, (torch.arange(32) * 2.0 ** -133).to(kind), r[15] * 2.0 ** 60, r[16].abs() * 2.0 ** -64]
+        one = torch.full((32,), top, dtype=kind); one[::3] = top * (1 - 2.0 ** -7); x.append(one)
+    return torch.stack(x)
+
+
+@pytest.mark.parametrize("kind", [BF, HF])
+@pytest.mark.parametrize("bits", [4, 8])
+def test_hard_groups(lap, kind, bits):
+    x = groups_of(kind, torch.Generator().manual_seed(5))
+    n = x.shape[0]
+    y = x.flip(0)
+    k = torch.cat([x, y, x.flip(1), y], dim=1).view(1, 1, n, 128).cuda()
+    got = lap.cache_pack(k, k.flip(-1), bits)
+    for a, c in ((k, got["k"]), (k.flip(-1), got["v"])):
+        check_bytes(c, ref.pack(a, bits), kind, 128, bits)
+    back = lap.cache_unpack(got["k"], got["v"], kind, 128)
+    assert same(back["k"], ref.unpack(got["k"], kind, 128, bits)) and same(back["v"], ref.unpack(got["v"], kind, 128, bits))
+
+
+@pytest.mark.parametrize("kind", [BF, HF])
+@pytest.mark.parametrize("bits", [4, 8])
+def test_few_values_and_many_ties(lap, kind, bits):
+    """Whole numbers, whose quotients often stand halfway."""
+    gen = torch.Generator().manual_seed(bits)
+    x = torch.randint(-120, 121, (1, 2, 300, 64), generator=gen).to(kind) * 0.25
+    got = lap.cache_pack(x.cuda(), x.cuda(), bits)
+    check_bytes(got["k"], ref.pack(x, bits), kind, 64, bits)
+
+
+def test_new_caches(lap):
+    """Without `out`: zeros where nothing goes, more slots than rows; nothing at all."""
+    x = torch.randn(2, 2, 5, 64, device="cuda").half()
+    got = lap.cache_pack(x, x, 8, slots=9, lens=i32([5, 2]))
+    assert got["k"].shape == (2, 2, 9, 80) and not got["k"][:, :, 5:].any() and not got["v"][1, :, 2:].any() and got["k"][1, :, :2].any()
+    none = x[:, :, :0]
+    assert lap.cache_pack(none, none, 4)["k"].shape == (2, 2, 0, 48)
+    held = lap.cache_pack(none, none, 4, slots=3)
+    assert not lap.cache_unpack(held["k"], held["v"], torch.float16, 64)["k"].any()
+    empty = torch.zeros(2, 2, 0, 48, dtype=torch.uint8, device="cuda")
+    assert lap.cache_unpack(empty, empty, torch.bfloat16, 64)["v"].shape == (2, 2, 0, 64)
+    back = lap.cache_unpack(empty, empty, torch.bfloat16, 64, length=4)
+    assert back["v"].shape == (2, 2, 4, 64) and not back["v"].any()
+    lap.cache_pack(x, x, out=dict(k=empty, v=empty.clone()))
+
+
+def test_broadcast_rows(lap):
+    """One key for all heads and sequences."""
+    x = torch.randn(1, 1, 40, 72, device="cuda").bfloat16()
+    got = lap.cache_pack(x.expand(3, 2, 40, 72), x.expand(3, 2, 40, 72), 4)
+    one = lap.cache_pack(x, x, 4)
+    assert torch.equal(got["k"], one["k"].expand_as(got["k"])) and torch.equal(got["v"], got["k"])
+
+
+def test_offsets_beyond_32_bits(lap):
+    """A cache's rows, and its sequences, further apart than 32 bits count."""
+    b, n, d, far = 2, 300, 128, 1 << 24
+    raw = torch.full(((n - 1) * far + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+    cache = torch.as_strided(raw, (b, 1, n, 80), (1024, 1024, far, 1))
+    x = torch.randn(b, 1, n, d, device="cuda").bfloat16()
+    other = torch.zeros(b, 1, n, 80, dtype=torch.uint8, device="cuda")
+    lap.cache_pack(x, x, out=dict(k=cache, v=other))
+    assert torch.equal(cache, other) and raw[80].item() == 0xA5
+    back = lap.cache_unpack(cache, other, torch.bfloat16, d)
+    assert torch.equal(back["k"], back["v"])
+
+
+def test_streams_and_graphs(lap):
+    """On another stream, and captured: replays with the program's own work between them, every one equal to the eager call."""
+    x, y = (torch.randn(4, 2, 200, 128, device="cuda").bfloat16() for _ in range(2))
+    want = lap.cache_pack(x, y, 4)
+    rows_of = lap.cache_unpack(want["k"], want["v"], torch.bfloat16, 128)
+    out = dict(k=torch.zeros_like(want["k"]), v=torch.zeros_like(want["v"]))
+    back = dict(k=torch.zeros_like(x), v=torch.zeros_like(y))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        lap.cache_pack(x, y, out=out, sync=False)
+        lap.cache_unpack(out["k"], out["v"], torch.bfloat16, 128, out=back, sync=False)
+    side.synchronize()
+    assert torch.equal(out["k"], want["k"]) and torch.equal(back["v"], rows_of["v"])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lap.cache_pack(x, y, out=out, sync=False)
+        lap.cache_unpack(out["k"], out["v"], torch.bfloat16, 128, out=back, sync=False)
+    for i in range(4):
+        x.copy_(torch.randn(x.shape, device="cuda"))
+        out["k"].zero_(), back["k"].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = lap.cache_pack(x, y, 4)
+        assert torch.equal(out["k"], eager["k"]) and torch.equal(out["v"], eager["v"]), i
+        assert torch.equal(back["k"], lap.cache_unpack(eager["k"], eager["v"], torch.bfloat16, 128)["k"]), i
+
+
+def test_refusals(lap):
+    x = torch.ones(2, 2, 5, 64, device="cuda").bfloat16()
+    c = lap.cache_pack(x, x, 4)
+    before = c["k"].clone()
+    for call in (lambda: lap.cache_pack(x, x), lambda: lap.cache_pack(x, x, 5), lambda: lap.cache_pack(x.float(), x, 4), lambda: lap.cache_pack(x, x.half(), 4),
+                 lambda: lap.cache_pack(x, x[:, :, :4], 4), lambda: lap.cache_pack(x, x.cpu(), 4), lambda: lap.cache_pack(x[0], x[0], 4),
+                 lambda: lap.cache_pack(x, x, 8, out=c), lambda: lap.cache_pack(x, x, slots=9, out=c), lambda: lap.cache_pack(x[:1], x[:1], out=c),
+                 lambda: lap.cache_pack(x, x, out=dict(k=c["k"], v=c["v"][..., :32])), lambda: lap.cache_pack(x, x, out=dict(k=c["k"].cpu(), v=c["v"])),
+                 lambda: lap.cache_pack(x, x, 4, lens=torch.zeros(2, dtype=torch.int64, device="cuda")), lambda: lap.cache_pack(x, x, 4, first=i32([1, 2, 3])),
+                 lambda: lap.cache_pack(x, x, 4, slots=-1), lambda: lap.cache_pack(x[..., :60], x[..., :60], 4),
+                 lambda: lap.cache_unpack(c["k"], c["v"], torch.float32, 64), lambda: lap.cache_unpack(c["k"], c["v"], torch.bfloat16, 72),
+                 lambda: lap.cache_unpack(c["k"], c["v"].half(), torch.bfloat16, 64), lambda: lap.cache_unpack(c["k"], c["v"], torch.bfloat16, 64, length=-1),
+                 lambda: lap.cache_unpack(c["k"], c["v"], torch.bfloat16, 64, length=3, out=dict(k=x, v=x)),
+                 lambda: lap.cache_unpack(c["k"], c["v"], torch.bfloat16, 64, lens=i32([1]))):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: lap.cache_pack(x, x, out=dict(k=c["k"], v=c["k"])), lambda: lap.cache_pack(x, x, out=dict(k=c["k"][:, :1].expand(2, 2, 5, 48), v=c["v"])),
+                 lambda: lap.cache_unpack(c["k"], c["v"], torch.bfloat16, 64, out=dict(k=x, v=x))):
+        with pytest.raises(lap.LapError) as e:
+            call()
+        assert e.value.status == -10
+    assert torch.equal(c["k"], before) and (x == 1).all()
