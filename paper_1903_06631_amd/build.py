@@ -12,7 +12,7 @@ OBJ_DIR = os.path.join(_HERE, "_build")
 SOURCES = ["api.hip", "load_profile.hip", "orderings.hip", "plan_prep.hip", "place_fast.hip", "place_reg.hip", "place_batch.hip", "place_wide.hip",
            "place_seg.hip", "swap_scores.hip", "select_swaps.hip", "detect_iteration.hip",
            "schedule_swaps.hip", "simulate_swaps.hip", "attention_api.hip", "attention.hip", "attention_grad.hip",
-           "attention_weights.hip", "attention_step.hip", "attention_step_packed.hip", "step_join.hip", "kv_cache.hip",
+           "attention_weights.hip", "attention_step.hip", "attention_step_packed.hip", "packed_join.hip", "kv_cache.hip",
            "cache_pack.hip"]
 
 FLAGS = [

@@ -124,7 +124,7 @@ lap::Rows keys_of(const lap_attention_shape *s, const lap_rows *x) { return rows
 lap::StepShape step_of(const lap_attention_shape *s, bool packed)
 {
     lap::StepShape p = {s->batch, s->q_heads, s->kv_heads, s->k_len, s->head_dim, s->scale, s->k_lens, s->type == LAP_T_F16, packed ? s->q_len : 1,
-                        packed ? s->q_lens : nullptr, 0, 0, 0, false};
+                        packed ? s->q_lens : nullptr, 0, 0, 0, 0, false};
     if (packed) lap::packed_step_split(p);
     else lap::step_split(p);
     return p;

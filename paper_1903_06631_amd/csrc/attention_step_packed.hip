@@ -23,8 +23,6 @@
 namespace lap {
 namespace {
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
 constexpr int TS = 32;                      // slots of a wave's tile
 constexpr uint32_t CHUNK_WAVES = 4;         // waves of a chunk's workgroup
 constexpr uint32_t WHOLE_WAVES = 8;         // and of one that goes through a whole cache
@@ -56,6 +54,11 @@ __device__ __forceinline__ float column_sum(float x)
     return half_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t bytes_at(const void *from, int size)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(from), 0, size, 0x00020000);
+}
+
 // The packed words of 32 slots that a lane holds, and where they stand in a row.  Lanes whose share of a row is past its last
 // group hold the last group's: queries are zero there, and outputs thrown away.
 template <int BITS, int DP> struct Words {
@@ -64,78 +67,77 @@ template <int BITS, int DP> struct Words {
     uint32_t k[2][KW], k_ends[2], v[8][VW], v_ends[8];
 };
 
+// Buffer loads: a lane's place within a tile does not change, the tile's start is in the scalar descriptor and so is its end, past
+// which such a load reads nothing and gives zeros.  (Ordinary loads took two 64-bit additions each, and with rows past the length
+// to be told from others their addresses took 32 registers.)
 template <int BITS, int DP> struct Loader {
     typedef Words<BITS, DP> W;
     const char *k, *v;                     // of the cache
     int64_t k_row, v_row;
-    uint32_t k_at, k_ends, v_at, v_ends;   // bytes from the start of a tile
-    uint32_t k_lane, v_lane;               // the same without the lane's slot
-    uint32_t k_gap, v_gap;                 // from the words to lo and step
-    int n, g;
+    uint32_t row_bytes;
+    int k_at, k_ends, v_at, v_ends;        // bytes from the start of a tile
     __device__ __forceinline__ Loader(const Rows &rk, const Rows &rv, uint32_t b, uint32_t kvh, uint32_t head_dim, int lane)
     {
-        n = lane & 15, g = lane >> 4;
+        const int n = lane & 15, g = lane >> 4;
         k = (const char *)rk.data + (int64_t)b * rk.batch + (int64_t)kvh * rk.head;
         v = (const char *)rv.data + (int64_t)b * rv.batch + (int64_t)kvh * rv.head;
         k_row = rk.row, v_row = rv.row;
+        row_bytes = pack_row_bytes(head_dim, BITS);
         const uint32_t groups = pack_groups(head_dim), ends = pack_ends(head_dim, BITS);
         const uint32_t kg = min((uint32_t)(DP == 128 ? g : g >> 1), groups - 1), vg = min((uint32_t)(DP == 128 ? n >> 2 : n >> 3), groups - 1);
-        k_lane = kg * (BITS * 4) + (DP == 128 ? 0 : (g & 1) * (BITS * 2));
-        v_lane = vg * (BITS * 4) + (DP == 128 ? (n & 3) * BITS : BITS == 8 ? (n & 7) * 4 : (n >> 1 & 3) * 4);
-        k_gap = ends + kg * 4 - k_lane, v_gap = ends + vg * 4 - v_lane;
-        k_at = n * (uint32_t)k_row + k_lane, v_at = 4 * g * (uint32_t)v_row + v_lane;
+        const uint32_t k_slot = n * (uint32_t)k_row, v_slot = 4 * g * (uint32_t)v_row;
+        k_at = k_slot + kg * (BITS * 4) + (DP == 128 ? 0 : (g & 1) * (BITS * 2));
+        v_at = v_slot + vg * (BITS * 4) + (DP == 128 ? (n & 3) * BITS : BITS == 8 ? (n & 7) * 4 : (n >> 1 & 3) * 4);
+        k_ends = k_slot + ends + kg * 4, v_ends = v_slot + ends + vg * 4;
     }
-    static __device__ __forceinline__ int slot(int i) { return i < 4 ? i : 12 + i; }      // of a lane's i-th value, less 4 g
-    static __device__ __forceinline__ uint32_t word(const char *p, uint32_t off) { return *(const uint32_t *)(p + off); }
-    template <int N> static __device__ __forceinline__ void words(uint32_t (&w)[N], const char *p, uint32_t off)
+    static __device__ __forceinline__ constexpr int slot(int i) { return i < 4 ? i : 12 + i; }      // of a lane's i-th value, less 4 g
+    // Rows at .. last, 32 at most, which are less than 2^30 bytes; none if there are none, however far `at` is behind.  (A load's
+    // scalar offset is taken off the range before it is checked, so there is none: rows further on have a descriptor of their own.)
+    struct Tile32 {
+        const char *base;
+        int row, size;
+        __device__ __forceinline__ Tile32(const char *from, int64_t row_, int at, int last, uint32_t row_bytes) : base(from + (int64_t)at * row_), row((int)row_)
+        {
+            const int n = last - at;
+            size = (int)(((uint32_t)min(TS - 1, n) * (uint32_t)row + row_bytes) & ~(uint32_t)(n >> 31));
+        }
+        __device__ __forceinline__ __amdgpu_buffer_rsrc_t from(int i) const { return bytes_at(base + i * row, max(size - i * row, 0)); }
+    };
+    template <int N> static __device__ __forceinline__ void words(uint32_t (&w)[N], __amdgpu_buffer_rsrc_t from, int off)
     {
         if constexpr (N % 4 == 0) {
 #pragma unroll
             for (int i = 0; i < N; i += 4) {
-                const u32x4 x = *(const u32x4 *)(p + off + 4 * i);
+                const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(from, off + 4 * i, 0, 0);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) w[i + j] = x[j];
             }
         } else if constexpr (N == 2) {
-            const uint2 x = *(const uint2 *)(p + off);
-            w[0] = x.x, w[1] = x.y;
+            const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(from, off, 0, 0);
+            w[0] = x[0], w[1] = x[1];
         } else {
-            w[0] = word(p, off);
+            w[0] = __builtin_amdgcn_raw_buffer_load_b32(from, off, 0, 0);
         }
     }
-    // keys of slots at .. at + 31; those past `last` are copies of it (at <= last)
+    // keys of slots at .. at + 31, as far as `last`
     __device__ __forceinline__ void keys(W &w, int at, int last) const
     {
-        const char *base = k + (int64_t)at * k_row;
-        if (at + TS - 1 <= last) {
+        const Tile32 tile(k, k_row, at, last, row_bytes);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const char *p = base + 16 * h * k_row;
-                words(w.k[h], p, k_at), w.k_ends[h] = word(p, k_at + k_gap);
-            }
-        } else {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint32_t off = (uint32_t)min(16 * h + n, last - at) * (uint32_t)k_row + k_lane;
-                words(w.k[h], base, off), w.k_ends[h] = word(base, off + k_gap);
-            }
+        for (int h = 0; h < 2; ++h) {
+            const auto from = tile.from(16 * h);
+            words(w.k[h], from, k_at);
+            w.k_ends[h] = __builtin_amdgcn_raw_buffer_load_b32(from, k_ends, 0, 0);
         }
     }
     __device__ __forceinline__ void values(W &w, int at, int last) const
     {
-        const char *base = v + (int64_t)at * v_row;
-        if (at + TS - 1 <= last) {
+        const Tile32 tile(v, v_row, at, last, row_bytes);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const char *p = base + slot(i) * v_row;
-                words(w.v[i], p, v_at), w.v_ends[i] = word(p, v_at + v_gap);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t off = (uint32_t)min(4 * g + slot(i), last - at) * (uint32_t)v_row + v_lane;
-                words(w.v[i], base, off), w.v_ends[i] = word(base, off + v_gap);
-            }
+        for (int i = 0; i < 8; ++i) {
+            const auto from = tile.from(slot(i));
+            words(w.v[i], from, v_at);
+            w.v_ends[i] = __builtin_amdgcn_raw_buffer_load_b32(from, v_ends, 0, 0);
         }
     }
 };
@@ -152,97 +154,123 @@ template <class T, int BITS, int DP> struct Columns {
     {
         constexpr int PER = BITS == 4 ? 4 : 2;                  // places of a half
         constexpr int HALVES = N / PER;                         // low and high ones of a lane's words
-        u32x4 x[N];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {                           // two slots at a time
-            const Pair<T, BITS> ends(w.v_ends[2 * s], w.v_ends[2 * s + 1]);
+        for (int h = 0; h < HALVES; ++h) {
+            u32x4 x[PER];
 #pragma unroll
-            for (int h = 0; h < HALVES; ++h) {
-                const uint32_t a = w.v[2 * s][h / 2], b = w.v[2 * s + 1][h / 2];
-                const uint32_t side = HALVES == 1 ? __builtin_amdgcn_perm(b, a, lane & 1 ? 0x07060302u : 0x05040100u) : h % 2 ? high_halves(a, b) : low_halves(a, b);
-#pragma unroll
-                for (int p = 0; p < PER; ++p) x[h * PER + p][s] = ends.get(side, p);
+            for (int s = 0; s < 4; ++s) {                       // two slots at a time
+                const Pair<T, BITS> ends(w.v_ends[2 * s], w.v_ends[2 * s + 1]);
+                const Levels<BITS> side = side_by_side<BITS>(w.v[2 * s][h / 2], w.v[2 * s + 1][h / 2], HALVES == 1 ? lane & 1 : h % 2);
+                x[0][s] = ends.template get<0>(side), x[1][s] = ends.template get<1>(side);
+                if constexpr (PER == 4) x[2][s] = ends.template get<2>(side), x[3][s] = ends.template get<3>(side);
             }
-        }
 #pragma unroll
-        for (int j = 0; j < N; ++j) f(j, __builtin_bit_cast(typename Elem<T>::x8, x[j]));
+            for (int j = 0; j < PER; ++j) f(h * PER + j, __builtin_bit_cast(typename Elem<T>::x8, x[j]));
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
 };
 
 template <class T, int BITS, int DP, int NR, int NW, Form FORM>
-__global__ __launch_bounds__(NW * 64, 2) void k_step_packed(StepShape s, StepWork w)
+__global__ __launch_bounds__(NW * 64, NR == 2 ? 3 : 4) void k_step_packed(StepShape s, StepWork w, bool many)
 {
     constexpr bool WHOLE = FORM != Form::CHUNK, IN_LDS = FORM == Form::WHOLE_IN_LDS;
     constexpr int R = 16 * NR, BOXES = NW / 2, PITCH = BOXES * DP + 4;
     __shared__ __align__(16) float kept[IN_LDS ? WHOLE_SCORES : 4];
     __shared__ __align__(16) float outs[R * PITCH];      // [row][half of the waves][DP]
+    __shared__ typename Elem<T>::x8 queries[NR][DP / 32][64];
     __shared__ float2 sums[NW][R];
     __shared__ float l2[R], totals[R];      // of a row: logarithm to base 2 of the whole sum, the sum on the maximum
-    const uint32_t group = s.q_heads / s.kv_heads * s.tokens, parts = (group + R - 1) / R;      // rows of queries of a key head
-    const uint32_t rows = s.batch * s.kv_heads * parts;
-    const uint32_t row = rows >= 256 ? blockIdx.x % rows : blockIdx.x / s.splits;
-    const uint32_t split = rows >= 256 ? blockIdx.x / rows : (blockIdx.x + row) % s.splits, part = row % parts;
-    const uint32_t kvh = row / parts % s.kv_heads, b = row / parts / s.kv_heads;
+    const uint32_t group = s.group, parts = (group + R - 1) / R;      // rows of queries of a key head
+    // Many caches: next to each other, so that the last chunks of ragged ones, which are empty, come last and to all dies.  Few: the
+    // chunks of one next to each other, which memory prefers.
+    const uint32_t b = many ? blockIdx.y : blockIdx.z, of_head = many ? blockIdx.x : blockIdx.y;
+    const uint32_t split = many ? blockIdx.z : (blockIdx.x + of_head) % s.splits;      // (not the last ones of all on one die)
+    const uint32_t kvh = parts == 1 ? of_head : of_head / parts, part = of_head - kvh * parts;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     const int n_rows = min(R, (int)(group - part * R)), first = (int)(kvh * group + part * R);      // of this workgroup, first of all of the sequence
     const int64_t row0 = (int64_t)b * s.q_heads * s.tokens + first;
     const int len = clamp_len(s.lens, b, s.slots), tokens = clamp_len(s.q_lens, b, s.tokens);
     const int c0 = split * s.chunk, c1 = min(c0 + (int)s.chunk, len);
 
-    typename Elem<T>::x8 qf[NR][DP / 32];
+    const int all_see = tokens == (int)s.tokens ? len - (int)(s.tokens - 1) : 0;      // slots below this one: every row
+    // Queries as operands, a wave's share of them for all waves: in registers they would cost a fifth of the waves that fit.
+    static_assert(NW >= DP / 32, "an operand for each wave at most");
+    typename Elem<T>::x8 mine[NR];
     int sees[NR];      // slots below this one
 #pragma unroll
     for (int a = 0; a < NR; ++a) {
-        const uint32_t of = (uint32_t)(first + min(16 * a + n, n_rows - 1)), head = of / s.tokens, token = of % s.tokens;
+        const uint32_t of = (uint32_t)(first + min(16 * a + n, n_rows - 1)), head = s.tokens == 1 ? of : of / s.tokens, token = of - head * s.tokens;
         sees[a] = (int)token < tokens ? len - (tokens - 1 - (int)token) : 0;
-        const T *q = (const T *)w.q.data + (int64_t)b * w.q.batch + (int64_t)head * w.q.head + (int64_t)token * w.q.row;
-#pragma unroll
-        for (int j = 0; j < DP / 32; ++j) {
-            const uint32_t e = (DP / 4) * g + 8 * j;
-            const typename Elem<T>::x8 z = {};
-            qf[a][j] = e < s.head_dim ? *(const typename Elem<T>::x8 *)(q + e) : z;
-        }
+        const uint32_t e = (DP / 4) * g + 8 * wave;
+        mine[a] = typename Elem<T>::x8{};
+        if (wave < DP / 32 && e < s.head_dim)
+            mine[a] = *(const typename Elem<T>::x8 *)((const T *)w.q.data + (int64_t)b * w.q.batch + (int64_t)head * w.q.head + (int64_t)token * w.q.row + e);
     }
-    const int all_see = tokens == (int)s.tokens ? len - (int)(s.tokens - 1) : 0;      // slots below this one: every row
     const Loader<BITS, DP> from(w.k, w.v, b, kvh, s.head_dim, lane);
     const int32_t *pos = w.positions ? w.positions + ((int64_t)b * s.kv_heads + kvh) * s.slots : nullptr;
+    // Every pass asks for the same loads and stores, of nothing where there is nothing: what is in flight is then known when
+    // the code is compiled, and a wait for the keys is none for the values that were asked for after them.
+    const auto places = [&](int at) {
+        return (int)__builtin_amdgcn_raw_buffer_load_b32(bytes_at(pos + at, uniform(pos ? max(0, min(TS, c1 - at)) * 4 : 0)), (lane & 31) * 4, 0, 0);
+    };
+    Words<BITS, DP> words;
+    int place;
+    int at = c0 + wave * TS;
+    place = places(at), from.keys(words, at, c1 - 1);
+    __builtin_amdgcn_sched_barrier(0);      // in the order in which the loop asks for them
+    from.values(words, at, c1 - 1);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int a = 0; a < NR; ++a)
+        if (wave < DP / 32) {
+            typename Elem<T>::x8 y;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = mine[a][held<BITS>(i)];
+            queries[a][wave][lane] = y;
+        }
+    __syncthreads();
+    // of the chunk's tiles: [tile][row of the key head][slot]
+    float *const scores = w.scores + (int64_t)(b * s.kv_heads + kvh) * s.score_row * group + (int64_t)part * R * TS;
     const uint32_t pitch = IN_LDS ? score_pitch(s.slots) : 0;
     const float c = s.scale * LOG2E;
-    constexpr float TIMES = IS_F16<T> ? 12.f : 0.f;      // p as a multiple of 2^-TIMES
+    constexpr float TIMES = IS_F16<T> ? 10.f : 0.f;      // p as a multiple of 2^-TIMES
+    constexpr float SLACK = 5.f;                         // by how much the running maximum, in base 2, may be left behind
 
     f32x4 acc[NR][DP / 16] = {};
     float m[NR], l[NR];
 #pragma unroll
-    for (int a = 0; a < NR; ++a) m[a] = LOWEST * c, l[a] = 0.f;
-    Words<BITS, DP> words;
-    int at = c0 + wave * TS;
-    int held = 0;
-    const auto places = [&](int at) { return pos ? pos[min(at + (lane & 31), len - 1)] : 0; };
-    if (at < c1) held = places(at), from.keys(words, at, len - 1), from.values(words, at, len - 1);
+    for (int a = 0; a < NR; ++a) m[a] = LOWEST, l[a] = 0.f;
     for (; at < c1; at += NW * TS) {
-        const bool more = at + NW * TS < c1;
+        const int next = at + NW * TS;
+        asm volatile("" ::: "memory");      // the queries are not to be kept in registers
         f32x4 x[NR][2] = {};
+        const Pair<T, BITS> ends[2] = {Pair<T, BITS>(words.k_ends[0]), Pair<T, BITS>(words.k_ends[1])};
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const Pair<T, BITS> ends(words.k_ends[h]);
+        for (int j = 0; j < DP / 32; ++j) {
+            typename Elem<T>::x8 q[NR];
 #pragma unroll
-            for (int j = 0; j < DP / 32; ++j) {
-                const auto k = eight_of<T, BITS>(words.k[h] + j * (BITS / 4), ends);
+            for (int a = 0; a < NR; ++a) q[a] = queries[a][j][lane];
 #pragma unroll
-                for (int a = 0; a < NR; ++a) x[a][h] = Small<T>::mfma(k, qf[a][j], x[a][h]);
+            for (int h = 0; h < 2; ++h) {
+                const auto k = __builtin_bit_cast(typename Elem<T>::x8, eight_as_held<T, BITS>(words.k[h] + j * (BITS / 4), ends[h]));
+#pragma unroll
+                for (int a = 0; a < NR; ++a) x[a][h] = Small<T>::mfma(k, q[a], x[a][h]);
             }
         }
-        const uint32_t live = (uint32_t)__ballot(held >= 0);      // one bit for each slot of the tile
-        if (more) held = places(at + NW * TS), from.keys(words, at + NW * TS, len - 1);
+        const uint32_t live = (uint32_t)__ballot(place >= 0);      // one bit for each slot of the tile
+        place = places(next), from.keys(words, next, c1 - 1);
         float p[NR][8];
 #pragma unroll
         for (int a = 0; a < NR; ++a)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) p[a][i] = x[a][i / 4][i % 4] * c;
+            for (int i = 0; i < 8; ++i) p[a][i] = x[a][i / 4][i % 4];
         if (live != ~0u || at + TS > all_see) {
+            int g4 = 4 * g;
+            asm volatile("" : "+v"(g4));      // or what comes of it is kept in registers throughout the loop
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int slot = 4 * g + from.slot(i);
+                const int slot = g4 + from.slot(i);
                 const bool used = (live >> slot) & 1;
 #pragma unroll
                 for (int a = 0; a < NR; ++a) p[a][i] = used && at + slot < sees[a] ? p[a][i] : -ATTN_INF;
@@ -266,31 +294,40 @@ __global__ __launch_bounds__(NW * 64, 2) void k_step_packed(StepShape s, StepWor
                 for (int i = 0; i < 8; ++i) {
                     const uint32_t e = words.v_ends[i];
                     const float y = IS_F16<T> ? (float)__builtin_bit_cast(f16x2, e)[0] : __uint_as_float(e << 16);
-                    if (4 * g + from.slot(i) == slot && y != y) words.v_ends[i] = 0;
+                    if (g4 + from.slot(i) == slot && y != y) words.v_ends[i] = 0;
                 }
             }
         }
 #pragma unroll
         for (int a = 0; a < NR; ++a) {
-            if (w.weights && 16 * a + n < n_rows) {
-                float *const to = IN_LDS ? kept + (16 * a + n) * pitch : w.scores + (row0 + 16 * a + n) * (int64_t)s.score_row;
-                *(f32x4 *)(to + at + 4 * g) = f32x4{p[a][0], p[a][1], p[a][2], p[a][3]};
-                *(f32x4 *)(to + at + 16 + 4 * g) = f32x4{p[a][4], p[a][5], p[a][6], p[a][7]};
+            const int r = 16 * a + n;
+            if constexpr (IN_LDS) {
+                if (w.weights && r < n_rows) {
+                    *(f32x4 *)(kept + r * pitch + at + 4 * g) = f32x4{p[a][0], p[a][1], p[a][2], p[a][3]};
+                    *(f32x4 *)(kept + r * pitch + at + 16 + 4 * g) = f32x4{p[a][4], p[a][5], p[a][6], p[a][7]};
+                }
+            } else {
+                const auto to = bytes_at(scores + (int64_t)at * group, w.weights ? n_rows * TS * 4 : 0);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{p[a][4 * h], p[a][4 * h + 1], p[a][4 * h + 2], p[a][4 * h + 3]}), to,
+                                                           r * (TS * 4) + 64 * h + 16 * g, 0, 0);
             }
             float top = p[a][0];
 #pragma unroll
             for (int i = 1; i < 8; ++i) top = fmaxf(top, p[a][i]);
             top = column_max(top);
-            if (__ballot(top > m[a])) {
-                const float up = fmaxf(m[a], top), by = exp2_fast(m[a] - up);
+            if (__ballot((top - m[a]) * c > SLACK)) {
+                const float up = fmaxf(m[a], top), by = exp2_fast((m[a] - up) * c);
                 m[a] = up;
                 l[a] *= by;
 #pragma unroll
                 for (int j = 0; j < DP / 16; ++j) acc[a][j] *= by;
             }
+            const float off = TIMES - m[a] * c;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                p[a][i] = exp2_fast(p[a][i] - (m[a] - TIMES));
+                p[a][i] = exp2_fast(__builtin_fmaf(p[a][i], c, off));
                 l[a] += p[a][i];
             }
         }
@@ -301,14 +338,14 @@ __global__ __launch_bounds__(NW * 64, 2) void k_step_packed(StepShape s, StepWor
 #pragma unroll
             for (int a = 0; a < NR; ++a) acc[a][j] = Small<T>::mfma(v, pf[a], acc[a][j]);
         });
-        if (more) from.values(words, at + NW * TS, len - 1);
+        from.values(words, next, c1 - 1);
     }
 
     // join the waves: their sums, then their outputs, each on the workgroup's maximum
-    constexpr float ONE = IS_F16<T> ? 0x1p-12f : 1.f;
+    constexpr float ONE = IS_F16<T> ? 0x1p-10f : 1.f;
 #pragma unroll
     for (int a = 0; a < NR; ++a) {
-        l[a] = column_sum(l[a]) * ONE;
+        l[a] = column_sum(l[a]) * ONE, m[a] *= c;
         if (g == 0) sums[wave][16 * a + n] = make_float2(m[a], l[a]);
     }
     __syncthreads();
@@ -366,7 +403,6 @@ __global__ __launch_bounds__(NW * 64, 2) void k_step_packed(StepShape s, StepWor
     }
     if constexpr (WHOLE) {
         if (!w.weights) return;
-        const float *const all = w.scores + row0 * (int64_t)s.score_row;
         const int64_t to = ((int64_t)b * s.kv_heads + kvh) * s.slots;
         const bool aligned = s.slots % 4 == 0 && ((uintptr_t)w.weights | (uintptr_t)w.before) % 16 == 0;
         for (uint32_t slot = threadIdx.x * 4; slot < s.slots; slot += NW * 64 * 4) {
@@ -374,8 +410,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_step_packed(StepShape s, StepWor
             if ((int)slot < len) {
 #pragma unroll 4
                 for (int r = 0; r < n_rows; ++r) {
-                    const f32x4 x = *(const f32x4 *)(IN_LDS ? kept + r * pitch + slot : all + (int64_t)r * s.score_row + slot);
-                    for (int j = 0; j < 4; ++j) sum[j] += exp2_fast(x[j] - l2[r]);
+                    const f32x4 x = *(const f32x4 *)(IN_LDS ? kept + r * pitch + slot : scores + (int64_t)(slot / TS) * (TS * n_rows) + r * TS + slot % TS);
+                    for (int j = 0; j < 4; ++j) sum[j] += exp2_fast(__builtin_fmaf(x[j], c, -l2[r]));
                 }
                 for (int j = 1; j < 4; ++j) sum[j] = (int)slot + j < len ? sum[j] : 0.f;
             }
@@ -391,20 +427,21 @@ __global__ __launch_bounds__(NW * 64, 2) void k_step_packed(StepShape s, StepWor
 
 template <class T, int BITS, int DP, int NR> hipError_t launch(const StepShape &s, const StepWork &w, hipStream_t st)
 {
-    const uint32_t rows = s.batch * s.kv_heads;
     if (s.whole) {
-        if (s.score_row) k_step_packed<T, BITS, DP, NR, WHOLE_WAVES, Form::WHOLE><<<rows, WHOLE_WAVES * 64, 0, st>>>(s, w);
-        else k_step_packed<T, BITS, DP, NR, WHOLE_WAVES, Form::WHOLE_IN_LDS><<<rows, WHOLE_WAVES * 64, 0, st>>>(s, w);
+        const dim3 grid(s.kv_heads, s.batch, 1);
+        if (s.score_row) k_step_packed<T, BITS, DP, NR, WHOLE_WAVES, Form::WHOLE><<<grid, WHOLE_WAVES * 64, 0, st>>>(s, w, true);
+        else k_step_packed<T, BITS, DP, NR, WHOLE_WAVES, Form::WHOLE_IN_LDS><<<grid, WHOLE_WAVES * 64, 0, st>>>(s, w, true);
         return hipGetLastError();
     }
-    const uint32_t group = s.q_heads / s.kv_heads * s.tokens, parts = (group + 16 * NR - 1) / (16 * NR);
-    k_step_packed<T, BITS, DP, NR, CHUNK_WAVES, Form::CHUNK><<<s.splits * parts * rows, CHUNK_WAVES * 64, 0, st>>>(s, w);
+    const uint32_t heads = s.kv_heads * ((s.group + 16 * NR - 1) / (16 * NR));
+    const bool many = (uint64_t)s.batch * heads >= 256 && s.splits <= 65535;
+    k_step_packed<T, BITS, DP, NR, CHUNK_WAVES, Form::CHUNK><<<many ? dim3(heads, s.batch, s.splits) : dim3(s.splits, heads, s.batch), CHUNK_WAVES * 64, 0, st>>>(s, w, many);
     const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? launch_step_join(s, w, st) : e;
+    return e == hipSuccess ? launch_packed_join(s, w, st) : e;
 }
 template <class T, int BITS, int DP> hipError_t launch(const StepShape &s, const StepWork &w, hipStream_t st)
 {
-    return s.q_heads / s.kv_heads * s.tokens <= 16 ? launch<T, BITS, DP, 1>(s, w, st) : launch<T, BITS, DP, 2>(s, w, st);
+    return s.group <= 16 ? launch<T, BITS, DP, 1>(s, w, st) : launch<T, BITS, DP, 2>(s, w, st);
 }
 template <class T> hipError_t launch(const StepShape &s, const StepWork &w, uint32_t bits, hipStream_t st)
 {
@@ -422,10 +459,11 @@ static bool whole_caches(uint64_t rows, uint32_t slots)
 
 void packed_step_split(StepShape &s)
 {
-    const uint32_t group = s.q_heads / s.kv_heads * s.tokens, of_part = group <= 16 ? 16 : 32;
+    s.group = s.q_heads / s.kv_heads * s.tokens;
+    const uint32_t group = s.group, of_part = group <= 16 ? 16 : 32;
     const uint64_t rows = (uint64_t)s.batch * s.kv_heads * ((group + of_part - 1) / of_part);
     const uint64_t least = CHUNK_WAVES * TS, most = 2048;
-    const uint64_t want = (uint64_t)s.slots * rows / 2048;
+    const uint64_t want = (uint64_t)s.slots * rows / 1024;
     const uint64_t chunk = (want < least ? least : want > most ? most : want) / least * least;
     s.chunk = (uint32_t)chunk;
     s.splits = (uint32_t)((s.slots + chunk - 1) / chunk);

@@ -38,6 +38,7 @@ uint32_t weights_parts(const AttnShape &s);
 hipError_t launch_attention_weights(const AttnShape &s, const Rows &q, const Rows &k, const float *lse, const float *before, float *weights,
                                     float *sums, hipStream_t st);
 
+constexpr uint32_t SCORE_TILE = 32;
 constexpr uint32_t MAX_GROUP = 256;      // rows of queries (heads times tokens) that share one key head in a step
 
 struct StepShape {
@@ -47,6 +48,7 @@ struct StepShape {
     bool half;
     uint32_t tokens;             // of every sequence (of rows in 16 bits: 1)
     const int32_t *q_lens;       // how many of them are in use, NULL: all
+    uint32_t group;              // rows of queries of a key head (set by packed_step_split)
     uint32_t chunk, splits;      // slots of a workgroup, workgroups of a cache (step_split)
     uint64_t score_row;          // floats between two heads' scores (0: they stay in LDS)
     bool whole;                  // one workgroup for all of a cache, and nothing to join
@@ -58,11 +60,11 @@ struct StepWork {
     float *lse, *weights;
     float *outs;            // [batch, q_heads, tokens, splits, 64 or 128]
     float2 *sums;           // [batch, q_heads, tokens, splits]: maximum in base 2, sum
-    float *scores;          // [batch, q_heads, tokens, score_row] in base 2, where weights are asked for
+    float *scores;          // [batch, q_heads, tokens, score_row] in base 2, where weights are asked for; packed: q.k [batch,
+                            // kv_heads, score_row / SCORE_TILE, rows of a key head, SCORE_TILE]
 };
 void step_split(StepShape &s);
 hipError_t launch_attention_step(const StepShape &s, const StepWork &w, hipStream_t st);
-hipError_t launch_step_join(const StepShape &s, const StepWork &w, hipStream_t st);
 
 // caches in 4 or 8 bits an element: packed_rows.h
 constexpr int PACK_GROUP = 32;
@@ -75,6 +77,7 @@ __host__ __device__ __forceinline__ uint32_t pack_row_bytes(uint32_t head_dim, u
 }
 
 void packed_step_split(StepShape &s);
+hipError_t launch_packed_join(const StepShape &s, const StepWork &w, hipStream_t st);
 hipError_t launch_attention_step_packed(const StepShape &s, const StepWork &w, uint32_t bits, hipStream_t st);
 
 struct PackShape {

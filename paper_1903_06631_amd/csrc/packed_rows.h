@@ -21,63 +21,97 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
-// lo and step of the two numbers of a pair, and a pair of levels as the numbers that they stand for: `place` counts the
-// pairs of a word from its lowest bits
+// Levels as numbers, two by two.  Words of 4 bits are split into two whose bytes are levels below 16: as numbers of eight bits with
+// three of fraction, such a byte is that many 2^-9, exactly, and one instruction converts two.  Masks, shifts to the right,
+// sums and products of 32 bits take half of the time of other vector instructions (and of packed ones of 16 bits), so a pair of binary16
+// costs 2.4 of the latter (with masked levels as the fraction of 1024 or 64, less that: 3.1), one of bfloat16 3.4 (each level
+// masked and converted alone: 4.4).  In 8 bits 3 and 4.
+template <int BITS> struct Levels;
+template <> struct Levels<4> {
+    uint32_t w[2];
+    __device__ __forceinline__ explicit Levels(uint32_t x) : w{x & 0x0F0F0F0Fu, (x >> 4) & 0x0F0F0F0Fu} {}
+};
+template <> struct Levels<8> {
+    uint32_t w;
+    __device__ __forceinline__ explicit Levels(uint32_t x) : w(x) {}
+};
+
+// Words of two slots, their levels two by two of the same element: place p of the low (or high) halves holds element 2 p (+ 1).
+template <int BITS> __device__ __forceinline__ Levels<BITS> side_by_side(uint32_t a, uint32_t b, bool high)
+{
+    const uint32_t sel = BITS == 4 ? (high ? 0x07030602u : 0x05010400u) : high ? 0x07060302u : 0x05040100u;
+    return Levels<BITS>(__builtin_amdgcn_perm(b, a, sel));
+}
+// A word of one row: place p holds, in 4 bits, elements e and e + 4, e = 0 2 1 3; in 8 bits 2 p and 2 p + 1.
+constexpr int HELD_4[8] = {0, 4, 2, 6, 1, 5, 3, 7};
+template <int BITS> __device__ __forceinline__ constexpr int held(int i) { return BITS == 4 ? HELD_4[i] : i; }      // of eight elements
+
+// lo and step of the two numbers of a pair, and what a pair of levels stands for
 template <class T, int BITS> struct Pair;
 
-// binary16: levels as the fraction of 1024 or 64 plus themselves, less that; one instruction for both of a pair, and lo + u
-// step is rounded once
+// binary16: one instruction for both, lo + u step is rounded once
 template <int BITS> struct Pair<_Float16, BITS> {
     f16x2 lo, step;
-    __device__ __forceinline__ explicit Pair(uint32_t ends)      // of one group
-    {
-        lo = __builtin_bit_cast(f16x2, low_halves(ends, ends)), step = __builtin_bit_cast(f16x2, high_halves(ends, ends));
-    }
-    __device__ __forceinline__ Pair(uint32_t a, uint32_t b)      // of two rows' groups
+    __device__ __forceinline__ explicit Pair(uint32_t ends) : Pair(ends, ends) {}      // of one group
+    __device__ __forceinline__ Pair(uint32_t a, uint32_t b)                            // of two rows' groups
     {
         lo = __builtin_bit_cast(f16x2, low_halves(a, b)), step = __builtin_bit_cast(f16x2, high_halves(a, b));
     }
-    __device__ __forceinline__ uint32_t get(uint32_t w, int place) const
+    template <int PLACE> __device__ __forceinline__ uint32_t get(const Levels<BITS> &x) const
     {
         f16x2 u;
-        if (BITS == 8) {
-            u = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, w, place ? 0x04030401u : 0x04020400u)) - (_Float16)1024;
-        } else {
-            if (place >= 2) w >>= 8;
-            if (place & 1) u = __builtin_bit_cast(f16x2, (w & 0x00F000F0u) | 0x54005400u) - (_Float16)64;
-            else u = __builtin_bit_cast(f16x2, (w & 0x000F000Fu) | 0x64006400u) - (_Float16)1024;
+        if constexpr (BITS == 4) {
+            u = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x.w[PLACE & 1], 512.f, PLACE >> 1));
+        } else {      // as the fraction of 1024
+            u = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, x.w, PLACE ? 0x04030401u : 0x04020400u)) - (_Float16)1024;
         }
         return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(u, step, lo));
     }
 };
 
-// bfloat16 has no such instructions: levels as 32-bit numbers, one at a time, u step exact, the sum rounded to 24 bits and then
-// to eight
+// bfloat16 has no such instruction: u step exact, the sum rounded to 24 bits and then to eight
 template <int BITS> struct Pair<__bf16, BITS> {
+    static constexpr float UNIT = BITS == 4 ? 512.f : 1.f;      // of the step for the levels as they are converted
     float lo[2], step[2];
     __device__ __forceinline__ explicit Pair(uint32_t ends) : Pair(ends, ends) {}
     __device__ __forceinline__ Pair(uint32_t a, uint32_t b)
     {
-        lo[0] = __uint_as_float(a << 16), step[0] = __uint_as_float(a & 0xFFFF0000u);
-        lo[1] = __uint_as_float(b << 16), step[1] = __uint_as_float(b & 0xFFFF0000u);
+        lo[0] = __uint_as_float(a << 16), step[0] = __uint_as_float(a & 0xFFFF0000u) * UNIT;
+        lo[1] = __uint_as_float(b << 16), step[1] = __uint_as_float(b & 0xFFFF0000u) * UNIT;
     }
-    __device__ __forceinline__ uint32_t get(uint32_t w, int place) const
+    template <int PLACE> __device__ __forceinline__ uint32_t get(const Levels<BITS> &x) const
     {
-        if (BITS == 4) w = (place & 1 ? w >> 4 : w) & 0x0F0F0F0Fu;
-        const int byte = BITS == 4 ? place / 2 : place;
-        const float u0 = (float)((w >> (8 * byte)) & 0xFF), u1 = (float)((w >> (16 + 8 * byte)) & 0xFF);
-        const bf16x2 x = {(__bf16)__builtin_fmaf(u0, step[0], lo[0]), (__bf16)__builtin_fmaf(u1, step[1], lo[1])};
-        return __builtin_bit_cast(uint32_t, x);
+        float u[2];
+        if constexpr (BITS == 4) {
+            const auto y = __builtin_amdgcn_cvt_pk_f32_fp8(x.w[PLACE & 1], PLACE >> 1);
+            u[0] = y[0], u[1] = y[1];
+        } else {
+            u[0] = (float)((x.w >> (8 * PLACE)) & 0xFF), u[1] = (float)((x.w >> (16 + 8 * PLACE)) & 0xFF);
+        }
+        const bf16x2 y = {(__bf16)__builtin_fmaf(u[0], step[0], lo[0]), (__bf16)__builtin_fmaf(u[1], step[1], lo[1])};
+        return __builtin_bit_cast(uint32_t, y);
     }
 };
 
-// eight elements of a row in order, from BITS / 4 words
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// eight elements of a row from BITS / 4 words, as they are held
+template <class T, int BITS> __device__ __forceinline__ u32x4 eight_as_held(const uint32_t *words, const Pair<T, BITS> &ends)
+{
+    if constexpr (BITS == 4) {
+        const Levels<4> x(words[0]);
+        return u32x4{ends.template get<0>(x), ends.template get<1>(x), ends.template get<2>(x), ends.template get<3>(x)};
+    } else {
+        const Levels<8> x(words[0]), y(words[1]);
+        return u32x4{ends.template get<0>(x), ends.template get<1>(x), ends.template get<0>(y), ends.template get<1>(y)};
+    }
+}
+// and in order
 template <class T, int BITS> __device__ __forceinline__ typename Elem<T>::x8 eight_of(const uint32_t *words, const Pair<T, BITS> &ends)
 {
-    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-    u32x4 x;
-#pragma unroll
-    for (int p = 0; p < 4; ++p) x[p] = BITS == 4 ? ends.get(words[0], p) : ends.get(words[p / 2], p % 2);
+    u32x4 x = eight_as_held<T, BITS>(words, ends);
+    if (BITS == 4) x = u32x4{low_halves(x[0], x[2]), low_halves(x[1], x[3]), high_halves(x[0], x[2]), high_halves(x[1], x[3])};
     return __builtin_bit_cast(typename Elem<T>::x8, x);
 }
 
