@@ -25,7 +25,7 @@ namespace {
 
 constexpr int TS = 32;                      // slots of a wave's tile
 constexpr uint32_t CHUNK_WAVES = 4;         // waves of a chunk's workgroup
-constexpr uint32_t WHOLE_WAVES = 8;         // and of one that goes through a whole cache
+constexpr uint32_t whole_waves(int nr) { return 8; }      // and of one that goes through a whole cache, all that a unit holds
 constexpr uint32_t WHOLE_SCORES = 6144;     // scores that the latter keeps in LDS
 
 __host__ __device__ __forceinline__ uint32_t score_pitch(uint32_t slots) { return (slots + TS - 1) / TS * TS + 4; }
@@ -235,12 +235,12 @@ __global__ __launch_bounds__(NW * 64, NR == 2 ? 3 : 4) void k_step_packed(StepSh
     const uint32_t pitch = IN_LDS ? score_pitch(s.slots) : 0;
     const float c = s.scale * LOG2E;
     constexpr float TIMES = IS_F16<T> ? 10.f : 0.f;      // p as a multiple of 2^-TIMES
-    constexpr float SLACK = 5.f;                         // by how much the running maximum, in base 2, may be left behind
+    const float slack = 5.f / c;                         // by how much the running maximum may be left behind: 2^5
 
     f32x4 acc[NR][DP / 16] = {};
-    float m[NR], l[NR];
+    float m[NR], limit[NR], off[NR], l[NR];      // limit: a product from which on m follows; off: what p's exponent is raised by
 #pragma unroll
-    for (int a = 0; a < NR; ++a) m[a] = LOWEST, l[a] = 0.f;
+    for (int a = 0; a < NR; ++a) m[a] = LOWEST, limit[a] = LOWEST + slack, off[a] = TIMES - LOWEST * c, l[a] = 0.f;
     for (; at < c1; at += NW * TS) {
         const int next = at + NW * TS;
         asm volatile("" ::: "memory");      // the queries are not to be kept in registers
@@ -316,18 +316,16 @@ __global__ __launch_bounds__(NW * 64, NR == 2 ? 3 : 4) void k_step_packed(StepSh
             float top = p[a][0];
 #pragma unroll
             for (int i = 1; i < 8; ++i) top = fmaxf(top, p[a][i]);
-            top = column_max(top);
-            if (__ballot((top - m[a]) * c > SLACK)) {
-                const float up = fmaxf(m[a], top), by = exp2_fast((m[a] - up) * c);
-                m[a] = up;
+            if (__ballot(top > limit[a])) {
+                const float up = fmaxf(m[a], column_max(top)), by = exp2_fast((m[a] - up) * c);
+                m[a] = up, limit[a] = up + slack, off[a] = TIMES - up * c;
                 l[a] *= by;
 #pragma unroll
                 for (int j = 0; j < DP / 16; ++j) acc[a][j] *= by;
             }
-            const float off = TIMES - m[a] * c;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                p[a][i] = exp2_fast(__builtin_fmaf(p[a][i], c, off));
+                p[a][i] = exp2_fast(__builtin_fmaf(p[a][i], c, off[a]));
                 l[a] += p[a][i];
             }
         }
@@ -429,8 +427,9 @@ template <class T, int BITS, int DP, int NR> hipError_t launch(const StepShape &
 {
     if (s.whole) {
         const dim3 grid(s.kv_heads, s.batch, 1);
-        if (s.score_row) k_step_packed<T, BITS, DP, NR, WHOLE_WAVES, Form::WHOLE><<<grid, WHOLE_WAVES * 64, 0, st>>>(s, w, true);
-        else k_step_packed<T, BITS, DP, NR, WHOLE_WAVES, Form::WHOLE_IN_LDS><<<grid, WHOLE_WAVES * 64, 0, st>>>(s, w, true);
+        constexpr uint32_t WAVES = whole_waves(NR);
+        if (s.score_row) k_step_packed<T, BITS, DP, NR, WAVES, Form::WHOLE><<<grid, WAVES * 64, 0, st>>>(s, w, true);
+        else k_step_packed<T, BITS, DP, NR, WAVES, Form::WHOLE_IN_LDS><<<grid, WAVES * 64, 0, st>>>(s, w, true);
         return hipGetLastError();
     }
     const uint32_t heads = s.kv_heads * ((s.group + 16 * NR - 1) / (16 * NR));
@@ -454,7 +453,7 @@ template <class T> hipError_t launch(const StepShape &s, const StepWork &w, uint
 static bool whole_caches(uint64_t rows, uint32_t slots)
 {
     const uint64_t rounds = (rows + 255) / 256;
-    return slots <= 1024 || (slots <= 2048 && rows >= 128) || (slots <= 4096 && rows >= 192 * rounds);
+    return slots <= 512 || (slots <= 1536 && slots <= 8 * rows) || (slots <= 8192 && 8 * rows >= 7 * 256 * rounds);
 }
 
 void packed_step_split(StepShape &s)
@@ -462,9 +461,9 @@ void packed_step_split(StepShape &s)
     s.group = s.q_heads / s.kv_heads * s.tokens;
     const uint32_t group = s.group, of_part = group <= 16 ? 16 : 32;
     const uint64_t rows = (uint64_t)s.batch * s.kv_heads * ((group + of_part - 1) / of_part);
-    const uint64_t least = CHUNK_WAVES * TS, most = 2048;
-    const uint64_t want = (uint64_t)s.slots * rows / 1024;
-    const uint64_t chunk = (want < least ? least : want > most ? most : want) / least * least;
+    const uint64_t least = CHUNK_WAVES * TS, most = 2048, places = 1024;
+    const uint64_t splits = rows < places ? places / rows : 1, want = ((s.slots + splits - 1) / splits + TS - 1) / TS * TS;
+    const uint64_t chunk = want < least ? least : want > most ? most : want;
     s.chunk = (uint32_t)chunk;
     s.splits = (uint32_t)((s.slots + chunk - 1) / chunk);
     if (!s.splits) s.splits = 1;

@@ -71,19 +71,18 @@ template <int BITS> struct Pair<_Float16, BITS> {
 
 // bfloat16 has no such instruction: u step exact, the sum rounded to 24 bits and then to eight
 template <int BITS> struct Pair<__bf16, BITS> {
-    static constexpr float UNIT = BITS == 4 ? 512.f : 1.f;      // of the step for the levels as they are converted
     float lo[2], step[2];
     __device__ __forceinline__ explicit Pair(uint32_t ends) : Pair(ends, ends) {}
     __device__ __forceinline__ Pair(uint32_t a, uint32_t b)
     {
-        lo[0] = __uint_as_float(a << 16), step[0] = __uint_as_float(a & 0xFFFF0000u) * UNIT;
-        lo[1] = __uint_as_float(b << 16), step[1] = __uint_as_float(b & 0xFFFF0000u) * UNIT;
+        lo[0] = __uint_as_float(a << 16), step[0] = __uint_as_float(a & 0xFFFF0000u);
+        lo[1] = __uint_as_float(b << 16), step[1] = __uint_as_float(b & 0xFFFF0000u);
     }
     template <int PLACE> __device__ __forceinline__ uint32_t get(const Levels<BITS> &x) const
     {
         float u[2];
         if constexpr (BITS == 4) {
-            const auto y = __builtin_amdgcn_cvt_pk_f32_fp8(x.w[PLACE & 1], PLACE >> 1);
+            const auto y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(x.w[PLACE & 1], 512.f, PLACE >> 1);
             u[0] = y[0], u[1] = y[1];
         } else {
             u[0] = (float)((x.w >> (8 * PLACE)) & 0xFF), u[1] = (float)((x.w >> (16 + 8 * PLACE)) & 0xFF);
