@@ -124,7 +124,7 @@ lap::Rows keys_of(const lap_attention_shape *s, const lap_rows *x) { return rows
 lap::StepShape step_of(const lap_attention_shape *s, bool packed)
 {
     lap::StepShape p = {s->batch, s->q_heads, s->kv_heads, s->k_len, s->head_dim, s->scale, s->k_lens, s->type == LAP_T_F16, packed ? s->q_len : 1,
-                        packed ? s->q_lens : nullptr, 0, 0, 0, 0, false};
+                        packed ? s->q_lens : nullptr, 0, 0, 0, 0, 0, false};
     if (packed) lap::packed_step_split(p);
     else lap::step_split(p);
     return p;
@@ -138,21 +138,37 @@ size_t ws_weights(const lap_attention_shape *s)
     const uint32_t parts = lap::weights_parts(shape_of(s));
     return parts == 1 ? 0 : up((size_t)s->batch * s->kv_heads * parts * s->k_len * 4);
 }
+// how much a step's outputs and sums of chunks, its scores and its table take
+struct StepBytes {
+    size_t outs, sums, scores, table;
+    size_t all() const { return outs + sums + scores + table; }
+};
+StepBytes bytes_of(const lap_attention_shape *s, const lap::StepShape &p, bool packed)
+{
+    const size_t rows = (size_t)s->batch * s->q_heads * p.tokens;
+    StepBytes n = {0, 0, up(rows * p.score_row * 4), 0};
+    if (p.whole) return n;
+    const size_t partial = packed ? (size_t)s->kv_heads * lap::step_parts(p.group) * p.shares * lap::step_part(p.group) : rows * p.splits;
+    n.outs = up(partial * padded_dim(s) * 4), n.sums = up(partial * sizeof(float2));
+    if (packed) n.table = up(s->batch * sizeof(uint2));
+    return n;
+}
+// the same whether there are lengths or not
 size_t ws_step(const lap_attention_shape *s, bool packed)
 {
-    const lap::StepShape p = step_of(s, packed);
-    const size_t rows = (size_t)s->batch * s->q_heads * p.tokens;
-    return p.whole ? up(rows * p.score_row * 4) : up(rows * p.splits * padded_dim(s) * 4) + up(rows * p.splits * sizeof(float2)) + up(rows * p.score_row * 4);
+    static const int32_t some = 0;
+    lap_attention_shape a = *s, b = *s;
+    a.k_lens = nullptr, b.k_lens = &some;
+    return std::max(bytes_of(&a, step_of(&a, packed), packed).all(), bytes_of(&b, step_of(&b, packed), packed).all());
 }
-void carve_step(lap::StepWork &w, const lap_attention_shape *s, const lap::StepShape &p, void *ws)
+void carve_step(lap::StepWork &w, const lap_attention_shape *s, const lap::StepShape &p, void *ws, bool packed)
 {
-    const size_t rows = (size_t)s->batch * s->q_heads * p.tokens;
+    const StepBytes n = bytes_of(s, p, packed);
     char *at = (char *)ws;
-    if (!p.whole) {
-        w.outs = (float *)at, at += up(rows * p.splits * padded_dim(s) * 4);
-        w.sums = (float2 *)at, at += up(rows * p.splits * sizeof(float2));
-    }
-    w.scores = (float *)at;
+    w.outs = (float *)at, at += n.outs;
+    w.sums = (float2 *)at, at += n.sums;
+    w.scores = (float *)at, at += n.scores;
+    w.table = (uint2 *)at;
 }
 
 // rows of bytes as rows of half as many 16-bit elements
@@ -326,8 +342,8 @@ int lap_attention_step(const lap_attention_shape *s, const lap_rows *q, const la
     if (!rc && s->k_len) rc = check_apart(out->data, {k->data, v->data});
     if (rc) return rc;
     const lap::StepShape p = step_of(s, false);
-    lap::StepWork w = {queries_of(s, q), keys_of(s, k), keys_of(s, v), queries_of(s, out), positions, before, lse, weights, nullptr, nullptr, nullptr};
-    carve_step(w, s, p, ws);
+    lap::StepWork w = {queries_of(s, q), keys_of(s, k), keys_of(s, v), queries_of(s, out), positions, before, lse, weights, nullptr, nullptr, nullptr, nullptr};
+    carve_step(w, s, p, ws, false);
     LAP_HIP(lap::launch_attention_step(p, w, (hipStream_t)hip_stream));
     return LAP_OK;
 }
@@ -419,8 +435,8 @@ int lap_attention_step_packed(const lap_attention_shape *s, const lap_rows *q, c
     if (rc) return rc;
     const lap::StepShape p = step_of(s, true);
     lap::StepWork w = {queries_of(s, q), packed_of(cache, &cache->k), packed_of(cache, &cache->v), queries_of(s, out), positions, before, lse, weights,
-                       nullptr, nullptr, nullptr};
-    carve_step(w, s, p, ws);
+                       nullptr, nullptr, nullptr, nullptr};
+    carve_step(w, s, p, ws, true);
     LAP_HIP(lap::launch_attention_step_packed(p, w, cache->bits, (hipStream_t)hip_stream));
     return LAP_OK;
 }

@@ -18,6 +18,7 @@
 // next keys when these ones are decoded, for the next values likewise.
 //
 // Chunks of long caches, one workgroup for short ones, the scores kept for the weights: as in attention_step.hip.
+#include "lap_dev.h"
 #include "packed_rows.h"
 
 namespace lap {
@@ -25,7 +26,7 @@ namespace {
 
 constexpr int TS = 32;                      // slots of a wave's tile
 constexpr uint32_t CHUNK_WAVES = 4;         // waves of a chunk's workgroup
-constexpr uint32_t whole_waves(int nr) { return 8; }      // and of one that goes through a whole cache, all that a unit holds
+constexpr uint32_t WHOLE_WAVES = 8;         // and of one that goes through a whole cache
 constexpr uint32_t WHOLE_SCORES = 6144;     // scores that the latter keeps in LDS
 
 __host__ __device__ __forceinline__ uint32_t score_pitch(uint32_t slots) { return (slots + TS - 1) / TS * TS + 4; }
@@ -171,8 +172,64 @@ template <class T, int BITS, int DP> struct Columns {
     }
 };
 
+// inclusive prefix sum over the wave
+__device__ __forceinline__ uint32_t wave_sums(uint32_t v)
+{
+    v += dpp_mov<0x111>(0u, v);
+    v += dpp_mov<0x112>(0u, v);
+    v += dpp_mov<0x114>(0u, v);
+    v += dpp_mov<0x118>(0u, v);
+    v += dpp_mov<0x142, 0xA>(0u, v);
+    v += dpp_mov<0x143, 0xC>(0u, v);
+    return v;
+}
+
+// Which slots of which sequence are a workgroup's.  Without lengths, chunks of s.chunk slots, as many for each sequence.  Lengths
+// are known on the GPU only, so it is there that all sequences are cut into chunks of one size, a number of tiles for each wave:
+// the least that makes no more of them than there are workgroups (for each key head), whatever the lengths are, as s.shares is
+// as many as chunks of all tiles plus one for each sequence.
+struct Share {
+    uint32_t b;
+    int len, first, slots;
+    bool any;
+};
+__device__ __forceinline__ Share share_of(const StepShape &s, uint32_t turn, uint2 *table, int lane)
+{
+    Share r = {};
+    if (!s.lens) {
+        const uint32_t n = s.shares / s.batch;
+        if (table)
+            for (uint32_t b = lane; b < s.batch; b += 64) table[b] = make_uint2(b * n, n);
+        r.any = true;
+        r.b = turn / n, r.len = (int)s.slots;
+        r.first = (int)((turn - r.b * n) * s.chunk), r.slots = (int)s.chunk;
+        return r;
+    }
+    const auto tiles_of = [&](uint32_t b) { return b < s.batch ? (uint32_t)(clamp_len(s.lens, b, s.slots) + TS - 1) / TS : 0; };
+    uint32_t own = tiles_of(lane), all = read_lane(wave_sums(own), 63);
+    for (uint32_t b = 64; b < s.batch; b += 64) all += read_lane(wave_sums(tiles_of(b + lane)), 63);
+    const uint32_t for_all = (s.shares - s.batch) * CHUNK_WAVES, each = uniform(max(1u, (all + for_all - 1) / for_all) * CHUNK_WAVES);      // tiles
+    uint32_t before = 0;
+    for (uint32_t b0 = 0; b0 < s.batch; b0 += 64) {
+        if (b0) own = tiles_of(b0 + lane);
+        const uint32_t n = (own + each - 1) / each, up = before + wave_sums(n);
+        if (table && b0 + lane < s.batch) table[b0 + lane] = make_uint2(up - n, n);
+        const int at = __popcll(ballot(up <= turn));      // sequences whose chunks all come before
+        if (!r.any && at < 64) {
+            r.any = true;
+            r.b = b0 + at;
+            r.len = uniform(clamp_len(s.lens, r.b, s.slots));
+            r.first = uniform((int)((turn - (read_lane(up, at) - read_lane(n, at))) * each * TS));
+            r.slots = (int)(each * TS);
+            if (!table) break;
+        }
+        before = read_lane(up, 63);
+    }
+    return r;
+}
+
 template <class T, int BITS, int DP, int NR, int NW, Form FORM>
-__global__ __launch_bounds__(NW * 64, NR == 2 ? 3 : 4) void k_step_packed(StepShape s, StepWork w, bool many)
+__global__ __launch_bounds__(NW * 64, NR == 2 ? 3 : 4) void k_step_packed(StepShape s, StepWork w)
 {
     constexpr bool WHOLE = FORM != Form::CHUNK, IN_LDS = FORM == Form::WHOLE_IN_LDS;
     constexpr int R = 16 * NR, BOXES = NW / 2, PITCH = BOXES * DP + 4;
@@ -182,16 +239,22 @@ __global__ __launch_bounds__(NW * 64, NR == 2 ? 3 : 4) void k_step_packed(StepSh
     __shared__ float2 sums[NW][R];
     __shared__ float l2[R], totals[R];      // of a row: logarithm to base 2 of the whole sum, the sum on the maximum
     const uint32_t group = s.group, parts = (group + R - 1) / R;      // rows of queries of a key head
-    // Many caches: next to each other, so that the last chunks of ragged ones, which are empty, come last and to all dies.  Few: the
-    // chunks of one next to each other, which memory prefers.
-    const uint32_t b = many ? blockIdx.y : blockIdx.z, of_head = many ? blockIdx.x : blockIdx.y;
-    const uint32_t split = many ? blockIdx.z : (blockIdx.x + of_head) % s.splits;      // (not the last ones of all on one die)
+    const uint32_t of_head = WHOLE ? blockIdx.x : blockIdx.x / s.shares, turn = WHOLE ? blockIdx.y : blockIdx.x - of_head * s.shares;
     const uint32_t kvh = parts == 1 ? of_head : of_head / parts, part = of_head - kvh * parts;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     const int n_rows = min(R, (int)(group - part * R)), first = (int)(kvh * group + part * R);      // of this workgroup, first of all of the sequence
-    const int64_t row0 = (int64_t)b * s.q_heads * s.tokens + first;
-    const int len = clamp_len(s.lens, b, s.slots), tokens = clamp_len(s.q_lens, b, s.tokens);
-    const int c0 = split * s.chunk, c1 = min(c0 + (int)s.chunk, len);
+    uint32_t b = turn;
+    int len, c0 = 0, c1;
+    if constexpr (WHOLE) {
+        c1 = len = clamp_len(s.lens, b, s.slots);
+    } else {
+        const Share mine = share_of(s, turn, blockIdx.x == 0 && wave == 0 ? w.table : nullptr, lane);
+        if (!mine.any) return;
+        b = mine.b, len = mine.len, c0 = mine.first, c1 = min(c0 + mine.slots, len);
+    }
+    const int tokens = clamp_len(s.q_lens, b, s.tokens);
+    const int64_t row0 = (int64_t)b * s.q_heads * s.tokens + first;      // of lse
+    const int64_t partial = (int64_t)blockIdx.x * R;                     // of outs and sums: [key head and part][share][row]
 
     const int all_see = tokens == (int)s.tokens ? len - (int)(s.tokens - 1) : 0;      // slots below this one: every row
     // Queries as operands, a wave's share of them for all waves: in registers they would cost a fifth of the waves that fit.
@@ -367,7 +430,7 @@ __global__ __launch_bounds__(NW * 64, NR == 2 ? 3 : 4) void k_step_packed(StepSh
                 l2[r] = some ? top + __log2f(total) : ATTN_INF;
                 totals[r] = total;
             } else {
-                w.sums[(row0 + r) * s.splits + split] = make_float2(top, total);
+                w.sums[partial + r] = make_float2(top, total);
             }
         }
     }
@@ -396,7 +459,7 @@ __global__ __launch_bounds__(NW * 64, NR == 2 ? 3 : 4) void k_step_packed(StepSh
             if (e < (int)s.head_dim)
                 *(typename Elem<T>::x4 *)((T *)w.out.data + (int64_t)b * w.out.batch + (int64_t)(of / s.tokens) * w.out.head + (int64_t)(of % s.tokens) * w.out.row + e) = o;
         } else {
-            *(f32x4 *)(w.outs + ((row0 + r) * s.splits + split) * DP + e) = z;
+            *(f32x4 *)(w.outs + (partial + r) * DP + e) = z;
         }
     }
     if constexpr (WHOLE) {
@@ -427,14 +490,11 @@ template <class T, int BITS, int DP, int NR> hipError_t launch(const StepShape &
 {
     if (s.whole) {
         const dim3 grid(s.kv_heads, s.batch, 1);
-        constexpr uint32_t WAVES = whole_waves(NR);
-        if (s.score_row) k_step_packed<T, BITS, DP, NR, WAVES, Form::WHOLE><<<grid, WAVES * 64, 0, st>>>(s, w, true);
-        else k_step_packed<T, BITS, DP, NR, WAVES, Form::WHOLE_IN_LDS><<<grid, WAVES * 64, 0, st>>>(s, w, true);
+        if (s.score_row) k_step_packed<T, BITS, DP, NR, WHOLE_WAVES, Form::WHOLE><<<grid, WHOLE_WAVES * 64, 0, st>>>(s, w);
+        else k_step_packed<T, BITS, DP, NR, WHOLE_WAVES, Form::WHOLE_IN_LDS><<<grid, WHOLE_WAVES * 64, 0, st>>>(s, w);
         return hipGetLastError();
     }
-    const uint32_t heads = s.kv_heads * ((s.group + 16 * NR - 1) / (16 * NR));
-    const bool many = (uint64_t)s.batch * heads >= 256 && s.splits <= 65535;
-    k_step_packed<T, BITS, DP, NR, CHUNK_WAVES, Form::CHUNK><<<many ? dim3(heads, s.batch, s.splits) : dim3(s.splits, heads, s.batch), CHUNK_WAVES * 64, 0, st>>>(s, w, many);
+    k_step_packed<T, BITS, DP, NR, CHUNK_WAVES, Form::CHUNK><<<s.kv_heads * step_parts(s.group) * s.shares, CHUNK_WAVES * 64, 0, st>>>(s, w);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? launch_packed_join(s, w, st) : e;
 }
@@ -456,22 +516,37 @@ static bool whole_caches(uint64_t rows, uint32_t slots)
     return slots <= 512 || (slots <= 1536 && slots <= 8 * rows) || (slots <= 8192 && 8 * rows >= 7 * 256 * rounds);
 }
 
+constexpr uint64_t FEW = 512, PLACES = 1024, PLACES_32 = 768;
 void packed_step_split(StepShape &s)
 {
     s.group = s.q_heads / s.kv_heads * s.tokens;
-    const uint32_t group = s.group, of_part = group <= 16 ? 16 : 32;
-    const uint64_t rows = (uint64_t)s.batch * s.kv_heads * ((group + of_part - 1) / of_part);
-    const uint64_t least = CHUNK_WAVES * TS, most = 2048, places = 1024;
-    const uint64_t splits = rows < places ? places / rows : 1, want = ((s.slots + splits - 1) / splits + TS - 1) / TS * TS;
-    const uint64_t chunk = want < least ? least : want > most ? most : want;
-    s.chunk = (uint32_t)chunk;
-    s.splits = (uint32_t)((s.slots + chunk - 1) / chunk);
-    if (!s.splits) s.splits = 1;
+    const uint64_t heads = (uint64_t)s.kv_heads * step_parts(s.group), rows = s.batch * heads;
     s.score_row = ((uint64_t)s.slots + TS - 1) / TS * TS;
-    s.whole = group <= 32 && whole_caches(rows, s.slots);
-    if (!s.whole) return;
-    s.chunk = s.slots, s.splits = 1;
-    if ((uint64_t)group * score_pitch(s.slots) <= WHOLE_SCORES) s.score_row = 0;
+    s.whole = s.group <= 32 && whole_caches(rows, s.slots);
+    s.chunk = s.splits = s.shares = 0;
+    if (!s.whole) {
+        const uint64_t tiles = s.score_row / TS, places = s.group <= 16 ? PLACES : PLACES_32;
+        // for each key head, of one sequence or of all of them
+        const uint64_t sequences = s.lens ? s.batch : 1, all = tiles * sequences;
+        const auto chunks = [&](uint64_t groups, uint64_t most) {
+            const uint64_t n = groups / heads / (s.batch / sequences);
+            // of all of them, half a chunk for each sequence besides, as the last ones are shorter
+            const uint64_t fits = sequences == 1 ? n : n > sequences ? n - sequences / 2 : n - n / 2;
+            return all <= fits * most ? fits : 0;
+        };
+        uint64_t n = chunks(FEW, 32);
+        if (!n) n = chunks(places, 64);
+        if (!n) n = (all + 63) / 64;
+        if (s.lens) {
+            s.shares = (uint32_t)(n + s.batch);
+        } else {
+            const uint64_t each = (tiles + n - 1) / n;
+            s.chunk = (uint32_t)((each < CHUNK_WAVES ? CHUNK_WAVES : each) * TS);
+            s.shares = (uint32_t)((s.slots + s.chunk - 1) / s.chunk * s.batch);
+        }
+        return;
+    }
+    if ((uint64_t)s.group * score_pitch(s.slots) <= WHOLE_SCORES) s.score_row = 0;
 }
 
 hipError_t launch_attention_step_packed(const StepShape &s, const StepWork &w, uint32_t bits, hipStream_t st)

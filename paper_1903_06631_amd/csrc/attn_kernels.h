@@ -48,7 +48,8 @@ struct StepShape {
     bool half;
     uint32_t tokens;             // of every sequence (of rows in 16 bits: 1)
     const int32_t *q_lens;       // how many of them are in use, NULL: all
-    uint32_t group;              // rows of queries of a key head (set by packed_step_split)
+    uint32_t group;              // rows of queries of a key head; this and the next by packed_step_split
+    uint32_t shares;             // workgroups for each part of a key head's rows, among which all sequences are shared out
     uint32_t chunk, splits;      // slots of a workgroup, workgroups of a cache (step_split)
     uint64_t score_row;          // floats between two heads' scores (0: they stay in LDS)
     bool whole;                  // one workgroup for all of a cache, and nothing to join
@@ -58,10 +59,11 @@ struct StepWork {
     const int32_t *positions;
     const float *before;
     float *lse, *weights;
-    float *outs;            // [batch, q_heads, tokens, splits, 64 or 128]
-    float2 *sums;           // [batch, q_heads, tokens, splits]: maximum in base 2, sum
+    float *outs;            // [batch, q_heads, splits, 64 or 128]; packed: [kv_heads, parts, shares, rows of a part, 64 or 128]
+    float2 *sums;           // the same without the last: maximum in base 2, sum
     float *scores;          // [batch, q_heads, tokens, score_row] in base 2, where weights are asked for; packed: q.k [batch,
                             // kv_heads, score_row / SCORE_TILE, rows of a key head, SCORE_TILE]
+    uint2 *table;           // packed: [batch] a sequence's first share, how many it has
 };
 void step_split(StepShape &s);
 hipError_t launch_attention_step(const StepShape &s, const StepWork &w, hipStream_t st);
@@ -76,6 +78,8 @@ __host__ __device__ __forceinline__ uint32_t pack_row_bytes(uint32_t head_dim, u
     return (pack_ends(head_dim, bits) + pack_groups(head_dim) * 4 + 15) / 16 * 16;
 }
 
+__host__ __device__ __forceinline__ uint32_t step_part(uint32_t group) { return group <= 16 ? 16 : 32; }      // rows of a workgroup
+__host__ __device__ __forceinline__ uint32_t step_parts(uint32_t group) { return (group + step_part(group) - 1) / step_part(group); }
 void packed_step_split(StepShape &s);
 hipError_t launch_packed_join(const StepShape &s, const StepWork &w, hipStream_t st);
 hipError_t launch_attention_step_packed(const StepShape &s, const StepWork &w, uint32_t bits, hipStream_t st);

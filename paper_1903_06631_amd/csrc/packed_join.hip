@@ -18,12 +18,12 @@ __device__ __forceinline__ float2 join_lanes(float2 a, uint32_t lanes)
     return a;
 }
 // and over a row's chunks, the lane-th of `lanes`
-__device__ __forceinline__ float2 join_chunks(const float2 *sums, uint32_t n, uint32_t lane, uint32_t lanes)
+__device__ __forceinline__ float2 join_chunks(const float2 *sums, uint32_t n, uint32_t stride, uint32_t lane, uint32_t lanes)
 {
-    float2 a = make_float2(sums[0].x, 0.f);
+    float2 a = make_float2(-__FLT_MAX__, 0.f);
 #pragma unroll 4
     for (uint32_t i = lane; i < n; i += lanes) {
-        const float2 x = sums[i];
+        const float2 x = sums[(int64_t)i * stride];
         const float top = fmaxf(a.x, x.x);
         a = make_float2(top, a.y * exp2_fast(a.x - top) + x.y * exp2_fast(x.x - top));
     }
@@ -44,17 +44,25 @@ __global__ __launch_bounds__(JOIN) void k_packed_join(StepShape s, StepWork w, u
         const uint32_t row = blockIdx.x * (JOIN_WAVES / waves) + wave / waves, first = wave % waves;
         f32xE y = {};
         float2 all = {};
+        const uint32_t b = row / of_one, of = row - b * of_one;
         if (row < rows) {
-            const float2 *sums = w.sums + (int64_t)row * s.splits;
-            const f32xE *outs = (const f32xE *)(w.outs + (int64_t)row * s.splits * DP) + lane;
-            all = join_lanes(join_chunks(sums, s.splits, lane, 64), 64);
-            for (uint32_t i = first; i < s.splits; i += waves * AHEAD) {
+            const uint32_t kvh = of / s.group, r = of - kvh * s.group, parts = step_parts(s.group), of_part = step_part(s.group);
+            const uint2 chunks = w.table[b];
+            const int64_t at = ((int64_t)(kvh * parts + r / of_part) * s.shares + chunks.x) * of_part + r % of_part;
+            const float2 *sums = w.sums + at;
+            const f32xE *outs = (const f32xE *)(w.outs + at * DP) + lane;
+            all = join_lanes(join_chunks(sums, chunks.y, of_part, lane, 64), 64);
+            for (uint32_t i = first; i < chunks.y; i += waves * AHEAD) {
                 f32xE x[AHEAD];
+                float m[AHEAD];
 #pragma unroll
-                for (int j = 0; j < AHEAD; ++j) x[j] = outs[(int64_t)min(i + j * waves, s.splits - 1) * 64];
+                for (int j = 0; j < AHEAD; ++j) {
+                    const int64_t k = (int64_t)min(i + j * waves, chunks.y - 1) * of_part;
+                    x[j] = outs[k * 64], m[j] = sums[k].x;
+                }
 #pragma unroll
-                for (int j = 0; j < AHEAD; ++j)      // a chunk without slots has written zeros
-                    if (i + j * waves < s.splits) y += x[j] * exp2_fast(sums[i + j * waves].x - all.x);
+                for (int j = 0; j < AHEAD; ++j)
+                    if (i + j * waves < chunks.y) y += x[j] * exp2_fast(m[j] - all.x);
             }
         }
         if (waves > 1) {
@@ -65,7 +73,7 @@ __global__ __launch_bounds__(JOIN) void k_packed_join(StepShape s, StepWork w, u
         }
         if (row >= rows || first) return;
         const bool some = all.y != 0.f;
-        const uint32_t b = row / of_one, head = row % of_one / s.tokens, token = row % s.tokens, e = lane * E;
+        const uint32_t head = s.tokens == 1 ? of : of / s.tokens, token = of - head * s.tokens, e = lane * E;
         typedef T TE __attribute__((ext_vector_type(E)));
         TE z;
         for (int j = 0; j < E; ++j) z[j] = (T)(some ? y[j] / all.y : 0.f);
@@ -77,7 +85,7 @@ __global__ __launch_bounds__(JOIN) void k_packed_join(StepShape s, StepWork w, u
     __shared__ f32x4 shares[JOIN];
     const uint32_t group = s.group;
     const uint32_t item = (blockIdx.x - row_groups) / pieces, piece = (blockIdx.x - row_groups) % pieces;
-    const uint32_t b = item / s.kv_heads, row0 = item * group;
+    const uint32_t b = item / s.kv_heads, row0 = item * group, of_part = step_part(group);
     const int len = clamp_len(s.lens, b, s.slots);
     const uint32_t quads = each / 4, share = threadIdx.x / quads, of = JOIN / quads;
     const uint32_t slot = piece * each + threadIdx.x % quads * 4;
@@ -90,9 +98,12 @@ __global__ __launch_bounds__(JOIN) void k_packed_join(StepShape s, StepWork w, u
         for (int j = 0; j < AHEAD; ++j)
             if (share + j * of < group) x[j] = *(const f32x4 *)(from + (share + j * of) * SCORE_TILE);
     const uint32_t lanes = group <= 4 ? 64 : group <= 8 ? 32 : group <= 16 ? 16 : 8, at_once = JOIN / lanes;      // lanes of a row
+    const uint2 chunks = w.table[b];
+    const int64_t of_head = (int64_t)(item - b * s.kv_heads) * step_parts(group);
     for (uint32_t r = threadIdx.x / lanes; r < (group + at_once - 1) / at_once * at_once; r += at_once) {
-        const uint32_t l = lane % lanes;
-        const float2 all = join_lanes(join_chunks(w.sums + (int64_t)(row0 + min(r, group - 1)) * s.splits, s.splits, l, lanes), lanes);
+        const uint32_t l = lane % lanes, row = min(r, group - 1);
+        const float2 *sums = w.sums + ((of_head + row / of_part) * s.shares + chunks.x) * of_part + row % of_part;
+        const float2 all = join_lanes(join_chunks(sums, chunks.y, of_part, l, lanes), lanes);
         if (l == 0 && r < group) l2[r] = all.y != 0.f ? all.x + __log2f(all.y) : ATTN_INF;
     }
     __syncthreads();
@@ -129,7 +140,7 @@ __global__ __launch_bounds__(JOIN) void k_packed_join(StepShape s, StepWork w, u
 
 template <class T, int DP> hipError_t launch(const StepShape &s, const StepWork &w, hipStream_t st)
 {
-    const uint32_t rows = s.batch * s.q_heads * s.tokens, waves = rows >= 1024 || s.splits <= AHEAD ? 1 : JOIN_WAVES;
+    const uint32_t rows = s.batch * s.q_heads * s.tokens, waves = rows >= 1024 || s.shares <= AHEAD * s.batch ? 1 : JOIN_WAVES;
     const uint32_t row_groups = (rows * waves + JOIN_WAVES - 1) / JOIN_WAVES;
     const uint64_t quads = (uint64_t)s.batch * s.kv_heads * ((s.slots + 3) / 4);
     const uint32_t each = quads >= 512 * JOIN ? 1024 : quads >= 128 * JOIN ? 256 : 128;
