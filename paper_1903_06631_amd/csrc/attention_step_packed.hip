@@ -197,7 +197,7 @@ __device__ __forceinline__ Share share_of(const StepShape &s, uint32_t turn, uin
 {
     Share r = {};
     if (!s.lens) {
-        const uint32_t n = s.shares / s.batch;
+        const uint32_t n = s.splits;
         if (table)
             for (uint32_t b = lane; b < s.batch; b += 64) table[b] = make_uint2(b * n, n);
         r.any = true;
@@ -205,20 +205,20 @@ __device__ __forceinline__ Share share_of(const StepShape &s, uint32_t turn, uin
         r.first = (int)((turn - r.b * n) * s.chunk), r.slots = (int)s.chunk;
         return r;
     }
-    const auto tiles_of = [&](uint32_t b) { return b < s.batch ? (uint32_t)(clamp_len(s.lens, b, s.slots) + TS - 1) / TS : 0; };
-    uint32_t own = tiles_of(lane), all = read_lane(wave_sums(own), 63);
-    for (uint32_t b = 64; b < s.batch; b += 64) all += read_lane(wave_sums(tiles_of(b + lane)), 63);
+    const auto length = [&](uint32_t b) { return b < s.batch ? (uint32_t)clamp_len(s.lens, b, s.slots) : 0; };
+    uint32_t own = length(lane), all = read_lane(wave_sums((own + TS - 1) / TS), 63);
+    for (uint32_t b = 64; b < s.batch; b += 64) all += read_lane(wave_sums((length(b + lane) + TS - 1) / TS), 63);
     const uint32_t for_all = (s.shares - s.batch) * CHUNK_WAVES, each = uniform(max(1u, (all + for_all - 1) / for_all) * CHUNK_WAVES);      // tiles
     uint32_t before = 0;
     for (uint32_t b0 = 0; b0 < s.batch; b0 += 64) {
-        if (b0) own = tiles_of(b0 + lane);
-        const uint32_t n = (own + each - 1) / each, up = before + wave_sums(n);
+        if (b0) own = length(b0 + lane);
+        const uint32_t n = ((own + TS - 1) / TS + each - 1) / each, up = before + wave_sums(n);
         if (table && b0 + lane < s.batch) table[b0 + lane] = make_uint2(up - n, n);
         const int at = __popcll(ballot(up <= turn));      // sequences whose chunks all come before
         if (!r.any && at < 64) {
             r.any = true;
             r.b = b0 + at;
-            r.len = uniform(clamp_len(s.lens, r.b, s.slots));
+            r.len = (int)read_lane(own, at);
             r.first = uniform((int)((turn - (read_lane(up, at) - read_lane(n, at))) * each * TS));
             r.slots = (int)(each * TS);
             if (!table) break;
@@ -239,8 +239,7 @@ __global__ __launch_bounds__(NW * 64, NR == 2 ? 3 : 4) void k_step_packed(StepSh
     __shared__ float2 sums[NW][R];
     __shared__ float l2[R], totals[R];      // of a row: logarithm to base 2 of the whole sum, the sum on the maximum
     const uint32_t group = s.group, parts = (group + R - 1) / R;      // rows of queries of a key head
-    const uint32_t of_head = WHOLE ? blockIdx.x : blockIdx.x / s.shares, turn = WHOLE ? blockIdx.y : blockIdx.x - of_head * s.shares;
-    const uint32_t kvh = parts == 1 ? of_head : of_head / parts, part = of_head - kvh * parts;
+    const uint32_t turn = WHOLE ? blockIdx.y : blockIdx.x, kvh = WHOLE ? blockIdx.x : blockIdx.y, part = blockIdx.z;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     const int n_rows = min(R, (int)(group - part * R)), first = (int)(kvh * group + part * R);      // of this workgroup, first of all of the sequence
     uint32_t b = turn;
@@ -248,13 +247,13 @@ __global__ __launch_bounds__(NW * 64, NR == 2 ? 3 : 4) void k_step_packed(StepSh
     if constexpr (WHOLE) {
         c1 = len = clamp_len(s.lens, b, s.slots);
     } else {
-        const Share mine = share_of(s, turn, blockIdx.x == 0 && wave == 0 ? w.table : nullptr, lane);
+        const Share mine = share_of(s, turn, turn + kvh + part + wave == 0 ? w.table : nullptr, lane);
         if (!mine.any) return;
         b = mine.b, len = mine.len, c0 = mine.first, c1 = min(c0 + mine.slots, len);
     }
     const int tokens = clamp_len(s.q_lens, b, s.tokens);
     const int64_t row0 = (int64_t)b * s.q_heads * s.tokens + first;      // of lse
-    const int64_t partial = (int64_t)blockIdx.x * R;                     // of outs and sums: [key head and part][share][row]
+    const int64_t partial = ((int64_t)(kvh * parts + part) * s.shares + turn) * R;      // of outs and sums: [key head][part][share][row]
 
     const int all_see = tokens == (int)s.tokens ? len - (int)(s.tokens - 1) : 0;      // slots below this one: every row
     // Queries as operands, a wave's share of them for all waves: in registers they would cost a fifth of the waves that fit.
@@ -489,12 +488,12 @@ __global__ __launch_bounds__(NW * 64, NR == 2 ? 3 : 4) void k_step_packed(StepSh
 template <class T, int BITS, int DP, int NR> hipError_t launch(const StepShape &s, const StepWork &w, hipStream_t st)
 {
     if (s.whole) {
-        const dim3 grid(s.kv_heads, s.batch, 1);
+        const dim3 grid(s.kv_heads, s.batch);      // the heads of a sequence to all dies (the other way 64 us in place of 50)
         if (s.score_row) k_step_packed<T, BITS, DP, NR, WHOLE_WAVES, Form::WHOLE><<<grid, WHOLE_WAVES * 64, 0, st>>>(s, w);
         else k_step_packed<T, BITS, DP, NR, WHOLE_WAVES, Form::WHOLE_IN_LDS><<<grid, WHOLE_WAVES * 64, 0, st>>>(s, w);
         return hipGetLastError();
     }
-    k_step_packed<T, BITS, DP, NR, CHUNK_WAVES, Form::CHUNK><<<s.kv_heads * step_parts(s.group) * s.shares, CHUNK_WAVES * 64, 0, st>>>(s, w);
+    k_step_packed<T, BITS, DP, NR, CHUNK_WAVES, Form::CHUNK><<<dim3(s.shares, s.kv_heads, step_parts(s.group)), CHUNK_WAVES * 64, 0, st>>>(s, w);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? launch_packed_join(s, w, st) : e;
 }
@@ -542,7 +541,8 @@ void packed_step_split(StepShape &s)
         } else {
             const uint64_t each = (tiles + n - 1) / n;
             s.chunk = (uint32_t)((each < CHUNK_WAVES ? CHUNK_WAVES : each) * TS);
-            s.shares = (uint32_t)((s.slots + s.chunk - 1) / s.chunk * s.batch);
+            s.splits = (uint32_t)((s.slots + s.chunk - 1) / s.chunk);
+            s.shares = s.splits * s.batch;
         }
         return;
     }
