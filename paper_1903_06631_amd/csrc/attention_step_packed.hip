@@ -198,8 +198,6 @@ __device__ __forceinline__ Share share_of(const StepShape &s, uint32_t turn, uin
     Share r = {};
     if (!s.lens) {
         const uint32_t n = s.splits;
-        if (table)
-            for (uint32_t b = lane; b < s.batch; b += 64) table[b] = make_uint2(b * n, n);
         r.any = true;
         r.b = turn / n, r.len = (int)s.slots;
         r.first = (int)((turn - r.b * n) * s.chunk), r.slots = (int)s.chunk;
@@ -512,7 +510,7 @@ template <class T> hipError_t launch(const StepShape &s, const StepWork &w, uint
 static bool whole_caches(uint64_t rows, uint32_t slots)
 {
     const uint64_t rounds = (rows + 255) / 256;
-    return slots <= 512 || (slots <= 1536 && slots <= 8 * rows) || (slots <= 8192 && 8 * rows >= 7 * 256 * rounds);
+    return slots <= 1024 || (slots <= 1536 && slots <= 8 * rows) || (slots <= 8192 && 8 * rows >= 7 * 256 * rounds);
 }
 
 constexpr uint64_t FEW = 512, PLACES = 1024, PLACES_32 = 768;

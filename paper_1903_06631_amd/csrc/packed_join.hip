@@ -30,6 +30,9 @@ __device__ __forceinline__ float2 join_chunks(const float2 *sums, uint32_t n, ui
     return a;
 }
 
+// a sequence's first chunk, how many it has
+__device__ __forceinline__ uint2 chunks_of(const StepShape &s, const StepWork &w, uint32_t b) { return s.lens ? w.table[b] : make_uint2(b * s.splits, s.splits); }
+
 // Workgroups below row_groups join the outputs of JOIN_WAVES / waves rows each, `waves` waves for one; the others add the
 // weights of `each` slots, four to a thread, the rows of the key head shared out where that leaves threads over.
 template <class T, int DP>
@@ -47,7 +50,7 @@ __global__ __launch_bounds__(JOIN) void k_packed_join(StepShape s, StepWork w, u
         const uint32_t b = row / of_one, of = row - b * of_one;
         if (row < rows) {
             const uint32_t kvh = of / s.group, r = of - kvh * s.group, parts = step_parts(s.group), of_part = step_part(s.group);
-            const uint2 chunks = w.table[b];
+            const uint2 chunks = chunks_of(s, w, b);
             const int64_t at = ((int64_t)(kvh * parts + r / of_part) * s.shares + chunks.x) * of_part + r % of_part;
             const float2 *sums = w.sums + at;
             const f32xE *outs = (const f32xE *)(w.outs + at * DP) + lane;
@@ -98,7 +101,7 @@ __global__ __launch_bounds__(JOIN) void k_packed_join(StepShape s, StepWork w, u
         for (int j = 0; j < AHEAD; ++j)
             if (share + j * of < group) x[j] = *(const f32x4 *)(from + (share + j * of) * SCORE_TILE);
     const uint32_t lanes = group <= 4 ? 64 : group <= 8 ? 32 : group <= 16 ? 16 : 8, at_once = JOIN / lanes;      // lanes of a row
-    const uint2 chunks = w.table[b];
+    const uint2 chunks = chunks_of(s, w, b);
     const int64_t of_head = (int64_t)(item - b * s.kv_heads) * step_parts(group);
     for (uint32_t r = threadIdx.x / lanes; r < (group + at_once - 1) / at_once * at_once; r += at_once) {
         const uint32_t l = lane % lanes, row = min(r, group - 1);

@@ -118,6 +118,57 @@ def test_forms(lap, b, kv, n, group, d, bits, kind):
     assert torch.allclose(got["out"].float(), plain["out"].float(), rtol=2 ** -6, atol=2 ** -6)
 
 
+@pytest.mark.parametrize("b,lens", [
+    (3, "none"), (3, "equal"), (3, "empty"), (5, "one long"), (65, "mixed"), (130, "mixed"), (130, "one long"), (64, "short"), (200, "empty")])
+@pytest.mark.parametrize("heads,kv,tokens,d,bits,kind", [(8, 2, 1, 64, 4, BF), (2, 1, 3, 128, 8, HF), (40, 1, 1, 48, 4, HF)])
+def test_chunks_of_sequences(lap, heads, kv, tokens, d, bits, kind, b, lens):
+    """Caches in chunks, shared out on the GPU by the lengths: more sequences than a wave has lanes, none with slots, all of the slots in
+    one; against the call on rows of 16 bits, and 64 bits for the longest one.  Equal calls give equal bits."""
+    n = 1700
+    gen = torch.Generator().manual_seed(b)
+    of = {"none": None, "equal": [n] * b, "empty": [0] * b, "short": [1 + i % 40 for i in range(b)],
+          "one long": [n if i == b // 2 else 0 for i in range(b)],
+          "mixed": [[0, -5, 31, n + 100, 700, 1, n - 1, 33][i % 8] for i in range(b)]}[lens]
+    k, v, _, _ = make(lap, gen, b, kv, n, d, kind, bits, of, numbers=0)
+    q = rows(gen, b, heads, tokens, d, kind, times=1.5)
+    w = torch.rand(b, kv, n, device="cuda")
+    q1 = q if tokens > 1 else q[:, :, 0]
+    got = lap.attention_step_packed(q1, k, v, w, lens=lens_tensor(of))
+    again = lap.attention_step_packed(q1, k, v, w, lens=lens_tensor(of))
+    assert all(torch.equal(got[x], again[x]) for x in got)
+    full = lap.cache_unpack(k, v, kind, d, lens=lens_tensor(of))
+    plain = lap.attention(q, full["k"], full["v"], causal=True, k_lens=lens_tensor(of))
+    added = lap.attention_weights(q, full["k"], plain["lse"], before=w, causal=True, k_lens=lens_tensor(of))["weights"]
+    lse, out = got["lse"].view(plain["lse"].shape), got["out"].view(q.shape)
+    assert torch.equal(lse.isneginf(), plain["lse"].isneginf())
+    assert torch.allclose(lse, plain["lse"], rtol=1e-5, atol=1e-4)
+    assert torch.allclose(out.float(), plain["out"].float(), rtol=2 ** -6, atol=2 ** -6)
+    assert torch.allclose(got["weights"], added, rtol=1e-4, atol=1e-4)
+    i = 0 if of is None else max(range(b), key=lambda j: min(of[j], n))
+    want = ref.Case(q[i:i + 1], full["k"][i:i + 1], full["v"][i:i + 1], causal=True, k_lens=None if of is None else [of[i]])
+    check({name: x[i:i + 1] for name, x in got.items()}, want, w[i:i + 1], (1, heads, tokens, d))
+
+
+def test_lengths_that_grow_between_replays(lap):
+    """A captured step reads its lengths when it is replayed."""
+    gen = torch.Generator().manual_seed(7)
+    b, n = 6, 3000
+    k, v, _, _ = make(lap, gen, b, 2, n, 128, BF, 4, numbers=0)
+    q, w, lens = rows(gen, b, 8, 1, 128, BF)[:, :, 0].contiguous(), torch.zeros(b, 2, n, device="cuda"), i32([1] * b)
+    out = dict(out=torch.empty_like(q), lse=torch.empty(b, 8, device="cuda"), weights=torch.empty_like(w))
+    ws = torch.empty(lap.attention_workspace_bytes(lap.AT_STEP_PACKED, q.shape, (b, 2, n, 128), BF), dtype=torch.uint8, device="cuda")
+    lap.attention_step_packed(q, k, v, w, lens=lens, out=out, ws=ws)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lap.attention_step_packed(q, k, v, w, lens=lens, out=out, ws=ws, sync=False)
+    for turn in ([1, 2, 3, 4, 5, 6], [0, 3000, 0, 17, 2999, 1000], [3000] * 6, [0] * 6, [5, 0, 0, 0, 0, 2500]):
+        lens.copy_(i32(turn))
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = lap.attention_step_packed(q, k, v, w, lens=lens)
+        assert all(torch.equal(out[x], eager[x]) for x in out), turn
+
+
 @pytest.mark.parametrize("kind,bits,d,group,n", [(BF, 4, 64, 4, 700), (HF, 8, 128, 1, 90), (HF, 4, 128, 32, 2047), (BF, 8, 96, 9, 5001)])
 def test_positions(lap, kind, bits, d, group, n):
     """Empty slots by their positions, all of a head's among them; what they hold is not a number."""
