@@ -5,7 +5,8 @@ probabilities are kept for the backward pass and once as it is here.  Both are p
 run, forward and backward, with every tensor at its planned offset in one pool.
 
 Serving: a prompt's keys and values go into a cache of a fixed number of slots, those that have received the most attention;
-then one token after the other is inserted, in place of the slot of the least weight, and attended.
+then one token after the other is inserted, in place of the slot of the least weight, and attended.  And into a cache of few
+bits: prompts of many lengths packed, then a few tokens at a time behind each.
 
     python examples/attention_within_a_limit.py
 """
@@ -136,6 +137,33 @@ def serve(batch=2, heads=8, kv_heads=2, prompt=1500, slots=256, recent=64, new=4
     return step["out"], full["out"], cache, k.shape[2]
 
 
+def serve_packed(bits=4, lengths=(1500, 40, 700), heads=8, kv_heads=2, slots=1600, new=(1, 1, 3, 1), size=128):
+    """One layer of a ragged batch of prompts and of tokens in a packed cache; returns the last tokens' output from it, from the
+    numbers that its rows stand for and from the numbers that were packed, and the bytes of the cache and of one in 16 bits."""
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    batch = len(lengths)
+    rows = lambda h, n: torch.randn(batch, h, n, size, generator=gen, device="cuda").bfloat16()
+    lens = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    k, v = rows(kv_heads, max(lengths)), rows(kv_heads, max(lengths))
+    cache = lap.cache_pack(k, v, bits, slots=slots, lens=lens, sync=False)
+    plain = [torch.zeros(batch, kv_heads, slots, size, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    for full, x in zip(plain, (k, v)):
+        full[:, :, :x.shape[2]] = x
+    for tokens in new:
+        k, v = rows(kv_heads, tokens), rows(kv_heads, tokens)
+        lap.cache_pack(k, v, first=lens, out=cache, sync=False)
+        at = (lens.long()[:, None] + torch.arange(tokens, device="cuda"))[:, None, :, None].expand(-1, kv_heads, -1, size)
+        for full, x in zip(plain, (k, v)):
+            full.scatter_(2, at, x)
+        lens += tokens
+        q = rows(heads, tokens)
+        out = lap.attention_step_packed(q, cache["k"], cache["v"], lens=lens, sync=False)["out"]
+    held = lap.cache_unpack(cache["k"], cache["v"], q.dtype, size, lens=lens, sync=False)
+    from_held = lap.attention(q, held["k"], held["v"], causal=True, k_lens=lens, sync=False)["out"]
+    from_all = lap.attention(q, *plain, causal=True, k_lens=lens)["out"]
+    return out, from_held, from_all, 2 * cache["k"].numel(), 4 * plain[0].numel()
+
+
 def main():
     grads, alone, plans = train()
     same = all(torch.equal(a[n], b[n]) for a, b in zip(grads, alone) for n in a)
@@ -145,6 +173,10 @@ def main():
     out, full, cache, tokens = serve()
     err = float((out.float() - full.float()).norm() / full.float().norm())
     print(f"serving: {cache['k'].shape[2]} slots in place of {tokens}; the last token's output differs from full attention's by {err:.2f} of its norm")
+    for bits in (4, 8):
+        out, _, full, packed, plain = serve_packed(bits)
+        err = float((out.float() - full.float()).norm() / full.float().norm())
+        print(f"serving: {mib(packed)} in {bits} bits in place of {mib(plain)}; the last tokens' outputs differ from those of all 16 bits by {err:.3f} of their norm")
 
 
 if __name__ == "__main__":

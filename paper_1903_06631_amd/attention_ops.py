@@ -358,15 +358,6 @@ def packed_row_bytes(bits: int, head_dim: int) -> int:
 _CACHE, _OUT = ("k_cache", "v_cache"), ("out k_cache", "out v_cache")
 
 
-def _empty(shape, dtype, device):
-    """A contiguous tensor, in three quarters of the time that torch.empty takes."""
-    strides, n = [], 1
-    for x in reversed(shape):
-        strides.insert(0, n)
-        n *= x or 1
-    return torch.empty_strided(shape, strides, dtype=dtype, device=device)
-
-
 def _packed(kind: int, d: int, k, v, index: int, names=_CACHE):
     """lap_packed_cache of rows of bytes that stand for d elements each, the shape of the rows."""
     b, h, n, row = shape = _four(k, names[0])
@@ -420,11 +411,12 @@ def cache_unpack(k_cache, v_cache, dtype, head_dim: int, *, lens=None, first=Non
     index = k_cache.get_device()
     if index < 0:
         _refuse("k_cache", k_cache, "a tensor on the GPU")
-    cache, (b, h, m, _) = _packed(kind, _count(head_dim, "head_dim"), k_cache, v_cache, index)
+    d = _count(head_dim, "head_dim")
+    cache, (b, h, m, _) = _packed(kind, d, k_cache, v_cache, index)
     n = m if length is None else _count(length, "length")
-    shape = (b, h, n, head_dim)
+    shape = (b, h, n, d)
     if out is None:
-        k = _empty(shape, dtype, k_cache.device)
+        k = k_cache.new_empty(shape, dtype=dtype)
         out = dict(k=k, v=torch.empty_like(k))
     rc = _on(index, lib.lap_cache_unpack, cache, n, _plain(lens, "lens", torch.int32, (b,), index), _plain(first, "first", torch.int32, (b,), index),
              _rows(out["k"], "out k", dtype, shape, index), _rows(out["v"], "out v", dtype, shape, index), _stream(index))
@@ -455,9 +447,8 @@ def attention_step_packed(q, k_cache, v_cache, weights=None, *, lens=None, posit
     slots, lse = (b, kv, n), (b, h) if tokens is None else (b, h, tokens)
     if out is None:
         # weights that are not as they have to be are refused below
-        out = dict(out=torch.empty_like(q), lse=_empty(lse, torch.float32, q.device), weights=None if weights is None else torch.empty_like(weights))
-    need = lib.lap_attention_workspace_bytes(AT_STEP_PACKED, s)
-    ws, have, at = _workspace(_empty((need,), torch.uint8, q.device) if ws is None and need else ws, need, index, q)
+        out = dict(out=torch.empty_like(q), lse=q.new_empty(lse, dtype=torch.float32), weights=None if weights is None else torch.empty_like(weights))
+    ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_STEP_PACKED, s), index, q)
     rc = _on(index, lib.lap_attention_step_packed, s, _rows(q, "q", t, qs, index), cache, _plain(positions, "positions", torch.int32, slots, index),
              _plain(weights, "weights", torch.float32, slots, index), _rows(out["out"], "out", t, qs, index),
              _plain(out["lse"], "lse", torch.float32, lse, index), _plain(out.get("weights"), "out weights", torch.float32, slots, index),
