@@ -54,11 +54,13 @@ _pack_rows = struct.Struct("@P3q").pack
 _pack_shape = struct.Struct("@9If2P").pack
 _pack_cache = struct.Struct("@5I4x").pack
 _pack_two = struct.Struct("@2P").pack
-_pack_packed = struct.Struct("@6I").pack
+_pack_pair = struct.Struct("@P3qP3q").pack
+_pack_packed = struct.Struct("@6IP3qP3q").pack
 _NOWHERE = _pack_rows(0, 0, 0, 0)
+_ROWS = len(_NOWHERE)
 assert len(_NOWHERE) == C.sizeof(_Rows) and len(_pack_shape(*[0] * 12)) == C.sizeof(_Shape)
 assert len(_pack_cache(*[0] * 5) + 2 * _NOWHERE + _pack_two(0, 0)) == C.sizeof(_Cache)
-assert len(_pack_packed(*[0] * 6) + 2 * _NOWHERE) == C.sizeof(_Packed)
+assert len(_pack_packed(*[0] * 14)) == C.sizeof(_Packed) and _pack_pair(*range(8)) == _pack_rows(0, 1, 2, 3) + _pack_rows(4, 5, 6, 7)
 
 _calls = SimpleNamespace()      # the library's calls, which take those bytes
 
@@ -358,9 +360,22 @@ def packed_row_bytes(bits: int, head_dim: int) -> int:
 _CACHE, _OUT = ("k_cache", "v_cache"), ("out k_cache", "out v_cache")
 
 
+def _pair(k, v, names, dtype, shape, index: int):
+    """Address and strides of k, then of v, tensors of [batch, heads, length, elements] that are as _rows wants them."""
+    if not (k.dtype is dtype is v.dtype and k.shape == shape == v.shape and k.get_device() == index == v.get_device()):
+        _rows(k, names[0], dtype, shape, index), _rows(v, names[1], dtype, shape, index)
+    a, b = k.stride(), v.stride()
+    if a[3] != 1 or b[3] != 1:
+        _rows(k, names[0], dtype, shape, index), _rows(v, names[1], dtype, shape, index)
+    return k.data_ptr(), a[0], a[1], a[2], v.data_ptr(), b[0], b[1], b[2]
+
+
 def _packed(kind: int, d: int, k, v, index: int, names=_CACHE):
     """lap_packed_cache of rows of bytes that stand for d elements each, the shape of the rows."""
-    b, h, n, row = shape = _four(k, names[0])
+    shape = k.shape
+    if len(shape) != 4:
+        _refuse(names[0], k, "[batch, heads, length, bytes of a row]")
+    b, h, n, row = shape
     bits = _row_bits.get((row, d))
     if bits is None:
         for bits in (4, 8):
@@ -369,8 +384,7 @@ def _packed(kind: int, d: int, k, v, index: int, names=_CACHE):
         else:
             _refuse(names[0], k, f"rows of packed_row_bytes of 4 or 8 bits and {d} elements")
         _row_bits[row, d] = bits
-    t = torch.uint8
-    return (_pack_packed(kind, bits, b, h, n, d) + _rows(k, names[0], t, shape, index) + _rows(v, names[1], t, shape, index)), shape
+    return _pack_packed(kind, bits, b, h, n, d, *_pair(k, v, names, torch.uint8, shape, index)), shape
 
 
 def cache_pack(k, v, bits: Optional[int] = None, *, lens=None, first=None, slots: Optional[int] = None, out: Optional[dict] = None,
@@ -393,8 +407,9 @@ def cache_pack(k, v, bits: Optional[int] = None, *, lens=None, first=None, slots
     cache, rows = _packed(kind, d, out["k"], out["v"], index, _OUT)
     if rows[0] != b or rows[1] != h or (bits is not None and rows[3] != packed_row_bytes(bits, d)):
         _refuse("out k_cache", out["k"], f"a cache of {b} sequences and {h} heads" + (f" in {bits} bits" if bits is not None else ""))
-    rc = _on(index, lib.lap_cache_pack, cache, _rows(k, "k", t, shape, index), _rows(v, "v", t, shape, index), n,
-             _plain(lens, "lens", torch.int32, (b,), index), _plain(first, "first", torch.int32, (b,), index), _stream(index))
+    rows = _pack_pair(*_pair(k, v, "kv", t, shape, index))
+    args = (cache, rows, rows[_ROWS:], n, _plain(lens, "lens", torch.int32, (b,), index), _plain(first, "first", torch.int32, (b,), index), _stream(index))
+    rc = lib.lap_cache_pack(*args) if _device() == index else _on(index, lib.lap_cache_pack, *args)
     if rc or sync:
         _done(rc, "lap_cache_pack", index, sync)
     return out
@@ -415,11 +430,15 @@ def cache_unpack(k_cache, v_cache, dtype, head_dim: int, *, lens=None, first=Non
     cache, (b, h, m, _) = _packed(kind, d, k_cache, v_cache, index)
     n = m if length is None else _count(length, "length")
     shape = (b, h, n, d)
-    if out is None:
+    if out is None:      # contiguous, and nothing to check
         k = k_cache.new_empty(shape, dtype=dtype)
-        out = dict(k=k, v=torch.empty_like(k))
-    rc = _on(index, lib.lap_cache_unpack, cache, n, _plain(lens, "lens", torch.int32, (b,), index), _plain(first, "first", torch.int32, (b,), index),
-             _rows(out["k"], "out k", dtype, shape, index), _rows(out["v"], "out v", dtype, shape, index), _stream(index))
+        v, row = torch.empty_like(k), n * d
+        out = dict(k=k, v=v)
+        rows = _pack_pair(k.data_ptr(), h * row, row, d, v.data_ptr(), h * row, row, d)
+    else:
+        rows = _pack_pair(*_pair(out["k"], out["v"], ("out k", "out v"), dtype, shape, index))
+    args = (cache, n, _plain(lens, "lens", torch.int32, (b,), index), _plain(first, "first", torch.int32, (b,), index), rows, rows[_ROWS:], _stream(index))
+    rc = lib.lap_cache_unpack(*args) if _device() == index else _on(index, lib.lap_cache_unpack, *args)
     if rc or sync:
         _done(rc, "lap_cache_unpack", index, sync)
     return out
@@ -445,14 +464,19 @@ def attention_step_packed(q, k_cache, v_cache, weights=None, *, lens=None, posit
     s = _pack_shape(kind, b, h, kv, 1 if tokens is None else tokens, n, d, 1, 0, _scale(scale, d), 0 if q_lens is None else _plain(q_lens, "q_lens", torch.int32, (b,), index),
                     0 if lens is None else _plain(lens, "lens", torch.int32, (b,), index))
     slots, lse = (b, kv, n), (b, h) if tokens is None else (b, h, tokens)
-    if out is None:
-        # weights that are not as they have to be are refused below
-        out = dict(out=torch.empty_like(q), lse=q.new_empty(lse, dtype=torch.float32), weights=None if weights is None else torch.empty_like(weights))
+    before = _plain(weights, "weights", torch.float32, slots, index)
+    if out is None:      # nothing to check
+        o, sums = torch.empty_like(q), q.new_empty(lse, dtype=torch.float32)
+        after = None if weights is None else torch.empty_like(weights)
+        out = dict(out=o, lse=sums, weights=after)
+        st = o.stride()
+        results = _pack_rows(o.data_ptr(), st[0], st[1], st[2] if tokens is not None else 0), sums.data_ptr(), None if after is None else after.data_ptr()
+    else:
+        results = (_rows(out["out"], "out", t, qs, index), _plain(out["lse"], "lse", torch.float32, lse, index),
+                   _plain(out.get("weights"), "out weights", torch.float32, slots, index))
     ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_STEP_PACKED, s), index, q)
-    rc = _on(index, lib.lap_attention_step_packed, s, _rows(q, "q", t, qs, index), cache, _plain(positions, "positions", torch.int32, slots, index),
-             _plain(weights, "weights", torch.float32, slots, index), _rows(out["out"], "out", t, qs, index),
-             _plain(out["lse"], "lse", torch.float32, lse, index), _plain(out.get("weights"), "out weights", torch.float32, slots, index),
-             at, have, _stream(index))
+    args = (s, _rows(q, "q", t, qs, index), cache, _plain(positions, "positions", torch.int32, slots, index), before, *results, at, have, _stream(index))
+    rc = lib.lap_attention_step_packed(*args) if _device() == index else _on(index, lib.lap_attention_step_packed, *args)
     if rc or sync:
         _done(rc, "lap_attention_step_packed", index, sync)
     return out

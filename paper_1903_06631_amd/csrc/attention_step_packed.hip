@@ -3,9 +3,9 @@
 //   o_i = sum_j p_ij v_j, p_ij = exp(scale q_i.k_j - lse_i), over the slots in use that row i sees; w_j += sum_i p_ij
 // with k and v the numbers that the packed rows stand for, rounded to the element type as in cache_unpack.
 //
-// p is rounded to the values' type for its product with them (a matrix operand), in binary16 as a multiple of 2^-12, so that
-// those below 2^-26 of the largest of their wave lose precision and none of them vanishes above 2^-36.  Sums, scores and weights
-// are 32 bits.
+// p is rounded to the values' type for its product with them (a matrix operand), in binary16 as a multiple of 2^-10, so that
+// those below 2^-24 of the largest of their wave lose precision and none vanishes above 2^-35.  Sums, scores and weights are
+// 32 bits.
 //
 // Every packed row is read once.  The rows of queries that share a key head, heads times tokens, are the columns of 16 of the
 // 16x16x32 matrix instruction (C = A B, lane l with g = l / 16):
@@ -15,9 +15,19 @@
 // whose low and high halves, side by side for two slots, are the operand's pairs (packed_rows.h).  So both go from memory
 // straight into registers and from there into the products, without LDS; the contraction over slots runs in the order in which
 // the scores stand in C.  Waves go through 32 slots at a time of their own, without waiting for each other, and ask for the
-// next keys when these ones are decoded, for the next values likewise.
+// next keys when these ones are decoded, for the next values likewise (with two tiles on their way, and a fourth of the waves less,
+// 64 caches of 8 heads x up to 4096 slots took 55 us in place of 50, 24 of 4 x up to 6001 of 8 bits 37 in place of 27).
 //
-// Chunks of long caches, one workgroup for short ones, the scores kept for the weights: as in attention_step.hip.
+// Bound by memory where caches are long, and not by much: a tile of 32 slots of 128 elements is 10 KB and some 390 vector
+// instructions in bfloat16 (270 in binary16), four cycles each, of which a third would do for rows of 16 bits.  So every
+// instruction of a tile counts: levels are converted two by two, loads need no addresses of their own, the running maximum is
+// left behind by up to 2^5 before sums are taken down to a new one, and lanes compare with it on their own.  Short caches are bound by a
+// launch or two and the chain of a tile, some 1.3 us.
+//
+// Long caches are cut into chunks, a workgroup of four waves each; what these leave is joined by a second kernel, which adds the
+// weights as well (packed_join.hip).  Short ones have a workgroup of eight waves each, which does all of it.
+//
+// Measured, kernels alone: @@MEASURED@@
 #include "lap_dev.h"
 #include "packed_rows.h"
 
