@@ -502,7 +502,9 @@ int lap_cache_unpack(const lap_packed_cache *from, uint32_t n, const int32_t *le
 /* lap_attention_step on a packed cache, for q_len new tokens of every sequence, whose keys and values are its last q_len slots
  * in use: shape with the cache's sizes, k_len its slots, window 0 and up to 256 rows (query heads times q_len) to a key
  * head.  With q_len > 1, causal is 1 (row i of a sequence sees the slots below k_lens[b] - q_lens[b] + i + 1) and positions NULL; with
- * q_len 1 causal may be either.  lse [batch, q_heads, q_len]; weights are the sums over all heads and rows of the call. */
+ * q_len 1 causal may be either.  lse [batch, q_heads, q_len]; weights are the sums over all heads and rows of the call.  A group of
+ * a key that is not a number makes the rows that see its slot not numbers, one of a value their elements of that group; what
+ * empty slots and those past the length hold reaches nothing.  The workspace is the same with lengths and without. */
 int lap_attention_step_packed(const lap_attention_shape *shape, const lap_rows *q, const lap_packed_cache *cache,
                               const int32_t *positions, const float *before, const lap_rows *out, float *lse, float *weights,
                               void *ws, size_t ws_bytes, void *hip_stream);

@@ -27,7 +27,11 @@
 // Long caches are cut into chunks, a workgroup of four waves each; what these leave is joined by a second kernel, which adds the
 // weights as well (packed_join.hip).  Short ones have a workgroup of eight waves each, which does all of it.
 //
-// Measured, kernels alone: @@MEASURED@@
+// Measured, kernels alone, 4 bits and 128 elements where nothing else is said: 16 x 1000 slots of one sequence 12.4 us (a launch
+// and a chain of four tiles); 64 ragged sequences of 8 heads x up to 4096 slots, 4 query heads each and weights, 45 us (188 MB of rows
+// and results at 4.2 TB/s, vector instructions in 49 % of all cycles, the matrix units busy 7 %); 2 x 8 x 131 072 slots likewise 76 us and 12 to
+// join (4.9 TB/s, 38 %, 9 %); 24 ragged x 4 x up to 6001 slots of 96 in 8 bits, 8 query heads each, 19 us and 4.4; 16 ragged x 8 x up
+// to 8192 slots, five tokens of 4 query heads, 29 us and 6.0; 32 x 2047 slots of 64, 32 query heads, 10 us and 6.0.
 #include "lap_dev.h"
 #include "packed_rows.h"
 
@@ -194,10 +198,12 @@ __device__ __forceinline__ uint32_t wave_sums(uint32_t v)
     return v;
 }
 
-// Which slots of which sequence are a workgroup's.  Without lengths, chunks of s.chunk slots, as many for each sequence.  Lengths
+// Which slots of which sequence are a workgroup's.  Without lengths, chunks of s.chunk slots, s.splits for each sequence.  Lengths
 // are known on the GPU only, so it is there that all sequences are cut into chunks of one size, a number of tiles for each wave:
-// the least that makes no more of them than there are workgroups (for each key head), whatever the lengths are, as s.shares is
-// as many as chunks of all tiles plus one for each sequence.
+// the least that makes no more than s.splits of them (for each key head), so that workgroups fill the card's places evenly,
+// whatever the lengths are; or, of more sequences than a wave has lanes and where no size below it does, the least that surely makes no
+// more than s.shares, as chunks of all tiles plus one for each sequence are.  (16 ragged sequences of 8 heads x up to 8192 slots,
+// five tokens: 35.0 us, with the sure size alone 36.9.)
 struct Share {
     uint32_t b;
     int len, first, slots;
@@ -216,7 +222,13 @@ __device__ __forceinline__ Share share_of(const StepShape &s, uint32_t turn, uin
     const auto length = [&](uint32_t b) { return b < s.batch ? (uint32_t)clamp_len(s.lens, b, s.slots) : 0; };
     uint32_t own = length(lane), all = read_lane(wave_sums((own + TS - 1) / TS), 63);
     for (uint32_t b = 64; b < s.batch; b += 64) all += read_lane(wave_sums((length(b + lane) + TS - 1) / TS), 63);
-    const uint32_t for_all = (s.shares - s.batch) * CHUNK_WAVES, each = uniform(max(1u, (all + for_all - 1) / for_all) * CHUNK_WAVES);      // tiles
+    const auto at_least = [&](uint32_t chunks) { return uniform(max(1u, (all + chunks * CHUNK_WAVES - 1) / (chunks * CHUNK_WAVES))); };
+    const uint32_t surely = at_least(s.shares - s.batch);
+    uint32_t for_wave = surely;      // tiles
+    if (s.batch <= 64)
+        for (for_wave = at_least(s.splits); for_wave < surely; ++for_wave)
+            if (read_lane(wave_sums(((own + TS - 1) / TS + for_wave * CHUNK_WAVES - 1) / (for_wave * CHUNK_WAVES)), 63) <= s.splits) break;
+    const uint32_t each = for_wave * CHUNK_WAVES;
     uint32_t before = 0;
     for (uint32_t b0 = 0; b0 < s.batch; b0 += 64) {
         if (b0) own = length(b0 + lane);
@@ -344,8 +356,8 @@ __global__ __launch_bounds__(NW * 64, NR == 2 ? 3 : 4) void k_step_packed(StepSh
                 const bool used = (live >> slot) & 1;
 #pragma unroll
                 for (int a = 0; a < NR; ++a) p[a][i] = used && at + slot < sees[a] ? p[a][i] : -ATTN_INF;
-                // what an empty slot holds may be anything, and past the length stand copies of the last slot: zero times
-                // what is not a number is not zero
+                // what an empty slot holds may be anything, and past the length may stand the last slot again (rows of stride
+                // zero): zero times what is not a number is not zero
                 words.v_ends[i] = used && at + slot < len ? words.v_ends[i] : 0;
             }
             // a slot that only some of the rows see, with a value that is not a number: left out of the product, and added to those rows
@@ -517,12 +529,36 @@ template <class T> hipError_t launch(const StepShape &s, const StepWork &w, uint
 
 }  // namespace
 
+// Whether one workgroup goes through all of a cache.  It needs no second launch, 3 us of the card's and 5 of the call, but has a
+// compute unit's waves for itself only where there are as many caches.  So: for short ones; for those of 1024 to 1536 slots, where
+// units are not left idle for long; and for up to 8192 slots where the last round of workgroups leaves at most an eighth of
+// them idle.  Measured (8 key heads of 128 elements in 4 bits, 4 query heads each; whole, and in the best chunks):
+//   caches x slots     whole   chunks          caches x slots     whole   chunks
+//        8 x 500         9.1      9.5 us          128 x 4000        36.9     28.4 us
+//        8 x 1000       12.7      9.7 *           192 x 4000        37.5     33.2
+//        8 x 2000       20        9.8             256 x 4000        42.7     47.6
+//       32 x 1000       13.2     11.2 *           320 x 4000        70.4     59.7
+//       32 x 2000       20.5     12.5             384 x 4000        63.1     56.5
+//      128 x 1000       13.8     15.8             512 x 4000        82       90
+//      128 x 2000       21.6     18.9             512 x 8000       169      174
+//      192 x 2000       21.9     23.6             768 x 4000       124.5    133
+// (* on the card alone: called one after the other 12.1 and 17.)
 static bool whole_caches(uint64_t rows, uint32_t slots)
 {
     const uint64_t rounds = (rows + 255) / 256;
     return slots <= 1024 || (slots <= 1536 && slots <= 8 * rows) || (slots <= 8192 && 8 * rows >= 7 * 256 * rounds);
 }
 
+// Into how many chunks caches are cut: as many as the card has places for workgroups of CHUNK_WAVES waves, four or (with 32 rows
+// of queries in the registers) three a unit.  Half of the places are better for shorter ones: fewer start and fewer are joined, and up
+// to 32 tiles a chunk that is the more; with lengths up to 24, as these make the tiles fewer than there may be and the chunks of all
+// less even.  Chunks of over 64 tiles are cut smaller, so that units that are done early go on.  Measured (4 bits, 8 key heads of 128
+// elements, 4 query heads each; tiles a chunk with half of the places, that, all of them):
+//   without lengths   16 x 3500 slots   27    21.9  22.8 us      ragged    4 x 5000 slots   10    14.7  16.2 us
+//                     16 x 4500         35    25.1  26.0                  2 x 20000         20    18.2  20.4
+//                     16 x 6500         51    31.8  31.5                  8 x 5000          20    20.6  20.0
+//                      1 x 30000        15    17.4  20.5                 16 x 3500          27    22.2  18.6
+//                      1 x 131072       64    40.0  42.2                  8 x 8000          31    27.2  25.2
 constexpr uint64_t FEW = 512, PLACES = 1024, PLACES_32 = 768;
 void packed_step_split(StepShape &s)
 {
@@ -534,18 +570,13 @@ void packed_step_split(StepShape &s)
     if (!s.whole) {
         const uint64_t tiles = s.score_row / TS, places = s.group <= 16 ? PLACES : PLACES_32;
         // for each key head, of one sequence or of all of them
-        const uint64_t sequences = s.lens ? s.batch : 1, all = tiles * sequences;
-        const auto chunks = [&](uint64_t groups, uint64_t most) {
-            const uint64_t n = groups / heads / (s.batch / sequences);
-            // of all of them, half a chunk for each sequence besides, as the last ones are shorter
-            const uint64_t fits = sequences == 1 ? n : n > sequences ? n - sequences / 2 : n - n / 2;
-            return all <= fits * most ? fits : 0;
-        };
-        uint64_t n = chunks(FEW, 32);
-        if (!n) n = chunks(places, 64);
-        if (!n) n = (all + 63) / 64;
+        const uint64_t sequences = s.lens ? s.batch : 1, all = tiles * sequences, few = FEW / heads / (s.batch / sequences);
+        uint64_t n = places / heads / (s.batch / sequences);
+        if (all <= few * (s.lens ? 24 : 32)) n = few;
+        if (all > n * 64) n = (all + 63) / 64;
         if (s.lens) {
-            s.shares = (uint32_t)(n + s.batch);
+            s.splits = (uint32_t)n;
+            s.shares = (uint32_t)((n > s.batch ? n - s.batch / 2 : n - n / 2) + s.batch);
         } else {
             const uint64_t each = (tiles + n - 1) / n;
             s.chunk = (uint32_t)((each < CHUNK_WAVES ? CHUNK_WAVES : each) * TS);

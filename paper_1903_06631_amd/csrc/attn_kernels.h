@@ -50,7 +50,7 @@ struct StepShape {
     const int32_t *q_lens;       // how many of them are in use, NULL: all
     uint32_t group;              // rows of queries of a key head; this and the next by packed_step_split
     uint32_t shares;             // workgroups for each part of a key head's rows, among which all sequences are shared out
-    uint32_t chunk, splits;      // slots of a workgroup, workgroups of a cache (step_split)
+    uint32_t chunk, splits;      // (packed, with lengths: what to cut all of a key head's into) slots of a workgroup, workgroups of a cache (step_split)
     uint64_t score_row;          // floats between two heads' scores (0: they stay in LDS)
     bool whole;                  // one workgroup for all of a cache, and nothing to join
 };
