@@ -405,3 +405,23 @@ def test_a_packed_cache_held_to_a_number_of_slots(lap, bits):
         small["weights"] = got["weights"]
         plain["weights"] = got["weights"].clone()
         position += 1
+
+
+@pytest.mark.parametrize("kind,bits,d,heads,kv,b,n", [(BF, 4, 16, 8, 8, 8191, 5), (HF, 8, 64, 3, 1, 65535, 3), (BF, 4, 64, 1, 1, 20000, 1100)])
+def test_as_many_caches_as_a_call_takes(lap, kind, bits, d, heads, kv, b, n):
+    """Each one's results those of a call for it and a few others."""
+    gen = torch.Generator(device="cuda").manual_seed(b)
+    k, v = (torch.randn(1, kv, n, d, generator=gen, device="cuda").to(kind).expand(b, kv, n, d) for _ in range(2))
+    times = torch.rand(b, 1, 1, 1, generator=gen, device="cuda").to(kind)
+    held = lap.cache_pack(k * times, v * (1 - times), bits)
+    q = torch.randn(b, heads, d, generator=gen, device="cuda").to(kind)
+    lens = torch.randint(0, n + 1, (b,), generator=gen, device="cuda").int()
+    w = torch.rand(b, kv, n, generator=gen, device="cuda")
+    got = lap.attention_step_packed(q, held["k"], held["v"], w, lens=lens)
+    for at in (0, b // 2, b - 7):
+        one = slice(at, at + 7)
+        few = lap.cache_pack((k * times)[one], (v * (1 - times))[one], bits)
+        assert torch.equal(few["k"], held["k"][one]) and torch.equal(few["v"], held["v"][one])
+        kn, vn = (packed_ref.unpack(few[x], kind, d, bits) for x in "kv")
+        want = ref.Case(q[one, :, None], kn, vn, causal=True, k_lens=lens[one].tolist())
+        check({name: x[one] for name, x in got.items()}, want, w[one], (7, heads, 1, d))

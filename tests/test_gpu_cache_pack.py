@@ -226,3 +226,35 @@ def test_refusals(lap):
             call()
         assert e.value.status == -10
     assert torch.equal(c["k"], before) and (x == 1).all()
+
+
+@pytest.mark.parametrize("kind", [BF, HF])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("d", [24, 64, 72, 128])
+@pytest.mark.parametrize("n", [3001, 4099])
+def test_many_rows(lap, n, d, bits, kind):
+    """Several rows to a thread, and past the caches: each row the bytes that it has alone, which are those of the definition."""
+    h = 7 if n < 4000 else 1280 // d
+    gen = torch.Generator().manual_seed(d + bits)
+    hard = groups_of(kind, gen).repeat(1, 4)[:, :d]
+    few = torch.cat([hard, torch.randn(61, d, generator=gen).to(kind)])
+    r = few.shape[0]
+    alone = lap.cache_pack(few.view(1, 1, r, d).cuda(), few.view(1, 1, r, d).cuda(), bits)["k"][0, 0]
+    check_bytes(alone, ref.pack(few, bits), kind, d, bits)
+    numbers = lap.cache_unpack(alone.view(1, 1, r, -1), alone.view(1, 1, r, -1), kind, d)["k"][0, 0]
+    assert same(numbers, ref.unpack(alone, kind, d, bits))
+    b, slots, lens, first = 2, n + 11, [n, n - 1234], [-2, 40]      # some rows past the cache's end and before its start
+    which = [torch.randint(r, (b, h, n), generator=gen).cuda() for _ in range(2)]
+    few = few.cuda()
+    k, v = (few[i] for i in which)
+    out = dict(k=empty_cache(b, h, slots, alone.shape[1]), v=empty_cache(b, h, slots, alone.shape[1]))
+    lap.cache_pack(k, v, lens=i32(lens), first=i32(first), out=out)
+    back = lap.cache_unpack(out["k"], out["v"], kind, d, lens=i32(lens), first=i32(first), length=n)
+    for i, cache, y in zip(which, (out["k"], out["v"]), (back["k"], back["v"])):
+        for s in range(b):
+            low, high = max(0, -first[s]), min(lens[s], slots - first[s])
+            rows_in = i[s, :, low:high]
+            assert torch.equal(cache[s, :, low + first[s]:high + first[s]], alone[rows_in])
+            assert (cache[s, :, :low + first[s]] == 0xA5).all() and (cache[s, :, high + first[s]:] == 0xA5).all()
+            assert torch.equal(y[s, :, low:high].view(torch.int16), numbers[rows_in].view(torch.int16))
+            assert not y[s, :, :low].view(torch.int16).any() and not y[s, :, high:].view(torch.int16).any()
