@@ -532,7 +532,7 @@ template <class T> hipError_t launch(const StepShape &s, const StepWork &w, uint
 // Whether one workgroup goes through all of a cache.  It needs no second launch, 3 us of the card's and 5 of the call, but has a
 // compute unit's waves for itself only where there are as many caches.  So: for short ones; for those of 1024 to 1536 slots, where
 // units are not left idle for long; and for up to 8192 slots where the last round of workgroups leaves at most an eighth of
-// them idle.  Measured (8 key heads of 128 elements in 4 bits, 4 query heads each; whole, and in the best chunks):
+// them idle (up to 2800 with lengths and one round: the longest cache's unit then works alone).  Measured (8 key heads of 128 elements in 4 bits, 4 query heads each; whole, and in the best chunks):
 //   caches x slots     whole   chunks          caches x slots     whole   chunks
 //        8 x 500         9.1      9.5 us          128 x 4000        36.9     28.4 us
 //        8 x 1000       12.7      9.7 *           192 x 4000        37.5     33.2
@@ -543,10 +543,12 @@ template <class T> hipError_t launch(const StepShape &s, const StepWork &w, uint
 //      128 x 2000       21.6     18.9             512 x 8000       169      174
 //      192 x 2000       21.9     23.6             768 x 4000       124.5    133
 // (* on the card alone: called one after the other 12.1 and 17.)
-static bool whole_caches(uint64_t rows, uint32_t slots)
+// Ragged, lengths evenly spread up to these, 256 x 2000 19.5 and 21.0, x 4096 33.6 and 28.7, 240 x 6000 46.6 and 35.5, 512 x 4096 45.8 and 49.0,
+// x 8192 84.4 and 82.7.
+static bool whole_caches(uint64_t rows, uint32_t slots, bool lens)
 {
     const uint64_t rounds = (rows + 255) / 256;
-    return slots <= 1024 || (slots <= 1536 && slots <= 8 * rows) || (slots <= 8192 && 8 * rows >= 7 * 256 * rounds);
+    return slots <= 1024 || (slots <= 1536 && slots <= 8 * rows) || (slots <= (lens && rounds == 1 ? 2800 : 8192) && 8 * rows >= 7 * 256 * rounds);
 }
 
 // Into how many chunks caches are cut: as many as the card has places for workgroups of CHUNK_WAVES waves, four or (with 32 rows
@@ -565,7 +567,7 @@ void packed_step_split(StepShape &s)
     s.group = s.q_heads / s.kv_heads * s.tokens;
     const uint64_t heads = (uint64_t)s.kv_heads * step_parts(s.group), rows = s.batch * heads;
     s.score_row = ((uint64_t)s.slots + TS - 1) / TS * TS;
-    s.whole = s.group <= 32 && whole_caches(rows, s.slots);
+    s.whole = s.group <= 32 && whole_caches(rows, s.slots, s.lens);
     s.chunk = s.splits = s.shares = 0;
     if (!s.whole) {
         const uint64_t tiles = s.score_row / TS, places = s.group <= 16 ? PLACES : PLACES_32;
