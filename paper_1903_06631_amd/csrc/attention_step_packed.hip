@@ -576,13 +576,14 @@ void packed_step_split(StepShape &s)
         uint64_t n = places / heads / (s.batch / sequences);
         if (all <= few * (s.lens ? 24 : 32)) n = few;
         if (all > n * 64) n = (all + 63) / 64;
+        if (!n) n = 1;      // (no slots, and more heads than places)
         if (s.lens) {
             s.splits = (uint32_t)n;
             s.shares = (uint32_t)((n > s.batch ? n - s.batch / 2 : n - n / 2) + s.batch);
         } else {
             const uint64_t each = (tiles + n - 1) / n;
             s.chunk = (uint32_t)((each < CHUNK_WAVES ? CHUNK_WAVES : each) * TS);
-            s.splits = (uint32_t)((s.slots + s.chunk - 1) / s.chunk);
+            s.splits = s.slots ? (uint32_t)((s.slots + s.chunk - 1) / s.chunk) : 1;      // without slots one that finds none
             s.shares = s.splits * s.batch;
         }
         return;

@@ -425,3 +425,14 @@ def test_as_many_caches_as_a_call_takes(lap, kind, bits, d, heads, kv, b, n):
         kn, vn = (packed_ref.unpack(few[x], kind, d, bits) for x in "kv")
         want = ref.Case(q[one, :, None], kn, vn, causal=True, k_lens=lens[one].tolist())
         check({name: x[one] for name, x in got.items()}, want, w[one], (7, heads, 1, d))
+
+
+@pytest.mark.parametrize("b,heads,kv,tokens,d", [(2, 40, 1, 1, 128), (3, 256, 1, 1, 64), (2, 16, 2, 5, 96), (64, 64, 8, 5, 128), (257, 40, 1, 1, 64), (600, 40, 1, 1, 128)])
+@pytest.mark.parametrize("lengths", [False, True])
+def test_without_slots_and_many_rows(lap, b, heads, kv, tokens, d, lengths):
+    """More than 32 rows to a key head, which never have a workgroup for a whole cache: of few key heads and of more than there are places."""
+    c = torch.zeros(b, kv, 0, packed_ref.row_bytes(d, 4), dtype=torch.uint8, device="cuda")
+    q = torch.ones(b, heads, tokens, d, device="cuda").half()
+    lens = i32([i % 3 for i in range(b)]) if lengths else None
+    got = lap.attention_step_packed(q, c, c, torch.zeros(b, kv, 0, device="cuda"), lens=lens)
+    assert (got["out"] == 0).all() and torch.isneginf(got["lse"]).all() and got["weights"].shape == (b, kv, 0)

@@ -110,3 +110,19 @@ def test_binding_refuses_before_the_library():
         with pytest.raises(ValueError):
             call()
     assert lap.packed_row_bytes(4, 128) == 80 and lap.packed_row_bytes(8, 128) == 144
+
+
+@pytest.mark.parametrize("q_shape,kv_shape", [((2, 40, 1, 128), (2, 1, 0, 128)), ((64, 64, 5, 128), (64, 8, 0, 128)), ((257, 40, 1, 128), (257, 1, 0, 128)),
+                                              ((600, 256, 1, 64), (600, 1, 0, 64)), ((1, 65535, 64, 8), (1, 65535, 0, 8))])
+def test_workspace_without_slots(q_shape, kv_shape):
+    """Caches without slots and more than 32 rows to a key head, of few key heads and of more than there are places for workgroups: a
+    workspace like any other's.  (In a process of its own: a division by zero in the library ends it.)"""
+    import os
+    import subprocess
+    import sys
+    code = ("import torch, paper_1903_06631_amd as lap\n"
+            f"print(lap.attention_workspace_bytes(lap.AT_STEP_PACKED, {q_shape}, {kv_shape}, torch.bfloat16))")
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0, f"ended with {r.returncode}: {r.stderr[-500:]}"
+    need = int(r.stdout.split()[-1])
+    assert need > 0 and need % 256 == 0
