@@ -257,7 +257,8 @@ __global__ __launch_bounds__(NW * 64, NR == 2 ? 3 : 4) void k_step_packed(StepSh
     __shared__ __align__(16) float outs[R * PITCH];      // [row][half of the waves][DP]
     __shared__ typename Elem<T>::x8 queries[NR][DP / 32][64];
     __shared__ float2 sums[NW][R];
-    __shared__ float l2[R], totals[R];      // of a row: logarithm to base 2 of the whole sum, the sum on the maximum
+    __shared__ float2 whole[R];      // of a row: its largest product and the logarithm to base 2 of its sum on that
+    __shared__ float totals[R];      // that sum
     const uint32_t group = s.group, parts = (group + R - 1) / R;      // rows of queries of a key head
     const uint32_t turn = WHOLE ? blockIdx.y : blockIdx.x, kvh = WHOLE ? blockIdx.x : blockIdx.y, part = blockIdx.z;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
@@ -318,11 +319,15 @@ __global__ __launch_bounds__(NW * 64, NR == 2 ? 3 : 4) void k_step_packed(StepSh
     const float c = s.scale * LOG2E;
     constexpr float TIMES = IS_F16<T> ? 10.f : 0.f;      // p as a multiple of 2^-TIMES
     const float slack = 5.f / c;                         // by how much the running maximum may be left behind: 2^5
+    // Maxima are those of the products, and differences are taken before the scale comes in: a scaled score may be so large that
+    // 32 bits hold it to whole powers of two only, and its own maximum's exponent has to be 0 all the same.  (With scaled
+    // maxima inside the multiplication, a subtraction less for each score, 16 sequences with five tokens below took 32.9 us in
+    // place of 33.3, two long ones the same.)
 
     f32x4 acc[NR][DP / 16] = {};
-    float m[NR], limit[NR], off[NR], l[NR];      // limit: a product from which on m follows; off: what p's exponent is raised by
+    float m[NR], l[NR];
 #pragma unroll
-    for (int a = 0; a < NR; ++a) m[a] = LOWEST, limit[a] = LOWEST + slack, off[a] = TIMES - LOWEST * c, l[a] = 0.f;
+    for (int a = 0; a < NR; ++a) m[a] = LOWEST, l[a] = 0.f;
     for (; at < c1; at += NW * TS) {
         const int next = at + NW * TS;
         asm volatile("" ::: "memory");      // the queries are not to be kept in registers
@@ -398,16 +403,16 @@ __global__ __launch_bounds__(NW * 64, NR == 2 ? 3 : 4) void k_step_packed(StepSh
             float top = p[a][0];
 #pragma unroll
             for (int i = 1; i < 8; ++i) top = fmaxf(top, p[a][i]);
-            if (__ballot(top > limit[a])) {
+            if (__ballot(top - m[a] > slack)) {
                 const float up = fmaxf(m[a], column_max(top)), by = exp2_fast((m[a] - up) * c);
-                m[a] = up, limit[a] = up + slack, off[a] = TIMES - up * c;
+                m[a] = up;
                 l[a] *= by;
 #pragma unroll
                 for (int j = 0; j < DP / 16; ++j) acc[a][j] *= by;
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                p[a][i] = exp2_fast(__builtin_fmaf(p[a][i], c, off[a]));
+                p[a][i] = exp2_fast(__builtin_fmaf(p[a][i] - m[a], c, TIMES));
                 l[a] += p[a][i];
             }
         }
@@ -425,7 +430,7 @@ __global__ __launch_bounds__(NW * 64, NR == 2 ? 3 : 4) void k_step_packed(StepSh
     constexpr float ONE = IS_F16<T> ? 0x1p-10f : 1.f;
 #pragma unroll
     for (int a = 0; a < NR; ++a) {
-        l[a] = column_sum(l[a]) * ONE, m[a] *= c;
+        l[a] = column_sum(l[a]) * ONE;
         if (g == 0) sums[wave][16 * a + n] = make_float2(m[a], l[a]);
     }
     __syncthreads();
@@ -435,18 +440,18 @@ __global__ __launch_bounds__(NW * 64, NR == 2 ? 3 : 4) void k_step_packed(StepSh
         const int r = 16 * a + n;
         float top = sums[0][r].x;
         for (int i = 1; i < NW; ++i) top = fmaxf(top, sums[i][r].x);
-        const float by = exp2_fast(m[a] - top) * ONE;
+        const float by = exp2_fast((m[a] - top) * c) * ONE;
 #pragma unroll
         for (int j = 0; j < DP / 16; ++j)
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[a][Columns<T, BITS, DP>::at(i, j)] = sees[a] > 0 ? acc[a][j][i] * by : 0.f;
         if (wave == 0 && g == 0 && r < n_rows) {
             float total = 0.f;
-            for (int i = 0; i < NW; ++i) total += sums[i][r].y * exp2_fast(sums[i][r].x - top);
+            for (int i = 0; i < NW; ++i) total += sums[i][r].y * exp2_fast((sums[i][r].x - top) * c);
             const bool some = total != 0.f;
             if constexpr (WHOLE) {
-                w.lse[row0 + r] = some ? top * LN2 + __logf(total) : -ATTN_INF;
-                l2[r] = some ? top + __log2f(total) : ATTN_INF;
+                w.lse[row0 + r] = some ? top * s.scale + __logf(total) : -ATTN_INF;
+                whole[r] = some ? make_float2(top, __log2f(total)) : make_float2(ATTN_INF, 0.f);
                 totals[r] = total;
             } else {
                 w.sums[partial + r] = make_float2(top, total);
@@ -491,7 +496,7 @@ __global__ __launch_bounds__(NW * 64, NR == 2 ? 3 : 4) void k_step_packed(StepSh
 #pragma unroll 4
                 for (int r = 0; r < n_rows; ++r) {
                     const f32x4 x = *(const f32x4 *)(IN_LDS ? kept + r * pitch + slot : scores + (int64_t)(slot / TS) * (TS * n_rows) + r * TS + slot % TS);
-                    for (int j = 0; j < 4; ++j) sum[j] += exp2_fast(__builtin_fmaf(x[j], c, -l2[r]));
+                    for (int j = 0; j < 4; ++j) sum[j] += exp2_fast(__builtin_fmaf(x[j] - whole[r].x, c, -whole[r].y));
                 }
                 for (int j = 1; j < 4; ++j) sum[j] = (int)slot + j < len ? sum[j] : 0.f;
             }

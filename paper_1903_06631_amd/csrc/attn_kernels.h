@@ -60,7 +60,7 @@ struct StepWork {
     const float *before;
     float *lse, *weights;
     float *outs;            // [batch, q_heads, splits, 64 or 128]; packed: [kv_heads, parts, shares, rows of a part, 64 or 128]
-    float2 *sums;           // the same without the last: maximum in base 2, sum
+    float2 *sums;           // the same without the last: maximum in base 2 (packed: of q.k), sum
     float *scores;          // [batch, q_heads, tokens, score_row] in base 2, where weights are asked for; packed: q.k [batch,
                             // kv_heads, score_row / SCORE_TILE, rows of a key head, SCORE_TILE]
     uint2 *table;           // packed: [batch] a sequence's first share, how many it has

@@ -10,24 +10,24 @@ namespace {
 
 constexpr int JOIN = 256, JOIN_WAVES = JOIN / 64, AHEAD = 8;
 
-// maximum and sum, over this many lanes next to each other
-__device__ __forceinline__ float2 join_lanes(float2 a, uint32_t lanes)
+// maximum of the products and sum, over this many lanes next to each other; c: products to exponents of two
+__device__ __forceinline__ float2 join_lanes(float2 a, uint32_t lanes, float c)
 {
     for (uint32_t d = lanes / 2; d; d >>= 1) {
         const float m = __shfl_xor(a.x, d, 64), l = __shfl_xor(a.y, d, 64), top = fmaxf(a.x, m);
-        a = make_float2(top, a.y * exp2_fast(a.x - top) + l * exp2_fast(m - top));
+        a = make_float2(top, a.y * exp2_fast((a.x - top) * c) + l * exp2_fast((m - top) * c));
     }
     return a;
 }
 // and over a row's chunks, the lane-th of `lanes`
-__device__ __forceinline__ float2 join_chunks(const float2 *sums, uint32_t n, uint32_t stride, uint32_t lane, uint32_t lanes)
+__device__ __forceinline__ float2 join_chunks(const float2 *sums, uint32_t n, uint32_t stride, uint32_t lane, uint32_t lanes, float c)
 {
     float2 a = make_float2(-__FLT_MAX__, 0.f);
 #pragma unroll 4
     for (uint32_t i = lane; i < n; i += lanes) {
         const float2 x = sums[(int64_t)i * stride];
         const float top = fmaxf(a.x, x.x);
-        a = make_float2(top, a.y * exp2_fast(a.x - top) + x.y * exp2_fast(x.x - top));
+        a = make_float2(top, a.y * exp2_fast((a.x - top) * c) + x.y * exp2_fast((x.x - top) * c));
     }
     return a;
 }
@@ -44,6 +44,7 @@ __global__ __launch_bounds__(JOIN) void k_packed_join(StepShape s, StepWork w, u
     typedef float f32xE __attribute__((ext_vector_type(E)));
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t of_one = s.q_heads * s.tokens, rows = s.batch * of_one;      // rows of queries
+    const float c = s.scale * LOG2E;
     if (blockIdx.x < row_groups) {
         __shared__ f32xE part[JOIN_WAVES][64];
         const uint32_t row = blockIdx.x * (JOIN_WAVES / waves) + wave / waves, first = wave % waves;
@@ -56,7 +57,7 @@ __global__ __launch_bounds__(JOIN) void k_packed_join(StepShape s, StepWork w, u
             const int64_t at = ((int64_t)(kvh * parts + r / of_part) * s.shares + chunks.x) * of_part + r % of_part;
             const float2 *sums = w.sums + at;
             const f32xE *outs = (const f32xE *)(w.outs + at * DP) + lane;
-            all = join_lanes(join_chunks(sums, chunks.y, of_part, lane, 64), 64);
+            all = join_lanes(join_chunks(sums, chunks.y, of_part, lane, 64, c), 64, c);
             for (uint32_t i = first; i < chunks.y; i += waves * AHEAD) {
                 f32xE x[AHEAD];
                 float m[AHEAD];
@@ -67,7 +68,7 @@ __global__ __launch_bounds__(JOIN) void k_packed_join(StepShape s, StepWork w, u
                 }
 #pragma unroll
                 for (int j = 0; j < AHEAD; ++j)
-                    if (i + j * waves < chunks.y) y += x[j] * exp2_fast(m[j] - all.x);
+                    if (i + j * waves < chunks.y) y += x[j] * exp2_fast((m[j] - all.x) * c);
             }
         }
         if (waves > 1) {
@@ -83,10 +84,10 @@ __global__ __launch_bounds__(JOIN) void k_packed_join(StepShape s, StepWork w, u
         TE z;
         for (int j = 0; j < E; ++j) z[j] = (T)(some ? y[j] / all.y : 0.f);
         if (e < s.head_dim) *(TE *)((T *)w.out.data + (int64_t)b * w.out.batch + (int64_t)head * w.out.head + (int64_t)token * w.out.row + e) = z;
-        if (lane == 0) w.lse[row] = some ? all.x * LN2 + __logf(all.y) : -ATTN_INF;
+        if (lane == 0) w.lse[row] = some ? all.x * s.scale + __logf(all.y) : -ATTN_INF;
         return;
     }
-    __shared__ float l2[MAX_GROUP];
+    __shared__ float2 whole[MAX_GROUP];      // of a row: its largest product and the logarithm to base 2 of its sum on that
     __shared__ f32x4 shares[JOIN];
     const uint32_t group = s.group;
     const uint32_t item = (blockIdx.x - row_groups) / pieces, piece = (blockIdx.x - row_groups) % pieces;
@@ -94,7 +95,6 @@ __global__ __launch_bounds__(JOIN) void k_packed_join(StepShape s, StepWork w, u
     const int len = clamp_len(s.lens, b, s.slots);
     const uint32_t quads = each / 4, share = threadIdx.x / quads, of = JOIN / quads;
     const uint32_t slot = piece * each + threadIdx.x % quads * 4;
-    const float c = s.scale * LOG2E;
     // the first scores are on their way while the sums are joined
     const float *from = w.scores + (int64_t)row0 * s.score_row + (int64_t)(slot / SCORE_TILE) * group * SCORE_TILE + slot % SCORE_TILE;
     f32x4 x[AHEAD] = {};
@@ -108,8 +108,8 @@ __global__ __launch_bounds__(JOIN) void k_packed_join(StepShape s, StepWork w, u
     for (uint32_t r = threadIdx.x / lanes; r < (group + at_once - 1) / at_once * at_once; r += at_once) {
         const uint32_t l = lane % lanes, row = min(r, group - 1);
         const float2 *sums = w.sums + ((of_head + row / of_part) * s.shares + chunks.x) * of_part + row % of_part;
-        const float2 all = join_lanes(join_chunks(sums, chunks.y, of_part, l, lanes), lanes);
-        if (l == 0 && r < group) l2[r] = all.y != 0.f ? all.x + __log2f(all.y) : ATTN_INF;
+        const float2 all = join_lanes(join_chunks(sums, chunks.y, of_part, l, lanes, c), lanes, c);
+        if (l == 0 && r < group) whole[r] = all.y != 0.f ? make_float2(all.x, __log2f(all.y)) : make_float2(ATTN_INF, 0.f);
     }
     __syncthreads();
     f32x4 sum = {};
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(JOIN) void k_packed_join(StepShape s, StepWork w, u
             for (int i = 0; i < AHEAD; ++i) {
                 const uint32_t r = r0 + i * of;
                 if (r < group)
-                    for (int j = 0; j < 4; ++j) sum[j] += exp2_fast(__builtin_fmaf(x[i][j], c, -l2[r]));
+                    for (int j = 0; j < 4; ++j) sum[j] += exp2_fast(__builtin_fmaf(x[i][j] - whole[r].x, c, -whole[r].y));
             }
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
