@@ -321,8 +321,8 @@ __global__ __launch_bounds__(NW * 64, NR == 2 ? 3 : 4) void k_step_packed(StepSh
     const float slack = 5.f / c;                         // by how much the running maximum may be left behind: 2^5
     // Maxima are those of the products, and differences are taken before the scale comes in: a scaled score may be so large that
     // 32 bits hold it to whole powers of two only, and its own maximum's exponent has to be 0 all the same.  (With scaled
-    // maxima inside the multiplication, a subtraction less for each score, 16 sequences with five tokens below took 32.9 us in
-    // place of 33.3, two long ones the same.)
+    // maxima inside the multiplication, a subtraction less for each score, the 16 sequences with five tokens took 32.9 us in
+    // place of 33.3, the two long ones the same.)
 
     f32x4 acc[NR][DP / 16] = {};
     float m[NR], l[NR];
@@ -496,7 +496,7 @@ __global__ __launch_bounds__(NW * 64, NR == 2 ? 3 : 4) void k_step_packed(StepSh
 #pragma unroll 4
                 for (int r = 0; r < n_rows; ++r) {
                     const f32x4 x = *(const f32x4 *)(IN_LDS ? kept + r * pitch + slot : scores + (int64_t)(slot / TS) * (TS * n_rows) + r * TS + slot % TS);
-                    for (int j = 0; j < 4; ++j) sum[j] += exp2_fast(__builtin_fmaf(x[j] - whole[r].x, c, -whole[r].y));
+                    for (int j = 0; j < 4; ++j) sum[j] += received(x[j], whole[r], c);
                 }
                 for (int j = 1; j < 4; ++j) sum[j] = (int)slot + j < len ? sum[j] : 0.f;
             }

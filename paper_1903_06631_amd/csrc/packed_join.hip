@@ -3,7 +3,7 @@
 // scores, 4 bytes for each slot and row of queries, are mostly still in the last cache).  Measured: 2 caches of 8 heads x 131 072
 // slots with weights of 4 query heads each 12.2 us (34 MB of scores, 17 of weights read and written), 32 of 2047 slots and 32 query heads 6.1,
 // without weights 4.3 to 5.6.
-#include "attn_core.h"
+#include "packed_rows.h"
 
 namespace lap {
 namespace {
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(JOIN) void k_packed_join(StepShape s, StepWork w, u
             for (int i = 0; i < AHEAD; ++i) {
                 const uint32_t r = r0 + i * of;
                 if (r < group)
-                    for (int j = 0; j < 4; ++j) sum[j] += exp2_fast(__builtin_fmaf(x[i][j] - whole[r].x, c, -whole[r].y));
+                    for (int j = 0; j < 4; ++j) sum[j] += received(x[i][j], whole[r], c);
             }
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {

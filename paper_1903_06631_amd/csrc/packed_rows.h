@@ -114,4 +114,13 @@ template <class T, int BITS> __device__ __forceinline__ typename Elem<T>::x8 eig
     return __builtin_bit_cast(typename Elem<T>::x8, x);
 }
 
+// What a slot receives from a row of queries: from its product, the row's largest one and the logarithm to base 2 of the row's sum on
+// that, with c, products to exponents of two.  A slot that the row does not see (minus infinity) receives nothing, also where the row's sum
+// is not a number.
+__device__ __forceinline__ float received(float x, float2 whole, float c)
+{
+    const float p = exp2_fast(__builtin_fmaf(x - whole.x, c, -whole.y));
+    return x == -ATTN_INF ? 0.f : p;
+}
+
 }  // namespace lap
