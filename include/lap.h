@@ -417,7 +417,8 @@ typedef struct {
 } lap_attention_shape;
 
 /* Bytes of workspace of a call with this shape, 256-byte aligned (0: ws may be NULL; also for a shape that is refused). */
-enum { LAP_AT_FORWARD = 0, LAP_AT_GRAD = 1, LAP_AT_WEIGHTS = 2, LAP_AT_STEP = 3, LAP_AT_STEP_PACKED = 4 };
+enum { LAP_AT_FORWARD = 0, LAP_AT_GRAD = 1, LAP_AT_WEIGHTS = 2, LAP_AT_STEP = 3, LAP_AT_STEP_PACKED = 4,
+       LAP_AT_STEP_PACKED_UNWEIGHTED = 5 };      /* of a call that asks for no weights (LAP_AT_STEP_PACKED does for both) */
 size_t lap_attention_workspace_bytes(int which_call, const lap_attention_shape *shape);
 
 /* out, and lse [batch, q_heads, q_len], which the backward pass and lap_attention_weights take. */

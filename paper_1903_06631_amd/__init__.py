@@ -37,6 +37,7 @@ from .attention_ops import (  # noqa: F401
     AT_GRAD,
     AT_STEP,
     AT_STEP_PACKED,
+    AT_STEP_PACKED_UNWEIGHTED,
     AT_WEIGHTS,
     attention,
     attention_grad,

@@ -23,7 +23,7 @@ from typing import Optional
 
 from . import binding
 
-AT_FORWARD, AT_GRAD, AT_WEIGHTS, AT_STEP, AT_STEP_PACKED = range(5)
+AT_FORWARD, AT_GRAD, AT_WEIGHTS, AT_STEP, AT_STEP_PACKED, AT_STEP_PACKED_UNWEIGHTED = range(6)
 
 
 class _Rows(C.Structure):
@@ -201,12 +201,12 @@ def _workspace(ws, need: int, index: int, like):
 
 
 def attention_workspace_bytes(which: int, q_shape, kv_shape, dtype, *, causal: bool = False) -> int:
-    """lap_attention_workspace_bytes: of a call (AT_FORWARD, AT_GRAD, AT_WEIGHTS, AT_STEP, AT_STEP_PACKED) on queries and keys of
-    these shapes, [batch, heads, length, head_dim], for a step's queries without a length.  dtype and head_dim are the elements',
+    """lap_attention_workspace_bytes: of a call (AT_FORWARD, AT_GRAD, AT_WEIGHTS, AT_STEP, AT_STEP_PACKED, or of a packed step without
+    weights AT_STEP_PACKED_UNWEIGHTED) on queries and keys of these shapes, [batch, heads, length, head_dim], for a step's queries without a length.  dtype and head_dim are the elements',
     also of a packed cache.  0: none, also where the call is refused."""
     lib = _lib()
     b, h, *n, d = q_shape
-    s = _pack_shape(_kinds[dtype], b, h, kv_shape[1], n[0] if n else 1, kv_shape[2], d, 1 if causal or which == AT_STEP_PACKED else 0, 0,
+    s = _pack_shape(_kinds[dtype], b, h, kv_shape[1], n[0] if n else 1, kv_shape[2], d, 1 if causal or which >= AT_STEP_PACKED else 0, 0,
                     1.0, 0, 0)
     return int(lib.lap_attention_workspace_bytes(which, s))
 
@@ -474,7 +474,7 @@ def attention_step_packed(q, k_cache, v_cache, weights=None, *, lens=None, posit
     else:
         results = (_rows(out["out"], "out", t, qs, index), _plain(out["lse"], "lse", torch.float32, lse, index),
                    _plain(out.get("weights"), "out weights", torch.float32, slots, index))
-    ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_STEP_PACKED, s), index, q)
+    ws, have, at = _workspace(ws, lib.lap_attention_workspace_bytes(AT_STEP_PACKED_UNWEIGHTED if weights is None else AT_STEP_PACKED, s), index, q)
     args = (s, _rows(q, "q", t, qs, index), cache, _plain(positions, "positions", torch.int32, slots, index), before, *results, at, have, _stream(index))
     rc = lib.lap_attention_step_packed(*args) if _device() == index else _on(index, lib.lap_attention_step_packed, *args)
     if rc or sync:

@@ -138,15 +138,15 @@ size_t ws_weights(const lap_attention_shape *s)
     const uint32_t parts = lap::weights_parts(shape_of(s));
     return parts == 1 ? 0 : up((size_t)s->batch * s->kv_heads * parts * s->k_len * 4);
 }
-// how much a step's outputs and sums of chunks, its scores and its table take
+// how much a step's outputs and sums of chunks, its scores (which only weights need) and its table take
 struct StepBytes {
     size_t outs, sums, scores, table;
     size_t all() const { return outs + sums + scores + table; }
 };
-StepBytes bytes_of(const lap_attention_shape *s, const lap::StepShape &p, bool packed)
+StepBytes bytes_of(const lap_attention_shape *s, const lap::StepShape &p, bool packed, bool weights)
 {
     const size_t rows = (size_t)s->batch * s->q_heads * p.tokens;
-    StepBytes n = {0, 0, up(rows * p.score_row * 4), 0};
+    StepBytes n = {0, 0, weights ? up(rows * p.score_row * 4) : 0, 0};
     if (p.whole) return n;
     const size_t partial = packed ? (size_t)s->kv_heads * lap::step_parts(p.group) * p.shares * lap::step_part(p.group) : rows * p.splits;
     n.outs = up(partial * padded_dim(s) * 4), n.sums = up(partial * sizeof(float2));
@@ -154,16 +154,16 @@ StepBytes bytes_of(const lap_attention_shape *s, const lap::StepShape &p, bool p
     return n;
 }
 // the same whether there are lengths or not
-size_t ws_step(const lap_attention_shape *s, bool packed)
+size_t ws_step(const lap_attention_shape *s, bool packed, bool weights)
 {
     static const int32_t some = 0;
     lap_attention_shape a = *s, b = *s;
     a.k_lens = nullptr, b.k_lens = &some;
-    return std::max(bytes_of(&a, step_of(&a, packed), packed).all(), bytes_of(&b, step_of(&b, packed), packed).all());
+    return std::max(bytes_of(&a, step_of(&a, packed), packed, weights).all(), bytes_of(&b, step_of(&b, packed), packed, weights).all());
 }
-void carve_step(lap::StepWork &w, const lap_attention_shape *s, const lap::StepShape &p, void *ws, bool packed)
+void carve_step(lap::StepWork &w, const lap_attention_shape *s, const lap::StepShape &p, void *ws, bool packed, bool weights)
 {
-    const StepBytes n = bytes_of(s, p, packed);
+    const StepBytes n = bytes_of(s, p, packed, weights);
     char *at = (char *)ws;
     w.outs = (float *)at, at += n.outs;
     w.sums = (float2 *)at, at += n.sums;
@@ -257,8 +257,9 @@ size_t lap_attention_workspace_bytes(int which_call, const lap_attention_shape *
     case LAP_AT_FORWARD: return up(lap::forward_workspace(shape_of(s)));
     case LAP_AT_GRAD: return ws_grad(s);
     case LAP_AT_WEIGHTS: return ws_weights(s);
-    case LAP_AT_STEP: return ws_step(s, false);
-    case LAP_AT_STEP_PACKED: return check_step_packed(s) ? 0 : ws_step(s, true);
+    case LAP_AT_STEP: return ws_step(s, false, true);
+    case LAP_AT_STEP_PACKED:
+    case LAP_AT_STEP_PACKED_UNWEIGHTED: return check_step_packed(s) ? 0 : ws_step(s, true, which_call == LAP_AT_STEP_PACKED);
     default: return 0;
     }
 }
@@ -338,12 +339,12 @@ int lap_attention_step(const lap_attention_shape *s, const lap_rows *q, const la
     if (!rc) rc = check_rows(v, s->batch, s->kv_heads, s->k_len, s->head_dim, false);
     if (!rc) rc = check_rows(out, s->batch, s->q_heads, 1, s->head_dim, true);
     if (!rc && (!lse || (before != nullptr) != (weights != nullptr))) rc = LAP_E_NULL;
-    if (!rc) rc = check_ws(ws, ws_bytes, ws_step(s, false));
+    if (!rc) rc = check_ws(ws, ws_bytes, ws_step(s, false, true));
     if (!rc && s->k_len) rc = check_apart(out->data, {k->data, v->data});
     if (rc) return rc;
     const lap::StepShape p = step_of(s, false);
     lap::StepWork w = {queries_of(s, q), keys_of(s, k), keys_of(s, v), queries_of(s, out), positions, before, lse, weights, nullptr, nullptr, nullptr, nullptr};
-    carve_step(w, s, p, ws, false);
+    carve_step(w, s, p, ws, false, true);
     LAP_HIP(lap::launch_attention_step(p, w, (hipStream_t)hip_stream));
     return LAP_OK;
 }
@@ -430,13 +431,13 @@ int lap_attention_step_packed(const lap_attention_shape *s, const lap_rows *q, c
     rc = check_rows(q, s->batch, s->q_heads, s->q_len, s->head_dim, false);
     if (!rc) rc = check_rows(out, s->batch, s->q_heads, s->q_len, s->head_dim, true);
     if (!rc && (!lse || (before != nullptr) != (weights != nullptr))) rc = LAP_E_NULL;
-    if (!rc) rc = check_ws(ws, ws_bytes, ws_step(s, true));
+    if (!rc) rc = check_ws(ws, ws_bytes, ws_step(s, true, weights != nullptr));
     if (!rc && s->k_len) rc = check_apart(out->data, {cache->k.data, cache->v.data});
     if (rc) return rc;
     const lap::StepShape p = step_of(s, true);
     lap::StepWork w = {queries_of(s, q), packed_of(cache, &cache->k), packed_of(cache, &cache->v), queries_of(s, out), positions, before, lse, weights,
                        nullptr, nullptr, nullptr, nullptr};
-    carve_step(w, s, p, ws, true);
+    carve_step(w, s, p, ws, true, weights != nullptr);
     LAP_HIP(lap::launch_attention_step_packed(p, w, cache->bits, (hipStream_t)hip_stream));
     return LAP_OK;
 }

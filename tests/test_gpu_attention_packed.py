@@ -436,3 +436,24 @@ def test_without_slots_and_many_rows(lap, b, heads, kv, tokens, d, lengths):
     lens = i32([i % 3 for i in range(b)]) if lengths else None
     got = lap.attention_step_packed(q, c, c, torch.zeros(b, kv, 0, device="cuda"), lens=lens)
     assert (got["out"] == 0).all() and torch.isneginf(got["lse"]).all() and got["weights"].shape == (b, kv, 0)
+
+
+@pytest.mark.parametrize("n,heads,tokens", [(900, 8, 1), (1000, 16, 1), (6000, 8, 3), (6000, 80, 1)])
+@pytest.mark.parametrize("lengths", [False, True])
+def test_workspace_without_weights(lap, n, heads, tokens, lengths):
+    """A workspace that just does for a call without weights, and one with room to spare: equal results, and nothing behind it is written."""
+    gen = torch.Generator().manual_seed(n)
+    b, kv = 3, 2
+    k, v, _, _ = make(lap, gen, b, kv, n, 128, BF, 4, numbers=0)
+    q = rows(gen, b, heads, tokens, 128, BF, times=1.5)
+    lens = i32([n, 0, n // 2]) if lengths else None
+    weighted = lap.attention_step_packed(q, k, v, torch.zeros(b, kv, n, device="cuda"), lens=lens)
+    need = lap.attention_workspace_bytes(lap.AT_STEP_PACKED_UNWEIGHTED, q.shape, (b, kv, n, 128), BF)
+    whole = torch.full((need + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+    for ws in (whole[:need], None):
+        got = lap.attention_step_packed(q, k, v, lens=lens, ws=ws)
+        assert torch.equal(got["out"], weighted["out"]) and torch.equal(got["lse"], weighted["lse"])
+    assert (whole[need:] == 0xA5).all()
+    if need:
+        with pytest.raises(lap.LapError):
+            lap.attention_step_packed(q, k, v, lens=lens, ws=whole[:need - 256])

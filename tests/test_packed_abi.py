@@ -126,3 +126,20 @@ def test_workspace_without_slots(q_shape, kv_shape):
     assert r.returncode == 0, f"ended with {r.returncode}: {r.stderr[-500:]}"
     need = int(r.stdout.split()[-1])
     assert need > 0 and need % 256 == 0
+
+
+def test_workspace_of_a_call_without_weights(lib):      # noqa: F811
+    """No room for the scores, which only the weights need: 64 rows of 131072 slots are more than the packed rows themselves."""
+    import torch
+    import paper_1903_06631_amd as lap
+    for q_shape, kv_shape in (((16, 32, 5, 128), (16, 8, 8192, 128)), ((2, 64, 8, 128), (2, 8, 131072, 128)), ((64, 512, 128), (64, 8, 4096, 128))):
+        need = [lap.attention_workspace_bytes(x, q_shape, kv_shape, torch.bfloat16) for x in (lap.AT_STEP_PACKED, lap.AT_STEP_PACKED_UNWEIGHTED)]
+        queries = q_shape[0] * q_shape[1] * (q_shape[2] if len(q_shape) == 4 else 1)
+        assert need[0] - need[1] == queries * kv_shape[2] * 4 and 0 < need[1] < 1 << 27
+    many, c = shape(k_len=9000), packed(slots=9000)
+    need = [lib.lap_attention_workspace_bytes(x, many) for x in (4, 5)]
+    def call(have, w):      # (the last of the checks, after the workspace's, refuses an output in the place of the keys)
+        return lib.lap_attention_step_packed(many, other(), c, None, w, rows(FAKE), FAKE, w, FAKE << 8, have, None)
+    assert need[1] < need[0] and call(need[1] - 1, None) == -3 and call(need[1], None) == -10
+    assert call(need[0] - 1, FAKE) == -3 and call(need[0], FAKE) == -10
+    assert lib.lap_attention_workspace_bytes(5, shape(causal=0)) == 0 and lib.lap_attention_workspace_bytes(6, many) == 0
