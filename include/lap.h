@@ -478,7 +478,7 @@ int lap_cache_insert(const lap_cache *cache, const lap_rows *k_new, const lap_ro
  * place of 256.  Elements of a row come in groups of 32, the last one perhaps shorter.  Of L = 2^bits - 1 levels, lo the least
  * element of a group and step the least number of the elements' type from (largest - least) / L on (the one below where
  * lo + L step would pass the type's largest), element x is held as u, the whole number nearest to (x - lo) / step, ties to even,
- * and stands for lo + u step, rounded once to the type; quotients and differences are 32-bit ones.  A group with an element that
+ * and stands for lo + u step, rounded once to binary16, or to 32 bits and then to bfloat16; quotients and differences are 32-bit ones.  A group with an element that
  * is not finite, or a range over 2^100, is not a number, all of it.  A row's bytes: the words of 32 bits of each group, `bits` of
  * them, whose low half holds the even elements from its lowest bits up and whose high half the odd ones; then lo and step of each
  * group, 16 bits each; then zeros up to a multiple of 16. */
@@ -504,8 +504,8 @@ int lap_cache_unpack(const lap_packed_cache *from, uint32_t n, const int32_t *le
  * in use: shape with the cache's sizes, k_len its slots, window 0 and up to 256 rows (query heads times q_len) to a key
  * head.  With q_len > 1, causal is 1 (row i of a sequence sees the slots below k_lens[b] - q_lens[b] + i + 1) and positions NULL; with
  * q_len 1 causal may be either.  lse [batch, q_heads, q_len]; weights are the sums over all heads and rows of the call.  A group of
- * a key that is not a number makes the rows that see its slot not numbers, one of a value their elements of that group; what
- * empty slots and those past the length hold reaches nothing.  The workspace is the same with lengths and without. */
+ * a key that is not a number makes the rows that see its slot not numbers, and the weights of the slots that these rows see; one of a
+ * value their elements of that group; what empty slots and those past the length hold reaches nothing.  The workspace is the same with lengths and without. */
 int lap_attention_step_packed(const lap_attention_shape *shape, const lap_rows *q, const lap_packed_cache *cache,
                               const int32_t *positions, const float *before, const lap_rows *out, float *lse, float *weights,
                               void *ws, size_t ws_bytes, void *hip_stream);

@@ -7,8 +7,8 @@
 // those below 2^-24 of the largest of their wave lose precision and none vanishes above 2^-35.  Sums, scores and weights are
 // 32 bits.
 //
-// Every packed row is read once.  The rows of queries that share a key head, heads times tokens, are the columns of 16 of the
-// 16x16x32 matrix instruction (C = A B, lane l with g = l / 16):
+// Every packed row is read once for each 16 rows of queries that share a key head, heads times tokens, or for each 32 where there are
+// more than 16.  These rows are the columns, 16 each, of the 16x16x32 matrix instruction (C = A B, lane l with g = l / 16):
 //   A: row l % 16, contraction indices 8 g .. 8 g + 7      B: column l % 16, the same      C: column l % 16, rows 4 g .. 4 g + 3
 // Keys are A of the scores: a lane holds a fourth of a slot's row, which is one group of 32 elements where rows have 128, so it
 // needs one lo and one step.  Values are A of the outputs, elements along the rows: a lane holds one word of eight slots,
@@ -18,8 +18,8 @@
 // next keys when these ones are decoded, for the next values likewise (with two tiles on their way, and a fourth of the waves less,
 // 64 caches of 8 heads x up to 4096 slots took 55 us in place of 50, 24 of 4 x up to 6001 of 8 bits 37 in place of 27).
 //
-// Bound by memory where caches are long, and not by much: a tile of 32 slots of 128 elements is 10 KB and some 390 vector
-// instructions in bfloat16 (270 in binary16), four cycles each, of which a third would do for rows of 16 bits.  So every
+// Bound by memory where caches are long, and not by much: a tile of 32 slots of 128 elements is 10 KB and some 400 vector
+// instructions in bfloat16 (280 in binary16), four cycles each, of which a third would do for rows of 16 bits.  So every
 // instruction of a tile counts: levels are converted two by two, loads need no addresses of their own, the running maximum is
 // left behind by up to 2^5 before sums are taken down to a new one, and lanes compare with it on their own.  Short caches are bound by a
 // launch or two and the chain of a tile, some 1.3 us.
@@ -29,9 +29,13 @@
 //
 // Measured, kernels alone, 4 bits and 128 elements where nothing else is said: 16 x 1000 slots of one sequence 12.4 us (a launch
 // and a chain of four tiles); 64 ragged sequences of 8 heads x up to 4096 slots, 4 query heads each and weights, 45 us (188 MB of rows
-// and results at 4.2 TB/s, vector instructions in 49 % of all cycles, the matrix units busy 7 %); 2 x 8 x 131 072 slots likewise 76 us and 12 to
-// join (4.9 TB/s, 38 %, 9 %); 24 ragged x 4 x up to 6001 slots of 96 in 8 bits, 8 query heads each, 19 us and 4.4; 16 ragged x 8 x up
-// to 8192 slots, five tokens of 4 query heads, 29 us and 6.0; 32 x 2047 slots of 64, 32 query heads, 10 us and 6.0.
+// and results at 4.2 TB/s, vector instructions in 51 % of all cycles, the matrix units busy 7 %); 2 x 8 x 131 072 slots likewise 76 us and 12 to
+// join (4.9 TB/s, 39 %, 9 %); 24 ragged x 4 x up to 6001 slots of 96 in 8 bits, 8 query heads each, 19 us and 4.4; 16 ragged x 8 x up
+// to 8192 slots, five tokens of 4 query heads, 30 us and 5.3; 32 x 2047 slots of 64, 32 query heads, 10 us and 6.0.
+//
+// More than 32 rows to a key head are parts of 32, workgroups of their own, of which each reads the cache from memory: the 64
+// sequences, without weights, 50 us with 16 rows and 173 MB read, 66 and 175 with 32, 111 and 351 with 40, 120 and 358 with 64, 454 and 1429 with 256.
+// The floor, the rows read once, is 35 us.
 #include "lap_dev.h"
 #include "packed_rows.h"
 

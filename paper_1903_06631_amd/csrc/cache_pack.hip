@@ -127,6 +127,9 @@ __device__ __forceinline__ Place place_of(const PackShape &s, const Rows &k, con
 // workgroups' worth 8.2 and 7.9).  More: several (unpacked 1, 2, 4 and 8 rows to a thread: 6 x 4 x up to 4099 rows of 80 in 12.3, 9.2, 8.8 and
 // 9.1 us, 2 x 8 x 131 072 in 303, 231, 245 and 252).  Many: plain rows that do not stay in the caches anyway pass them by, so
 // that packed ones, and what is written, do not make way for them (8 x 8 x up to 16 384 rows packed and unpacked 154 us, otherwise 202).
+// From 32 MiB of plain rows on, which is where unpacking alone gains: 52 MiB 10.2 us in place of 12.5, 128 MiB 26 and 27, 256 MiB 50 and 63.  Where attention
+// reads the unpacked rows next it would be from some 256 MiB on: both calls, 8 key heads and 16 (512) new tokens of 32 query heads, 52 MiB 48 (181) us
+// and with rows that stay 42 (158), 128 MiB 91 (422) and 79 (373), 256 MiB 170 (849) and 186 (819).
 enum class How { FEW, SOME, PASSING };
 __host__ __device__ constexpr int rows_of_thread(How how, bool write) { return how == How::FEW ? 1 : write || how == How::SOME ? 4 : 2; }
 

@@ -2,7 +2,7 @@
 //
 // Elements come in groups of 32 (the last one of a row perhaps shorter).  Of L = 2^bits - 1 levels, lo the least element and
 // step the least number of the elements' type from (largest - least) / L on, element x is held as u, the whole number
-// nearest to (x - lo) / step, and stands for lo + u step, rounded once.  Bytes of a row: the words of all groups, `bits` of 32
+// nearest to (x - lo) / step, and stands for lo + u step, rounded once (binary16) or to 32 bits and then to the type (bfloat16).  Bytes of a row: the words of all groups, `bits` of 32
 // bits for each; then lo and step of each group, 16 bits each; then zeros up to a multiple of 16.
 //
 // A word's low half holds its even elements from the lowest bits up, its high half the odd ones at the same places.  So one
